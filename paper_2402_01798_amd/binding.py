@@ -26,8 +26,10 @@ except ImportError as e:                # the loops below do the same, slower
 LIB_PATH = os.environ.get("TQ_LIBRARY_PATH") or os.path.join(HERE, "libtq.so")
 
 OK, EINVAL, EALIGN, EUNSUPPORTED, EHIP = 0, 1, 2, 3, 4
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2                # F16: the calls of tq_mx.h and tq_distill.h only
 GRID_UNIFORM, GRID_NONUNIFORM, GRID_BISCALED = 0, 1, 2
+MX_NEAREST, MX_STOCHASTIC = 0, 1
+DISTILL_MAX_TOP = 1024
 NBINS = 898
 MAX_WORKERS = 64
 STATS_BYTES = 3632
@@ -95,6 +97,21 @@ def lib():
             f.restype = i32
         for f in (L.tq_stats, L.tq_stats_static, L.tq_params, L.tq_compress, L.tq_decompress_aggregate,
                   L.tq_decompress_aggregate_update, L.tq_stats_multi, L.tq_params_multi, L.tq_compress_multi):
+            f.restype = i32
+        L.tq_mx_code_bytes.argtypes = L.tq_mx_scale_bytes.argtypes = [u64, u64]
+        L.tq_mx_quantize.argtypes = [vp, i32, u64, u64, u64, i32, u64, u32, u32, vp, vp, vp, vp, vp]
+        L.tq_mx_dequantize.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
+        L.tq_mx_matmul_workspace_bytes.argtypes = L.tq_mx_linear_workspace_bytes.argtypes = [u64, u64, u64]
+        for f in (L.tq_mx_code_bytes, L.tq_mx_scale_bytes, L.tq_mx_matmul_workspace_bytes, L.tq_mx_linear_workspace_bytes):
+            f.restype = u64
+        L.tq_mx_matmul.argtypes = [vp, vp, vp, vp, u64, u64, u64, vp, u64, vp, i32, u64, vp, u64, vp]
+        L.tq_mx_linear.argtypes = [vp, i32, u64, u64, vp, vp, u64, u64, vp, i32, u64, vp, u64, vp]
+        distill = [vp, i32, u64, u64, u64, vp, i32, vp, u64, f32]
+        L.tq_distill_forward.argtypes = distill + [vp, vp, vp]
+        L.tq_distill_backward.argtypes = distill + [vp, vp, vp, u64, vp]
+        L.tq_distill.argtypes = distill + [vp, vp, vp, u64, vp]
+        for f in (L.tq_mx_quantize, L.tq_mx_dequantize, L.tq_mx_matmul, L.tq_mx_linear, L.tq_distill_forward,
+                  L.tq_distill_backward, L.tq_distill):
             f.restype = i32
         for name in _NATIVE:
             f = getattr(L, name)
@@ -502,6 +519,162 @@ def tq_decompress_aggregate_segments(payloads, params, seg, out, bits, weights=N
     _check(lib().tq_decompress_aggregate_segments(pp, qq, ww, N, d, dev, host, nseg, bits, int(bool(accumulate)),
                                                   _dev(out, "out"), _stream()), "tq_decompress_aggregate_segments")
     return out
+
+
+# Microscaled 4-bit matrices (tq_mx.h) and distillation (tq_distill.h).  Matrices are 2-D tensors whose rows may be apart (a slice
+# of a wider one); the elements of a row are not.
+
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _matrix(t, what):
+    """(address, type code, rows, cols, row length)"""
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (what, t.dtype))
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions" % what)
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if not t.is_cuda or (step != 1 and cols > 1):
+        raise ValueError("%s must be a device tensor with contiguous rows" % what)
+    if rows <= 1:
+        ld = max(ld, cols)                  # a single row's stride says nothing
+    if ld < cols:
+        raise ValueError("the rows of %s overlap" % what)
+    return t.data_ptr(), code, rows, cols, ld
+
+
+class MxMatrix:
+    """A matrix [rows, cols] in microscaled 4-bit form: ``codes`` uint8 [rows, 64 G], ``scales`` uint8 [G, rows, 4], G groups of
+    128 elements in a row (see tq_mx.h)."""
+
+    __slots__ = ("codes", "scales", "rows", "cols")
+
+    def __init__(self, codes, scales, rows, cols):
+        groups = -(-cols // 128)
+        if rows < 1 or cols < 1:
+            raise ValueError("a matrix in 4-bit form has elements")
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        if tuple(codes.shape) != (rows, 64 * groups) or tuple(scales.shape) != (groups, rows, 4):
+            raise ValueError("codes and scales do not match a [%d, %d] matrix" % (rows, cols))
+        _dev(codes, "codes")
+        _dev(scales, "scales")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+
+    def args(self):
+        return self.codes.data_ptr(), self.scales.data_ptr()
+
+
+def alloc_mx(rows, cols, device="cuda"):
+    groups = -(-cols // 128)
+    return MxMatrix(torch.empty((rows, 64 * groups), dtype=torch.uint8, device=device),
+                    torch.empty((groups, rows, 4), dtype=torch.uint8, device=device), rows, cols)
+
+
+def mx_matmul_workspace_bytes(m, n, k):
+    return int(lib().tq_mx_matmul_workspace_bytes(m, n, k))
+
+
+def mx_linear_workspace_bytes(m, n, k):
+    return int(lib().tq_mx_linear_workspace_bytes(m, n, k))
+
+
+def _scratch(workspace):
+    return (None, 0) if workspace is None else (_dev(workspace, "workspace") or None, workspace.nbytes)
+
+
+def tq_mx_quantize(x, form, form_t=None, rounding=MX_NEAREST, seed=0, worker=0, step=0):
+    """``form`` takes x [rows, cols], ``form_t`` its transpose; either may be None."""
+    px, code, rows, cols, ld = _matrix(x, "x")
+    if form is not None and (form.rows != rows or form.cols != cols):
+        raise ValueError("form must be [%d, %d]" % (rows, cols))
+    if form_t is not None and (form_t.rows != cols or form_t.cols != rows):
+        raise ValueError("form_t must be [%d, %d]" % (cols, rows))
+    none = (None, None)
+    _check(lib().tq_mx_quantize(px, code, rows, cols, ld, rounding, seed, worker, step, *(none if form is None else form.args()),
+                                *(none if form_t is None else form_t.args()), _stream()), "tq_mx_quantize")
+    return form, form_t
+
+
+def tq_mx_dequantize(form, out):
+    po, code, rows, cols, ld = _matrix(out, "out")
+    if (rows, cols) != (form.rows, form.cols):
+        raise ValueError("out must be [%d, %d]" % (form.rows, form.cols))
+    _check(lib().tq_mx_dequantize(*form.args(), rows, cols, po, code, ld, _stream()), "tq_mx_dequantize")
+    return out
+
+
+def tq_mx_matmul(a, b, out, workspace=None, add=None):
+    """out [m, n] = a [m, k] b [n, k]^T (+ add, float32, which may be out)."""
+    po, code, m, n, ld = _matrix(out, "out")
+    if a.cols != b.cols or a.rows != m or b.rows != n:
+        raise ValueError("[%d, %d] times [%d, %d]^T does not fit out [%d, %d]" % (a.rows, a.cols, b.rows, b.cols, m, n))
+    pd, lda = None, 0
+    if add is not None:
+        pd, acode, am, an, lda = _matrix(add, "add")
+        if acode != F32 or (am, an) != (m, n):
+            raise ValueError("add must be float32 of out's shape")
+    _check(lib().tq_mx_matmul(*a.args(), *b.args(), m, n, a.cols, pd, lda, po, code, ld, *_scratch(workspace), _stream()),
+           "tq_mx_matmul")
+    return out
+
+
+def tq_mx_linear(x, w, out, workspace=None):
+    """out [m, n] = Q(x [m, k]) w [n, k]^T, Q the nearest rounding to 4-bit form."""
+    px, code, m, k, ldx = _matrix(x, "x")
+    po, ocode, om, n, ldo = _matrix(out, "out")
+    if w.cols != k or w.rows != n or om != m:
+        raise ValueError("[%d, %d] times [%d, %d]^T does not fit out [%d, %d]" % (m, k, w.rows, w.cols, om, n))
+    _check(lib().tq_mx_linear(px, code, m, ldx, *w.args(), n, k, po, ocode, ldo, *_scratch(workspace), _stream()), "tq_mx_linear")
+    return out
+
+
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def _distill_args(z, ids, t, temperature, **per_row):
+    pz, code, rows, vocab, ldz = _matrix(z, "z")
+    id_bytes = _ID_BYTES.get(ids.dtype)
+    if id_bytes is None or t.dtype != torch.float32:
+        raise TypeError("ids must be int32 or int64, t float32")
+    if ids.dim() != 2 or ids.shape[0] != rows or t.shape != ids.shape:
+        raise ValueError("ids and t must be [%d, top]" % rows)
+    for name, v in per_row.items():
+        if v.dtype != torch.float32:
+            raise TypeError("%s must be float32" % name)
+        if v.numel() != (2 * rows if name == "stats" else rows):
+            raise ValueError("%s must have %s a row" % (name, "two elements" if name == "stats" else "one element"))
+    return (pz, code, rows, vocab, ldz, _dev(ids, "ids"), id_bytes, _dev(t, "t"), ids.shape[1], temperature), \
+        tuple(_dev(v, name) for name, v in per_row.items())
+
+
+def _gradient(z, dz):
+    pd, code, rows, cols, ld = _matrix(dz, "dz")
+    if dz.dtype != z.dtype or dz.shape != z.shape:
+        raise ValueError("dz must have z's type and shape")
+    return pd, ld
+
+
+def tq_distill_forward(z, ids, t, loss, stats, temperature=1.0):
+    """``stats`` [rows, 2]: what tq_distill_backward needs of the row."""
+    args, out = _distill_args(z, ids, t, temperature, loss=loss, stats=stats)
+    _check(lib().tq_distill_forward(*args, *out, _stream()), "tq_distill_forward")
+    return loss, stats
+
+
+def tq_distill_backward(z, ids, t, stats, grad, dz, temperature=1.0):
+    """``dz`` may be ``z``."""
+    args, rows = _distill_args(z, ids, t, temperature, stats=stats, grad=grad)
+    _check(lib().tq_distill_backward(*args, *rows, *_gradient(z, dz), _stream()), "tq_distill_backward")
+    return dz
+
+
+def tq_distill(z, ids, t, grad, loss, dz, temperature=1.0):
+    """Loss and gradient in one call; ``dz`` may be ``z``."""
+    args, rows = _distill_args(z, ids, t, temperature, grad=grad, loss=loss)
+    _check(lib().tq_distill(*args, *rows, *_gradient(z, dz), _stream()), "tq_distill")
+    return loss, dz
 
 
 def stats_to_numpy(stats):

@@ -19,7 +19,8 @@ FOLD_TEST_LIB = os.path.join(HERE, "libtq_foldtest.so")
 
 MARSHAL = os.path.join(HERE, "_tq_marshal.so")
 
-SOURCES = ["tq_api.hip", "tq_stats.hip", "tq_params.hip", "tq_compress.hip", "tq_decode.hip"]
+LEARN_SOURCES = ["tq_learn_api.hip", "tq_mx_cast.hip", "tq_mx_matmul.hip", "tq_distill.hip"]
+SOURCES = ["tq_api.hip", "tq_stats.hip", "tq_params.hip", "tq_compress.hip", "tq_decode.hip"] + LEARN_SOURCES
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -39,11 +40,13 @@ def build(force: bool = False, extra_flags=(), verbose: bool = False, lib: str =
     os.makedirs(obj_dir, exist_ok=True)
     headers = [os.path.join(ROOT, "include", "tq.h"), os.path.join(CSRC, "tq_device.h"),
                os.path.join(CSRC, "tq_layout.h"), __file__]
+    learn_headers = [os.path.join(ROOT, "include", "tq_mx.h"), os.path.join(ROOT, "include", "tq_distill.h"),
+                     os.path.join(CSRC, "tq_mx_device.h")]
 
     def compile_one(src):
         s = os.path.join(CSRC, src)
         o = os.path.join(obj_dir, src.replace(".hip", ".o"))
-        if force or _stale(o, [s] + headers):
+        if force or _stale(o, [s] + headers + (learn_headers if src in LEARN_SOURCES else [])):
             cmd = [HIPCC, *FLAGS, *extra_flags, "-c", s, "-o", o]
             if verbose:
                 print(" ".join(cmd))

@@ -1,0 +1,250 @@
+// Matrices to microscaled 4-bit form and back (tq_mx.h).
+#include "tq_mx_device.h"
+
+namespace tq {
+namespace {
+
+struct CastArgs {
+    const void* x;
+    uint8_t *codes, *scales, *codes_t, *scales_t;
+    uint64_t ld;
+    uint32_t rows, cols, groups, groups_t;     // groups of 128 along a row, along a column
+    uint32_t k0, k1, worker, step;
+    uint32_t tiles_x, log_lanes;               // rows kernel: workgroups along a row, lanes along a row
+    uint64_t tiles;
+};
+
+// Along the rows: a lane takes 8 elements, four lanes a block, 16 lanes a group.  A workgroup is 2^log_lanes lanes along a row
+// times as many rows as fit.
+template <int DTYPE, bool STOCHASTIC, bool VEC>
+__global__ __launch_bounds__(256) void mx_cast_rows_kernel(CastArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    const uint32_t block = linear_block();
+    if (block >= a.tiles) return;
+    const uint32_t lane = threadIdx.x & ((1u << a.log_lanes) - 1), sub = threadIdx.x >> a.log_lanes;
+    const uint32_t by = block / a.tiles_x, bx = block - by * a.tiles_x;
+    const uint64_t row = (uint64_t)by * (256u >> a.log_lanes) + sub;
+    const uint32_t oct = (bx << a.log_lanes) + lane;             // which 8 elements of the row
+    if (row >= a.rows || oct >= a.groups * 16) return;           // 16 lanes of a group leave together
+    const int n = (int)min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8);
+    float v[8];
+    load8<DTYPE, VEC>(static_cast<const T*>(a.x) + row * a.ld + (uint64_t)oct * 8, n, v);
+    uint32_t draws[4] = {};
+    if constexpr (STOCHASTIC) philox4x32_10(oct, (uint32_t)row, a.worker, a.step, a.k0, a.k1, draws);
+    uint32_t largest = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
+    largest = quad_max(largest);
+    const uint32_t byte = mx_scale_byte<STOCHASTIC>(largest);
+    const uint32_t w = mx_codes<STOCHASTIC>(v, byte, draws);
+    reinterpret_cast<uint32_t*>(a.codes)[row * (a.groups * 16) + oct] = w;
+    if ((oct & 3) == 0) a.scales[((uint64_t)(oct / 16) * a.rows + row) * 4 + (oct / 4 & 3)] = (uint8_t)byte;
+}
+
+// Along the columns, or both ways: a workgroup takes 128 x 128 elements, a wavefront 32 rows of them, which are whole blocks in
+// either direction.  Lane 4 c + r of a wavefront holds columns 8 c .. 8 c + 7 of rows 8 r .. 8 r + 7: a row's block is
+// four lanes 4 apart, a column's four neighbouring lanes.  The transposed codes go through LDS, so that a column's 64 bytes are
+// written at once.
+template <int DTYPE, bool STOCHASTIC, bool VEC, bool ROWS>
+__global__ __launch_bounds__(256) void mx_cast_tile_kernel(CastArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    __shared__ uint32_t codes_t[128][17];                        // 16 words of a column; one more against bank conflicts
+    __shared__ uint8_t scale_t[128][4], scale[128][4];
+    const uint32_t block = linear_block();
+    if (block >= a.tiles) return;
+    const uint32_t ty = block / a.tiles_x, tx = block - ty * a.tiles_x;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 2, r = lane & 3;
+    const uint32_t row0 = ty * 128 + wave * 32 + r * 8, oct = tx * 16 + c;
+    const int n = (int)max(min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8), (int64_t)0);
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t row = row0 + i;
+        load8<DTYPE, VEC>(static_cast<const T*>(a.x) + (uint64_t)min(row, a.rows - 1) * a.ld + (uint64_t)oct * 8, row < a.rows ? n : 0, v[i]);
+    }
+    uint32_t byte_t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        uint32_t largest = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude_bits(v[i][j]));
+        byte_t[j] = mx_scale_byte<STOCHASTIC>(quad_max(largest));
+        if (r == 0) scale_t[c * 8 + j][wave] = (uint8_t)byte_t[j];
+    }
+    uint32_t w_t[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t row = row0 + i;
+        uint32_t draws[4] = {};
+        if constexpr (STOCHASTIC) philox4x32_10(oct, row, a.worker, a.step, a.k0, a.k1, draws);
+        if constexpr (ROWS) {
+            uint32_t largest = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[i][j]));
+            const uint32_t byte = mx_scale_byte<STOCHASTIC>(stride4_max(largest));
+            const uint32_t w = mx_codes<STOCHASTIC>(v[i], byte, draws);
+            if (row < a.rows) reinterpret_cast<uint32_t*>(a.codes)[(uint64_t)row * (a.groups * 16) + oct] = w;
+            if ((c & 3) == 0) scale[wave * 32 + r * 8 + i][c / 4] = (uint8_t)byte;
+        }
+        if constexpr (STOCHASTIC) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t d = j & 1 ? draws[j / 2] >> 16 : draws[j / 2] & 0xFFFFu;
+                w_t[j] |= (mx_draw(v[i][j], (int)byte_t[j], d) | (__float_as_uint(v[i][j]) >> 28 & 8u)) << (4 * i);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (!STOCHASTIC) {
+            const float column[8] = {v[0][j], v[1][j], v[2][j], v[3][j], v[4][j], v[5][j], v[6][j], v[7][j]};
+            const uint32_t none[4] = {};
+            w_t[j] = mx_codes<false>(column, byte_t[j], none);
+        } else if (byte_t[j] == 255) {
+            w_t[j] = 0;
+        }
+        codes_t[c * 8 + j][wave * 4 + r] = w_t[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t column = h * 64 + threadIdx.x / 4, piece = threadIdx.x & 3;
+        const uint64_t out = (uint64_t)tx * 128 + column;
+        if (out < a.cols) {
+            const uint32_t* p = &codes_t[column][piece * 4];
+            *reinterpret_cast<u32x4*>(a.codes_t + (out * a.groups_t + ty) * 64 + piece * 16) = u32x4{p[0], p[1], p[2], p[3]};
+        }
+    }
+    if (threadIdx.x < 128) {
+        const uint64_t column = (uint64_t)tx * 128 + threadIdx.x;
+        if (column < a.cols)
+            *reinterpret_cast<uint32_t*>(a.scales_t + ((uint64_t)ty * a.cols + column) * 4) = *reinterpret_cast<const uint32_t*>(scale_t[threadIdx.x]);
+    } else if (ROWS) {
+        const uint64_t row = (uint64_t)ty * 128 + (threadIdx.x - 128);
+        if (row < a.rows)
+            *reinterpret_cast<uint32_t*>(a.scales + ((uint64_t)tx * a.rows + row) * 4) = *reinterpret_cast<const uint32_t*>(scale[threadIdx.x - 128]);
+    }
+}
+
+// Back: a lane takes 8 elements, as in mx_cast_rows_kernel.
+template <int DTYPE, bool VEC>
+__global__ __launch_bounds__(256) void mx_dequantize_kernel(CastArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    const uint32_t block = linear_block();
+    if (block >= a.tiles) return;
+    const uint32_t lane = threadIdx.x & ((1u << a.log_lanes) - 1), sub = threadIdx.x >> a.log_lanes;
+    const uint32_t by = block / a.tiles_x, bx = block - by * a.tiles_x;
+    const uint64_t row = (uint64_t)by * (256u >> a.log_lanes) + sub;
+    const uint32_t oct = (bx << a.log_lanes) + lane;
+    if (row >= a.rows || (uint64_t)oct * 8 >= a.cols) return;
+    const uint32_t w = reinterpret_cast<const uint32_t*>(a.codes)[row * (a.groups * 16) + oct];
+    const uint32_t byte = a.scales[((uint64_t)(oct / 16) * a.rows + row) * 4 + (oct / 4 & 3)];
+    float v[8];
+    // A power of two from its byte: the smallest is a subnormal number, 255 is NaN.
+    const float scale = __uint_as_float(byte == 255 ? 0x7FC00000u : byte == 0 ? 0x00400000u : byte << 23);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f32x2 p;
+        if (j == 0) p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+        else if (j == 1) p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+        else if (j == 2) p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+        else p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+        v[2 * j] = p.x * scale;
+        v[2 * j + 1] = p.y * scale;
+    }
+    const int n = (int)min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8);
+    store8<DTYPE, VEC>(static_cast<T*>(const_cast<void*>(a.x)) + row * a.ld + (uint64_t)oct * 8, n, v);
+}
+
+template <int DTYPE, bool STOCHASTIC, bool VEC>
+void launch_cast(const CastArgs& a, bool rows, bool cols, dim3 grid, hipStream_t st)
+{
+    if (!cols) mx_cast_rows_kernel<DTYPE, STOCHASTIC, VEC><<<grid, 256, 0, st>>>(a);
+    else if (rows) mx_cast_tile_kernel<DTYPE, STOCHASTIC, VEC, true><<<grid, 256, 0, st>>>(a);
+    else mx_cast_tile_kernel<DTYPE, STOCHASTIC, VEC, false><<<grid, 256, 0, st>>>(a);
+}
+
+template <int DTYPE>
+void launch_cast(const CastArgs& a, bool stochastic, bool vec, bool rows, bool cols, dim3 grid, hipStream_t st)
+{
+    if (stochastic) vec ? launch_cast<DTYPE, true, true>(a, rows, cols, grid, st) : launch_cast<DTYPE, true, false>(a, rows, cols, grid, st);
+    else vec ? launch_cast<DTYPE, false, true>(a, rows, cols, grid, st) : launch_cast<DTYPE, false, false>(a, rows, cols, grid, st);
+}
+
+// Lanes along a row and workgroups of the kernels that go along the rows.
+bool rows_grid(CastArgs& a, uint64_t octs, dim3& grid)
+{
+    a.log_lanes = 4;
+    while (a.log_lanes < 8 && (1ull << a.log_lanes) < octs) ++a.log_lanes;
+    a.tiles_x = (uint32_t)((octs + (1ull << a.log_lanes) - 1) >> a.log_lanes);
+    const uint64_t per = 256u >> a.log_lanes;
+    a.tiles = a.tiles_x * ((a.rows + per - 1) / per);
+    return fold_grid(a.tiles, 256, 1, grid);
+}
+
+bool whole_lines(const void* p, uint64_t ld, int dtype)
+{
+    const uint64_t size = dtype == TQ_F32 ? 4 : 2;
+    return ((reinterpret_cast<uintptr_t>(p) | ld * size) & 15u) == 0;
+}
+
+}  // namespace
+}  // namespace tq
+
+hipError_t tq_launch_mx_quantize(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ld, int rounding, uint64_t seed,
+                                 uint32_t worker, uint32_t step, void* codes, void* scales, void* codes_t, void* scales_t,
+                                 hipStream_t st)
+{
+    using namespace tq;
+    CastArgs a = {};
+    a.x = x;
+    a.codes = static_cast<uint8_t*>(codes);
+    a.scales = static_cast<uint8_t*>(scales);
+    a.codes_t = static_cast<uint8_t*>(codes_t);
+    a.scales_t = static_cast<uint8_t*>(scales_t);
+    a.ld = ld;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.groups = (uint32_t)((cols + kMxGroup - 1) / kMxGroup);
+    a.groups_t = (uint32_t)((rows + kMxGroup - 1) / kMxGroup);
+    a.k0 = (uint32_t)seed;
+    a.k1 = (uint32_t)(seed >> 32);
+    a.worker = worker;
+    a.step = step;
+    dim3 grid;
+    if (codes_t) {
+        a.tiles_x = a.groups;
+        a.tiles = (uint64_t)a.groups * a.groups_t;
+        if (!fold_grid(a.tiles, 256, 1, grid)) return hipErrorInvalidValue;
+    } else if (!rows_grid(a, (uint64_t)a.groups * 16, grid)) {
+        return hipErrorInvalidValue;
+    }
+    const bool vec = whole_lines(x, ld, dtype), stochastic = rounding == TQ_MX_STOCHASTIC;
+    if (dtype == TQ_F32) launch_cast<TQ_F32>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
+    else if (dtype == TQ_BF16) launch_cast<TQ_BF16>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
+    else launch_cast<TQ_F16>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
+    return hipGetLastError();
+}
+
+hipError_t tq_launch_mx_dequantize(const void* codes, const void* scales, uint64_t rows, uint64_t cols, void* out, int dtype,
+                                   uint64_t ldo, hipStream_t st)
+{
+    using namespace tq;
+    CastArgs a = {};
+    a.x = out;
+    a.codes = static_cast<uint8_t*>(const_cast<void*>(codes));
+    a.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
+    a.ld = ldo;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.groups = (uint32_t)((cols + kMxGroup - 1) / kMxGroup);
+    dim3 grid;
+    if (!rows_grid(a, (cols + 7) / 8, grid)) return hipErrorInvalidValue;
+    const bool vec = whole_lines(out, ldo, dtype);
+    if (dtype == TQ_F32) vec ? mx_dequantize_kernel<TQ_F32, true><<<grid, 256, 0, st>>>(a) : mx_dequantize_kernel<TQ_F32, false><<<grid, 256, 0, st>>>(a);
+    else vec ? mx_dequantize_kernel<TQ_BF16, true><<<grid, 256, 0, st>>>(a) : mx_dequantize_kernel<TQ_BF16, false><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}

@@ -1,0 +1,106 @@
+"""Plain 64-bit statements of the 4-bit matrix format and of distillation, written from their definitions (tq_mx.h,
+tq_distill.h), for the tests of the kernels."""
+import numpy as np
+import torch
+
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}      # p bits of significand: 2^-p of a value in [1, 2)
+
+
+def philox(c0, c1, c2, c3, seed):
+    """Philox4x32-10 on Python integers: four words."""
+    m = 0xFFFFFFFF
+    k0, k1 = seed & m, seed >> 32 & m
+    for _ in range(10):
+        p0, p1 = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = p1 >> 32 ^ c1 ^ k0, p1 & m, p0 >> 32 ^ c3 ^ k1, p0 & m
+        k0, k1 = k0 + 0x9E3779B9 & m, k1 + 0xBB67AE85 & m
+    return c0, c1, c2, c3
+
+
+def draws(rows, cols, seed, worker, step):
+    out = np.zeros((rows, -(-cols // 8) * 8), dtype=np.int64)
+    for i in range(rows):
+        for j in range(0, cols, 8):
+            for w, word in enumerate(philox(j // 8, i, worker, step, seed)):
+                out[i, j + 2 * w], out[i, j + 2 * w + 1] = word & 0xFFFF, word >> 16
+    return out[:, :cols]
+
+
+def mx_form(x, r=None):
+    """(codes [rows, 64 G], scales [G, rows, 4]) of a float64 matrix that float32 holds; r = draws for stochastic rounding."""
+    rows, cols = x.shape
+    groups = -(-cols // 128)
+    nibbles = np.zeros((rows, groups * 128), dtype=np.uint8)
+    scales = np.zeros((groups, rows, 4), dtype=np.uint8)
+    for i in range(rows):
+        for j in range(0, cols, 32):
+            v = x[i, j:j + 32]
+            a = np.abs(v)
+            if not np.isfinite(a).all():
+                scales[j // 128, i, j // 32 % 4] = 255
+                continue
+            largest = a.max()
+            if largest > 0:
+                mantissa, e = np.frexp(largest)             # in [0.5, 1): largest = mantissa 2^e
+                e = e - 3 + (1 if r is not None and mantissa > 0.75 else 0)
+                byte = max(int(e) + 127, 0)
+            else:
+                byte = 0
+            scales[j // 128, i, j // 32 % 4] = byte
+            t = a * 2.0 ** (127 - byte)
+            for n, tn in enumerate(t):
+                low = int(np.searchsorted(GRID, min(tn, 6.0), side="right")) - 1
+                if low == 7:
+                    code = 7
+                else:
+                    share = (tn - GRID[low]) / (GRID[low + 1] - GRID[low])
+                    if r is None:
+                        up = share > 0.5 or (share == 0.5 and low % 2 == 1)
+                    else:
+                        up = int(np.floor(share * 65536)) + int(r[i, j + n]) >= 65536
+                    code = low + up
+                nibbles[i, j + n] = code + (8 if np.signbit(v[n]) else 0)
+    return nibbles[:, 0::2] | nibbles[:, 1::2] << 4, scales
+
+
+def mx_values(codes, scales, cols):
+    rows = codes.shape[0]
+    nibbles = np.stack([codes & 15, codes >> 4], axis=2).reshape(rows, -1)[:, :cols]
+    s = scales.astype(np.float64).transpose(1, 0, 2).reshape(rows, -1)
+    power = np.where(s == 255, np.nan, 2.0 ** (s - 127)).repeat(32, axis=1)[:, :cols]
+    return np.where(nibbles >= 8, -1.0, 1.0) * GRID[nibbles & 7] * power
+
+
+def product_bound(a, b, k, out, ref):
+    """How far a product of exact terms may be off: k additions in 32 bits, each off by one unit at most, and the rounding."""
+    return k * 2.0 ** -23 * (np.abs(a) @ np.abs(b).T) + 1.001 * HALF_ULP[out] * np.abs(ref) + (2.0 ** -25 if out == "f16" else 0.0)
+
+
+def distill(z, ids, t, tau, grad=None):
+    """(loss, stats [rows, 2], dz, q) in float64, as tq_distill.h defines them."""
+    rows, vocab = z.shape
+    loss, stats, dz, all_q = np.zeros(rows), np.zeros((rows, 2)), np.zeros((rows, vocab)), np.zeros((rows, vocab))
+    for i in range(rows):
+        with np.errstate(all="ignore"):
+            peak = z[i].max()
+            x = np.full(vocab, -np.inf) if peak == -np.inf else (z[i] - peak) / tau
+            log_sum = np.log(np.exp(x).sum())
+            stats[i] = peak, log_sum
+            q = all_q[i] = np.zeros(vocab) if peak == -np.inf else np.exp(x - log_sum)
+            there = (ids[i] >= 0) & (ids[i] < vocab) & (t[i] != -np.inf)
+            if not there.any():
+                continue
+            e = np.exp(t[i][there] / tau - (t[i][there] / tau).max())
+            p, place = e / e.sum(), ids[i][there]
+            if np.isnan(p).any():
+                loss[i] = np.nan
+            for pn, at in zip(p, place):
+                if pn > 0:
+                    loss[i] += tau * tau * pn * (np.log(pn) - (-np.inf if peak == -np.inf else x[at] - log_sum))
+            if grad is not None and grad[i] != 0:
+                teacher = np.zeros(vocab)
+                np.add.at(teacher, place, p)
+                dz[i] = np.nan if np.isnan(p).any() else tau * grad[i] * (q - teacher)
+    return loss, stats, dz, all_q
