@@ -1,4 +1,6 @@
 // Products of microscaled 4-bit matrices (tq_mx.h): out = A B^T (+ add).
+#include <type_traits>
+
 #include "tq_mx_device.h"
 
 namespace tq {
@@ -9,11 +11,12 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct MatmulArgs {
+    const void* x;                 // tokens that are not in 4-bit form yet, in place of a and sa
     const uint8_t *a, *sa, *b, *sb;
     const float* add;
     void* out;
-    uint64_t lda, ldo;
-    uint32_t m, n, groups;
+    uint64_t ldx, lda, ldo;
+    uint32_t m, n, k, groups;
     uint32_t tiles_x;
     uint64_t tiles;
 };
@@ -37,28 +40,349 @@ __device__ __forceinline__ void store_one(const MatmulArgs& g, uint32_t row, uin
     static_cast<typename E::type*>(g.out)[row * g.ldo + col] = E::store(v);
 }
 
-// A wavefront's 32 x 32 outputs straight from memory.
-template <int DTYPE>
-__global__ __launch_bounds__(64) void mx_matmul_direct_kernel(MatmulArgs g)
+typedef __attribute__((address_space(1))) const void global_bytes;
+typedef __attribute__((address_space(3))) void lds_bytes;
+
+// Which tile this workgroup takes.  Workgroups go to the 8 dies in turn; each die takes a run of tiles, which goes down 4 tiles and
+// then on to the next column, so that the tiles at work on a die at a time share their rows in its cache.
+__device__ __forceinline__ bool find_tile(const MatmulArgs& g, uint32_t& ty, uint32_t& tx)
 {
-    const uint32_t block = linear_block();
-    if (block >= g.tiles) return;
-    const uint32_t ty = block / g.tiles_x, tx = block - ty * g.tiles_x;
-    const uint32_t lane = threadIdx.x, r = lane & 31, half = lane >> 5;
-    const uint32_t ra = min(ty * 32 + r, g.m - 1), rb = min(tx * 32 + r, g.n - 1);      // rows past the end repeat the last
-    const uint8_t* pa = g.a + (uint64_t)ra * g.groups * 64 + half * 16;
-    const uint8_t* pb = g.b + (uint64_t)rb * g.groups * 64 + half * 16;
-    f32x16 acc = {};
-    for (uint32_t i = 0; i < g.groups; ++i) {
-        const int sa = *reinterpret_cast<const int*>(g.sa + ((uint64_t)i * g.m + ra) * 4) >> (8 * half);
-        const int sb = *reinterpret_cast<const int*>(g.sb + ((uint64_t)i * g.n + rb) * 4) >> (8 * half);
-        const i32x4* qa = reinterpret_cast<const i32x4*>(pa + (uint64_t)i * 64);
-        const i32x4* qb = reinterpret_cast<const i32x4*>(pb + (uint64_t)i * 64);
-        acc = mfma32<0>(qa[0], qb[0], acc, sa, sb);
-        acc = mfma32<2>(qa[2], qb[2], acc, sa, sb);
+    const uint32_t block = linear_block(), per = (uint32_t)(g.tiles + 7) / 8, tile = (block & 7) * per + (block >> 3);
+    if (block >= 8 * per || tile >= g.tiles) return false;
+    const uint32_t tiles_y = (uint32_t)(g.tiles / g.tiles_x);
+    const uint32_t band = tile / (4 * g.tiles_x), rows = min(4u, tiles_y - band * 4), in = tile - band * 4 * g.tiles_x;
+    ty = band * 4 + in % rows;
+    tx = in / rows;
+    return true;
+}
+
+// BM x BN outputs by WM x WN wavefronts, GROUPS groups of 128 elements of k at a time through a ring of STAGES buffers in LDS.  A
+// buffer holds BM rows of A and BN of B, 64 GROUPS bytes each, then the groups' scales, 4 bytes for each row.
+template <int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+struct Tile {
+    static constexpr int kThreads = WM * WN * KS * 64, kWaves = WM * WN;     // wavefronts of a part
+    static constexpr int kFragsM = BM / WM / 32, kFragsN = BN / WN / 32;
+    static constexpr int kRow = 64 * GROUPS;                       // bytes
+    static constexpr int kPieces = 4 * GROUPS;                     // of 16 bytes in a row
+    static constexpr int kRows = 64 / kPieces;                     // that one request of a wavefront covers
+    static constexpr int kScales = (BM + BN) * kRow;               // where a buffer's scales begin
+    static constexpr int kStage = kScales + (BM + BN) * 4 * GROUPS;
+    static constexpr int kLoads = (BM + BN) / kRows / kWaves;      // requests of codes, by every wavefront
+    static constexpr int kScaleLoads = ((BM + BN) * GROUPS / 64 + kWaves - 1) / kWaves;
+    static constexpr int kPerStage = kLoads + kScaleLoads;
+    static constexpr int kRing = STAGES * kStage;
+    static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
+    static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
+    static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % kRows == 0, "every wavefront requests the same");
+};
+
+// Waits until the requests of all but the newest `newer` stages (at most N) are there.
+template <int PER, int N>
+__device__ __forceinline__ void wait_for_stages(uint32_t newer)
+{
+    if constexpr (N > 0) {
+        if (newer < N) return wait_for_stages<PER, N - 1>(newer);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER * N) : "memory");
+}
+
+template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+__global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(MatmulArgs g)
+{
+    using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
+    extern __shared__ char lds[];
+    uint32_t ty, tx;
+    if (!find_tile(g, ty, tx)) return;
+    const uint32_t lane = threadIdx.x & 63, wave_in_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t part = wave_in_all / S::kWaves, wave = wave_in_all % S::kWaves;
+    const uint32_t r = lane & 31, half = lane >> 5, wm = wave / WN, wn = wave % WN;
+    const uint32_t row0 = ty * BM, col0 = tx * BN;
+
+    // A row's pieces lie in the buffer in another order from row to row: piece p of row n in place p ^ turn(n), so that 16 rows'
+    // pieces of the same k, which are read together, lie in 64 different banks.
+    constexpr auto turn = [](uint32_t n) { return GROUPS == 1 ? n >> 2 & 3 : n >> 1 & 7; };
+    const uint8_t* from[S::kLoads];                                // rows past the end repeat the last
+    uint32_t scale_row[S::kScaleLoads];
+    static_assert(S::kRows * S::kWaves % 16 == 0, "turn, of period 16, is the same in each of a wavefront's requests");
+    const uint32_t piece = (lane % S::kPieces) ^ turn(wave * S::kRows + lane / S::kPieces);
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const uint32_t c = i * S::kWaves + wave;                   // A's rows first
+        const bool is_a = c < BM / S::kRows;
+        const uint32_t row = (is_a ? c : c - BM / S::kRows) * S::kRows + lane / S::kPieces;
+        from[i] = (is_a ? g.a : g.b) + (uint64_t)(is_a ? min(row0 + row, g.m - 1) : min(col0 + row, g.n - 1)) * g.groups * 64;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) store_one<DTYPE>(g, ty * 32 + (i / 4) * 8 + half * 4 + i % 4, tx * 32 + r, acc[i]);
+    for (int i = 0; i < S::kScaleLoads; ++i) {
+        const uint32_t c = (i * S::kWaves + wave) % ((BM + BN) * GROUPS / 64);     // group after group: A's rows, then B's
+        const uint32_t row = c % ((BM + BN) / 64) * 64 + lane;
+        scale_row[i] = row < BM ? min(row0 + row, g.m - 1) : min(col0 + row - BM, g.n - 1);
+    }
+    // this part of k, in trips of GROUPS groups; `most` is the longest part's
+    const uint32_t all = (g.groups + GROUPS - 1) / GROUPS, most = (all + KS - 1) / KS, first_trip = part * most;
+    const uint32_t trips = KS == 1 ? all : first_trip < all ? min(most, all - first_trip) : 0;
+    char* ring = lds + part * S::kRing;
+    auto fetch = [&](uint32_t t, uint32_t stage) {
+        char* base = ring + stage * S::kStage;
+        const uint32_t first = (first_trip + t) * GROUPS;
+        // the second half of the last stage may not be there: the first again, which is not used
+        const uint32_t at = (GROUPS == 1 || first + 1 < g.groups ? piece : piece & 3) * 16;
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i) {
+            const uint32_t c = i * S::kWaves + wave;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)first * 64 + at), (lds_bytes*)(base + c * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < S::kScaleLoads; ++i) {
+            const uint32_t c = (i * S::kWaves + wave) % ((BM + BN) * GROUPS / 64), in_group = c % ((BM + BN) / 64);
+            const uint64_t group = min(first + c / ((BM + BN) / 64), g.groups - 1);
+            const uint32_t* q = in_group < BM / 64 ? reinterpret_cast<const uint32_t*>(g.sa) + group * g.m
+                                                   : reinterpret_cast<const uint32_t*>(g.sb) + group * g.n;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(q + scale_row[i]), (lds_bytes*)(base + S::kScales + c * 256), 4, 0, 0);
+        }
+    };
+
+    const uint32_t ra = wm * S::kFragsM * 32 + r, rb = BM + wn * S::kFragsN * 32 + r;
+    f32x16 acc[S::kFragsM][S::kFragsN] = {};
+#pragma unroll
+    for (uint32_t t = 0; t < STAGES - 1; ++t)
+        if (t < trips) fetch(t, t);
+    uint32_t stage = 0, free_stage = STAGES - 1;
+    for (uint32_t t = 0; t < most; ++t) {
+        // this trip's requests are there, and every wavefront is done with the buffer that is filled next
+        wait_for_stages<S::kPerStage, STAGES - 2>(t < trips ? trips - 1 - t : 0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + STAGES - 1 < trips) fetch(t + STAGES - 1, free_stage);
+        const char* base = ring + stage * S::kStage;
+#pragma unroll
+        for (int h = 0; h < GROUPS; ++h) {
+            if (KS > 1 && h == 0 && t >= trips) break;             // a shorter part
+            if (h && (first_trip + t) * GROUPS + h >= g.groups) break;
+            int sa[S::kFragsM], sb[S::kFragsN];
+            i32x4 a[2][S::kFragsM], b[2][S::kFragsN];
+            const char* scales = base + S::kScales + h * (BM + BN) * 4;
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i) sa[i] = *reinterpret_cast<const int*>(scales + (ra + i * 32) * 4) >> (8 * half);
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j) sb[j] = *reinterpret_cast<const int*>(scales + (rb + j * 32) * 4) >> (8 * half);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t at = ((4 * h + 2 * s + half) ^ turn(lane)) * 16;
+#pragma unroll
+                for (int i = 0; i < S::kFragsM; ++i) a[s][i] = *reinterpret_cast<const i32x4*>(base + (ra + i * 32) * S::kRow + at);
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j) b[s][j] = *reinterpret_cast<const i32x4*>(base + (rb + j * 32) * S::kRow + at);
+            }
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = mfma32<0>(a[0][i], b[0][j], acc[i][j], sa[i], sb[j]);
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = mfma32<2>(a[1][i], b[1][j], acc[i][j], sa[i], sb[j]);
+        }
+        free_stage = stage;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    if constexpr (KS > 1) {                                        // the parts' sums, joined in their order
+        __syncthreads();                                           // the rings are done with
+        float* sums = reinterpret_cast<float*>(lds);
+        const uint32_t at = (part * BM + wm * S::kFragsM * 32 + half * 4) * (BN + 1) + wn * S::kFragsN * 32 + r;
+#pragma unroll
+        for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sums[at + (i * 32 + (e / 4) * 8 + e % 4) * (BN + 1) + j * 32] = acc[i][j][e];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < BM * BN; i += S::kThreads) {
+            const uint32_t row = i / BN, col = i % BN;
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < KS; ++q) v += sums[(q * BM + row) * (BN + 1) + col];
+            store_one<DTYPE>(g, row0 + row, col0 + col, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kFragsN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                store_one<DTYPE>(g, row0 + (wm * S::kFragsM + i) * 32 + (e / 4) * 8 + half * 4 + e % 4,
+                                 col0 + (wn * S::kFragsN + j) * 32 + r, acc[i][j][e]);
+}
+
+// Few rows of A (at most 32) against 32 rows of B, 8 wavefronts over parts of k: serving, where B is read once and bounds it.  The
+// rows of A, cast here if they are not in 4-bit form yet, stay in LDS; B comes through a ring for each wavefront, whose first
+// requests are on their way while A is prepared.
+constexpr int kFewWaves = 8, kFewStages = 2, kFewStage = 32 * 128 + 256, kFewRing = kFewWaves * kFewStages * kFewStage;
+constexpr uint32_t kFewBytes = 160 << 10;                         // the LDS of a compute unit
+constexpr uint32_t kFewRowsInForm = 16, kFewRows = 32;
+
+__host__ __device__ constexpr uint64_t few_row_bytes(uint64_t groups) { return groups * 64 + 16; }
+__host__ __device__ constexpr uint64_t few_bytes(uint64_t m, uint64_t groups) { return kFewRing + m * (few_row_bytes(groups) + groups * 4); }
+
+// X: the type of g.x, or -1 for rows in 4-bit form.  VEC: rows of x are 16-byte aligned.
+template <int DTYPE, int X, bool VEC>
+__global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArgs g)
+{
+    extern __shared__ char lds[];
+    const uint32_t tx = linear_block();
+    if (tx >= g.tiles) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
+    const uint32_t col0 = tx * 32, pairs = (g.groups + 1) / 2;
+    const uint32_t per = (pairs + kFewWaves - 1) / kFewWaves, first = wave * per, trips = first < pairs ? min(per, pairs - first) : 0;
+    char* ring = lds + wave * (kFewStages * kFewStage);
+    const uint32_t row_bytes = (uint32_t)few_row_bytes(g.groups);
+    char* codes = lds + kFewRing;
+    char* scales = codes + g.m * row_bytes;                        // [m][groups][4]
+
+    const uint8_t* from[4];
+    const uint32_t piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};      // of rows 8 i + lane / 8, i even and odd
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from[i] = g.b + (uint64_t)min(col0 + i * 8 + (lane >> 3), g.n - 1) * g.groups * 64;
+    const uint32_t row_b = min(col0 + r, g.n - 1);
+    auto fetch = [&](uint32_t t, uint32_t stage) {
+        char* base = ring + stage * kFewStage;
+        const uint32_t group = 2 * (first + t);
+        const bool both = group + 1 < g.groups;                    // the second half of the last may not be there: the first again
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at = both ? piece[i & 1] : piece[i & 1] & 3;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)group * 64 + at * 16), (lds_bytes*)(base + i * 1024), 16, 0, 0);
+        }
+        const uint64_t mine = both ? group + half : group;
+        __builtin_amdgcn_global_load_lds((global_bytes*)(g.sb + (mine * g.n + row_b) * 4), (lds_bytes*)(base + 4096), 4, 0, 0);
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < kFewStages; ++t)
+        if (t < trips) fetch(t, t);
+
+    if constexpr (X < 0) {
+        for (uint32_t i = threadIdx.x; i < g.m * g.groups * 4; i += kFewWaves * 64) {
+            const uint32_t row = i / (g.groups * 4), p = i - row * (g.groups * 4);
+            *reinterpret_cast<i32x4*>(codes + row * row_bytes + p * 16) = *reinterpret_cast<const i32x4*>(g.a + (uint64_t)i * 16);
+        }
+        for (uint32_t i = threadIdx.x; i < g.m * g.groups; i += kFewWaves * 64) {
+            const uint32_t group = i / g.m, row = i - group * g.m;
+            *reinterpret_cast<int*>(scales + (row * g.groups + group) * 4) = *reinterpret_cast<const int*>(g.sa + (uint64_t)i * 4);
+        }
+    } else {
+        using T = typename Element<X>::type;
+        const uint32_t octs = g.groups * 16;                       // of 8 elements in a row: four neighbouring lanes are a block
+        for (uint32_t i = threadIdx.x; i < g.m * octs; i += kFewWaves * 64) {
+            const uint32_t row = i / octs, oct = i - row * octs;
+            float v[8];
+            load8<X, VEC>(static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
+            uint32_t largest = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
+            const uint32_t byte = mx_scale_byte<false>(quad_max(largest));
+            const uint32_t none[4] = {};
+            *reinterpret_cast<uint32_t*>(codes + row * row_bytes + oct * 4) = mx_codes<false>(v, byte, none);
+            if ((oct & 3) == 0) scales[row * octs / 4 + oct / 4] = (char)byte;
+        }
+    }
+    __syncthreads();
+
+    const char* my_codes = codes + min(r, g.m - 1) * row_bytes;
+    const char* my_scales = scales + min(r, g.m - 1) * g.groups * 4;
+    f32x16 acc = {};
+    uint32_t stage = 0;
+    for (uint32_t t = 0; t < trips; ++t) {
+        wait_for_stages<5, kFewStages - 1>(trips - 1 - t);
+        const char* base = ring + stage * kFewStage;
+        const uint32_t group = 2 * (first + t);
+        const bool both = group + 1 < g.groups;
+        i32x4 a[4], b[4];
+        int sa[2], sb[2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            b[s] = *reinterpret_cast<const i32x4*>(base + r * 128 + ((2 * s + half) ^ (r >> 1 & 7)) * 16);
+            a[s] = *reinterpret_cast<const i32x4*>(my_codes + (group + (both ? s / 2 : 0)) * 64 + (2 * (s & 1) + half) * 16);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sb[h] = *reinterpret_cast<const int*>(base + 4096 + (h * 32 + r) * 4) >> (8 * half);
+            sa[h] = *reinterpret_cast<const int*>(my_scales + (group + (both ? h : 0)) * 4) >> (8 * half);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
+        if (t + kFewStages < trips) fetch(t + kFewStages, stage);
+        acc = mfma32<0>(a[0], b[0], acc, sa[0], sb[0]);
+        acc = mfma32<2>(a[1], b[1], acc, sa[0], sb[0]);
+        if (both) {
+            acc = mfma32<0>(a[2], b[2], acc, sa[1], sb[1]);
+            acc = mfma32<2>(a[3], b[3], acc, sa[1], sb[1]);
+        }
+        stage ^= 1;
+    }
+    __syncthreads();                                               // the rings are done with
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[(wave * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < g.m * 32; i += kFewWaves * 64) {
+        const uint32_t row = i / 32, col = i & 31;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) v += sums[(w * 32 + row) * 33 + col];
+        store_one<DTYPE>(g, row, col0 + col, v);
+    }
+}
+
+template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+hipError_t launch_tile(MatmulArgs& g, hipStream_t st)
+{
+    using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
+    g.tiles_x = (g.n + BN - 1) / BN;
+    g.tiles = (uint64_t)g.tiles_x * ((g.m + BM - 1) / BM);
+    dim3 grid;
+    if (!fold_grid((g.tiles + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
+    mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES><<<grid, S::kThreads, S::kBytes, st>>>(g);
+    return hipGetLastError();
+}
+
+template <int DTYPE, int X>
+hipError_t launch_few(MatmulArgs& g, hipStream_t st)
+{
+    g.tiles = (g.n + 31) / 32;
+    dim3 grid;
+    if (!fold_grid(g.tiles, kFewWaves * 64, 1, grid)) return hipErrorInvalidValue;
+    const uint32_t bytes = (uint32_t)few_bytes(g.m, g.groups);
+    const bool vec = X >= 0 && ((reinterpret_cast<uintptr_t>(g.x) | g.ldx * (X == TQ_F32 ? 4 : 2)) & 15u) == 0;
+    if (vec) mx_matmul_few_kernel<DTYPE, X, true><<<grid, kFewWaves * 64, bytes, st>>>(g);
+    else mx_matmul_few_kernel<DTYPE, X, false><<<grid, kFewWaves * 64, bytes, st>>>(g);
+    return hipGetLastError();
+}
+
+// Which kernel.  Times in us, in turn, replayed from a graph; `256`, `128`, `64` are tiles of that side (16, 8 and 4 wavefronts),
+// `64/4` tiles of 64 with k in 4 parts (16 wavefronts), `few` the kernel for few rows:
+//   m x n x k            256    128     64   64/4    few
+//   8192 x 8192 x 8192   309    405    647    629              large tiles move least through the caches
+//   4096 x 4096 x 4096  45.2   56.0   85.4    102
+//   1037 x 8192 x 4096  37.7   38.6   46.6   57.7
+//   2048 x 2048 x 2048  20.9   11.6   13.7   18.0              256 leaves three quarters of the device without a tile
+//   4096 x 1000 x 784   14.5    8.9    9.4   15.3
+//   2056 x 1000 x 1999  20.5   10.4    9.9   13.7
+//   512 x 4096 x 4096   32.0   15.2   12.0   13.0
+//   256 x 4096 x 4096   31.8   14.7   10.6    7.6              64 too: the parts of k run beside each other
+//   128 x 8192 x 8192   54.8   25.8   18.0   12.7
+//   784 x 1000 x 64      8.1    4.8    3.9    4.6              nothing to part
+//   1 x 8192 x 8192     57.5   28.1   19.9    9.7    7.4
+template <int DTYPE>
+hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
+{
+    if (g.m <= kFewRowsInForm && few_bytes(g.m, g.groups) <= kFewBytes) return launch_few<DTYPE, -1>(g, st);
+    auto tiles = [&](uint64_t side) { return (g.m + side - 1) / side * ((g.n + side - 1) / side); };
+    const uint64_t of_256 = tiles(256), of_128 = tiles(128), of_64 = tiles(64), units = 256;
+    // A round of tiles of 256, one on each compute unit, takes as long as 820 tiles of 128.
+    if ((of_256 + units - 1) / units * 820 <= of_128) return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
+    if (of_128 >= units) return launch_tile<DTYPE, 128, 128, 2, 4, 1, 1, 3>(g, st);
+    if (of_64 > units || g.groups < 4) return launch_tile<DTYPE, 64, 64, 2, 2, 1, 1, 3>(g, st);
+    return launch_tile<DTYPE, 64, 64, 2, 2, 4, 2, 2>(g, st);
 }
 
 }  // namespace
@@ -81,13 +405,34 @@ hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, con
     g.ldo = ldo;
     g.m = (uint32_t)m;
     g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
     g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
-    g.tiles_x = (uint32_t)((n + 31) / 32);
-    g.tiles = g.tiles_x * ((m + 31) / 32);
-    dim3 grid;
-    if (!fold_grid(g.tiles, 64, 1, grid)) return hipErrorInvalidValue;
-    if (dtype == TQ_F32) mx_matmul_direct_kernel<TQ_F32><<<grid, 64, 0, st>>>(g);
-    else if (dtype == TQ_BF16) mx_matmul_direct_kernel<TQ_BF16><<<grid, 64, 0, st>>>(g);
-    else mx_matmul_direct_kernel<TQ_F16><<<grid, 64, 0, st>>>(g);
-    return hipGetLastError();
+    if (dtype == TQ_F32) return launch_matmul<TQ_F32>(g, st);
+    return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
+}
+
+bool tq_mx_linear_in_one(uint64_t m, uint64_t k) { return m <= tq::kFewRows && tq::few_bytes(m, (k + tq::kMxGroup - 1) / tq::kMxGroup) <= tq::kFewBytes; }
+
+hipError_t tq_launch_mx_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const void* sw, uint64_t n,
+                                   uint64_t k, void* out, int dtype, uint64_t ldo, hipStream_t st)
+{
+    using namespace tq;
+    MatmulArgs g = {};
+    g.x = x;
+    g.ldx = ldx;
+    g.b = static_cast<const uint8_t*>(w);
+    g.sb = static_cast<const uint8_t*>(sw);
+    g.out = out;
+    g.ldo = ldo;
+    g.m = (uint32_t)m;
+    g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
+    g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
+    auto as = [&](auto D) {
+        constexpr int T = decltype(D)::value;
+        if (x_dtype == TQ_F32) return launch_few<T, TQ_F32>(g, st);
+        return x_dtype == TQ_BF16 ? launch_few<T, TQ_BF16>(g, st) : launch_few<T, TQ_F16>(g, st);
+    };
+    if (dtype == TQ_F32) return as(std::integral_constant<int, TQ_F32>{});
+    return dtype == TQ_BF16 ? as(std::integral_constant<int, TQ_BF16>{}) : as(std::integral_constant<int, TQ_F16>{});
 }
