@@ -17,206 +17,330 @@ struct DistillArgs {
     void* dz;
     uint64_t ldz, lddz;
     uint32_t rows, vocab, top;
-    int wide_ids;
+    int wide_ids, past_caches;
     float tau, inv_tau;
-};
-
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
-}
-// Over the workgroup, in a fixed order; `part` holds one value per wavefront.  Begins and ends with a barrier.
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float v, float* part)
-{
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) s += part[w];
-    return s;
-}
-template <int WAVES>
-__device__ __forceinline__ float group_max(float v, float* part)
-{
-    v = wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = part[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) s = fmaxf(s, part[w]);
-    return s;
-}
-
-// Running maximum (of z) and sum of exp((z - max) / tau).
-struct Softmax {
-    float m = -INFINITY, s = 0.0f;
-    // -inf - -inf has no value: while nothing but -inf was seen, the sum of nothing is 0
-    static __device__ __forceinline__ float scale(float from, float to, float c) { return from == -INFINITY ? 0.0f : exp2f((from - to) * c); }
-    __device__ __forceinline__ void take(const float (&v)[8], float c)
-    {
-        float top = v[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j]);
-        if (top > m) {
-            s *= scale(m, top, c);
-            m = top;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s += v[j] == -INFINITY ? 0.0f : exp2f((v[j] - m) * c);
-    }
-    __device__ __forceinline__ void join(float m2, float s2, float c)
-    {
-        const float to = fmaxf(m, m2);
-        s = s * scale(m, to, c) + s2 * scale(m2, to, c);
-        m = to;
-    }
 };
 
 enum { kForward = 0, kBackward = 1, kBoth = 2 };
 
-// One workgroup a row, 8 elements a thread at a time.
-template <int DTYPE, int MODE, int THREADS>
+// A row as whole 16-byte vectors at aligned addresses, up to kIn - 1 loose elements before them and as many behind.
+template <int DTYPE>
+struct Row {
+    using E = Element<DTYPE>;
+    using T = typename E::type;
+    static constexpr uint32_t kIn = 16 / sizeof(T);                // elements of a vector
+    static constexpr uint32_t kNothing = DTYPE == TQ_F32 ? 0xFF800000u : DTYPE == TQ_BF16 ? 0xFF80FF80u : 0xFC00FC00u;      // -inf
+    uint32_t head, vectors, tail;
+
+    __device__ __forceinline__ Row(const T* p, uint32_t n)
+    {
+        head = min((uint32_t)(-(reinterpret_cast<uintptr_t>(p) / sizeof(T))) & (kIn - 1), n);
+        vectors = (n - head) / kIn;
+        tail = n - head - vectors * kIn;
+    }
+    // The loose element of this thread (of the first 2 kIn ones), or -1.
+    __device__ __forceinline__ int64_t loose(uint32_t tid) const
+    {
+        if (tid < head) return tid;
+        if (tid >= kIn && tid - kIn < tail) return (int64_t)head + (uint64_t)vectors * kIn + (tid - kIn);
+        return -1;
+    }
+    __device__ __forceinline__ u32x4 load(const T* p, uint32_t k) const
+    {
+        return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p + head) + (uint64_t)k * 16);
+    }
+    static __device__ __forceinline__ void unpack(u32x4 w, float (&v)[kIn])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (uint32_t e = 0; e < kIn; ++e) v[e] = __uint_as_float(w[e]);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < kIn / 2; ++e) unpack2<DTYPE>(w[e], v[2 * e], v[2 * e + 1]);
+        }
+    }
+    // Vector k of the gradient, which begins at p and lies as the row does (WHOLE) or not.
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(T* p, uint32_t k, const float (&v)[kIn], bool past_caches) const
+    {
+        T* q = p + head + (uint64_t)k * kIn;
+        if constexpr (WHOLE) {
+            u32x4 w;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (uint32_t e = 0; e < kIn; ++e) w[e] = __float_as_uint(v[e]);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < kIn / 2; ++e) w[e] = pack2<DTYPE>(v[2 * e], v[2 * e + 1]);
+            }
+            if (past_caches) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(q));
+            else *reinterpret_cast<u32x4*>(q) = w;
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < kIn; ++e) q[e] = E::store(v[e]);
+        }
+    }
+};
+
+// Sums and maxima of two values over the workgroup, in a fixed order.  `part` holds two values per wavefront and is used once.
+template <int WAVES, bool MAX>
+__device__ __forceinline__ void group_reduce(float& x, float& y, float (*part)[2])
+{
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        x = op(x, __shfl_xor(x, d));
+        y = op(y, __shfl_xor(y, d));
+    }
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+            part[threadIdx.x >> 6][0] = x;
+            part[threadIdx.x >> 6][1] = y;
+        }
+        __syncthreads();
+        x = part[0][0];
+        y = part[0][1];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            x = op(x, part[w][0]);
+            y = op(y, part[w][1]);
+        }
+    }
+}
+
+// Running maximum and sum of exp((z - maximum) / tau) of a thread's elements.
+struct Softmax {
+    float m = -INFINITY, s = 0.0f;
+    template <int N>
+    __device__ __forceinline__ void take(const float (&v)[N], float c)
+    {
+        float top = v[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
+        if (top > m) {
+            s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+        }
+        const float low = m == -INFINITY ? 0.0f : m;               // -inf - -inf has no value; there the sum stays 0
+#pragma unroll
+        for (int j = 0; j < N; ++j) s += __builtin_amdgcn_exp2f((v[j] - low) * c);
+    }
+};
+
+// The compiler would keep the values that it has unpacked for the next pass over them, in twice the registers.
+__device__ __forceinline__ void keep_packed(u32x4& w) { asm volatile("" : "+v"(w)); }
+
+// One workgroup a row.  VECTORS > 0: the row stays in the registers, VECTORS x 16 bytes a thread, so memory is read once; 0: it is
+// read again for the gradient.  WHOLE: dz lies to its 16-byte lines as z does.
+template <int DTYPE, int MODE, int THREADS, int VECTORS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
 {
     using E = Element<DTYPE>;
     using T = typename E::type;
+    using R = Row<DTYPE>;
     constexpr int WAVES = THREADS / 64;
-    __shared__ float part[WAVES], part_s[WAVES];
-    __shared__ int id[TQ_DISTILL_MAX_TOP];
-    __shared__ float prob[TQ_DISTILL_MAX_TOP];
+    constexpr uint32_t IN = R::kIn;
+    __shared__ float parts[3][WAVES][2];
+    extern __shared__ char entries[];                              // the teacher's: id, logit and then probability, z, whether
+    int* id = reinterpret_cast<int*>(entries);                     // an earlier one has the id
+    float* t = reinterpret_cast<float*>(id + a.top);
+    float* at_id = t + a.top;
+    int* again = reinterpret_cast<int*>(at_id + a.top);
     const uint32_t row = linear_block(), tid = threadIdx.x;
     if (row >= a.rows) return;
     const T* z = static_cast<const T*>(a.z) + (uint64_t)row * a.ldz;
-    T* dz = MODE == kForward ? nullptr : static_cast<T*>(a.dz) + (uint64_t)row * a.lddz;
+    const R lies(z, a.vocab);
     const float grad = MODE == kForward ? 0.0f : a.grad[row];
     const float c = a.inv_tau * kLog2e;
 
-    // the teacher
-    float peak = -INFINITY;
-    bool bad = false;
+    u32x4 held[VECTORS > 0 ? VECTORS : 1];
+#pragma unroll
+    for (int i = 0; i < VECTORS; ++i) {
+        held[i] = u32x4{R::kNothing, R::kNothing, R::kNothing, R::kNothing};
+        if (tid + i * THREADS < lies.vectors) held[i] = lies.load(z, tid + i * THREADS);
+    }
+    const int64_t loose = lies.loose(tid);
+    const float z_loose = loose >= 0 ? E::load(z[loose]) : -INFINITY;
+
+    float t_peak = -INFINITY;
+    bool bad = false, twice = false;
     for (uint32_t i = tid; i < a.top; i += THREADS) {
         const uint64_t at = (uint64_t)row * a.top + i;
         const int64_t w = a.wide_ids ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
-        const float t = a.t[at];
-        const bool there = w >= 0 && w < (int64_t)a.vocab && t != -INFINITY;
+        const float v = a.t[at];
+        const bool there = w >= 0 && w < (int64_t)a.vocab && v != -INFINITY;
         id[i] = there ? (int)w : -1;
-        prob[i] = t;
+        t[i] = v;
+        again[i] = 0;
+        at_id[i] = there ? E::load(z[w]) : 0.0f;
         if (there) {
-            peak = fmaxf(peak, t);
-            bad |= !(t < INFINITY);
+            t_peak = fmaxf(t_peak, v);
+            bad |= !(v < INFINITY);
         }
     }
-    peak = group_max<WAVES>(peak, part);
-    float sum = 0.0f;
-    for (uint32_t i = tid; i < a.top; i += THREADS) sum += id[i] < 0 ? 0.0f : exp2f((prob[i] - peak) * c);
-    sum = group_sum<WAVES>(bad ? NAN : sum, part);
-    const bool empty = sum == 0.0f;
-    const float log_sum = empty ? 0.0f : logf(sum);
+    if constexpr (MODE != kForward) {                              // each pair of entries once, spread over the threads
+        __syncthreads();
+        const uint32_t slices = a.top < THREADS ? THREADS / a.top : 1, slice = tid / a.top, step = a.top < THREADS ? a.top : THREADS;
+        if (slice < slices || a.top >= THREADS)
+            for (uint32_t i = a.top < THREADS ? tid - slice * a.top : tid; i < a.top; i += step) {
+                const int mine = id[i];
+                for (uint32_t j = a.top < THREADS ? slice : 0; mine >= 0 && j < i; j += slices)
+                    if (id[j] == mine) {
+                        again[i] = 1;
+                        twice = true;
+                    }
+            }
+    }
 
-    // the student
-    float top = 0.0f, log_total = 0.0f;                          // the row's largest logit, ln sum exp((z - top) / tau)
-    if (MODE == kBackward) {
+    float top = z_loose, log_total = 0.0f;                         // the row's largest logit, ln sum exp((z - top) / tau)
+    Softmax q;
+    if constexpr (MODE != kBackward && VECTORS > 0) {
+#pragma unroll
+        for (int i = 0; i < VECTORS; ++i) {
+            float v[IN];
+            R::unpack(held[i], v);
+#pragma unroll
+            for (uint32_t j = 0; j < IN; ++j) top = fmaxf(top, v[j]);
+        }
+    } else if constexpr (MODE != kBackward) {
+        const float first[1] = {z_loose};
+        q.take(first, c);
+#pragma unroll 4
+        for (uint32_t k = tid; k < lies.vectors; k += THREADS) {
+            float v[IN];
+            R::unpack(lies.load(z, k), v);
+            q.take(v, c);
+        }
+        top = q.m;
+    }
+    group_reduce<WAVES, true>(t_peak, top, parts[0]);
+    float t_sum = 0.0f, total = 0.0f;
+    for (uint32_t i = tid; i < a.top; i += THREADS)
+        if (id[i] >= 0) t_sum += __builtin_amdgcn_exp2f((t[i] - t_peak) * c);
+    if (bad) t_sum = NAN;
+    if constexpr (MODE != kBackward) {
+        const float low = top == -INFINITY ? 0.0f : top;
+        if constexpr (VECTORS > 0) {
+            total = __builtin_amdgcn_exp2f((z_loose - low) * c);
+#pragma unroll
+            for (int i = 0; i < VECTORS; ++i) {
+                float v[IN];
+                keep_packed(held[i]);
+                R::unpack(held[i], v);
+#pragma unroll
+                for (uint32_t j = 0; j < IN; ++j) total += __builtin_amdgcn_exp2f((v[j] - low) * c);
+            }
+        } else {
+            total = q.m == -INFINITY ? q.s : q.s * __builtin_amdgcn_exp2f((q.m - low) * c);
+        }
+    }
+    group_reduce<WAVES, false>(t_sum, total, parts[1]);
+    const bool empty = t_sum == 0.0f;
+    const float t_log = empty ? 0.0f : logf(t_sum);
+    if constexpr (MODE == kBackward) {
         top = a.stats_in[2 * (uint64_t)row];
         log_total = a.stats_in[2 * (uint64_t)row + 1];
     } else {
-        Softmax q;
-        for (uint64_t i = (uint64_t)tid * 8; i < a.vocab; i += THREADS * 8) {
-            float v[8];
-            const int n = (int)min((uint64_t)a.vocab - i, (uint64_t)8);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < n ? E::load(z[i + j]) : -INFINITY;
-            q.take(v, c);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) q.join(__shfl_xor(q.m, d), __shfl_xor(q.s, d), c);
-        __syncthreads();
-        if ((tid & 63) == 0) {
-            part[tid >> 6] = q.m;
-            part_s[tid >> 6] = q.s;
-        }
-        __syncthreads();
-        Softmax all;
-        for (int w = 0; w < WAVES; ++w) all.join(part[w], part_s[w], c);
-        top = all.m;
-        log_total = logf(all.s);
+        log_total = logf(total);
     }
     // where nothing is left of the row every z is -inf and q is 0: any finite numbers do
     const bool none = log_total == -INFINITY;
-    const float low = none ? 0.0f : top, log_low = none ? 0.0f : log_total;
+    const float low = none || top == -INFINITY ? 0.0f : top, log_low = none ? 0.0f : log_total;
 
-    // loss, and the elements that the teacher names; an id's first entry takes the probabilities of all its entries
-    float loss = 0.0f;
-    float named[TQ_DISTILL_MAX_TOP / THREADS ? TQ_DISTILL_MAX_TOP / THREADS : 1];
-    int k = 0;
+    float loss = 0.0f, count = twice ? 1.0f : 0.0f;
+    for (uint32_t i = tid; i < a.top; i += THREADS) {
+        const float x = (t[i] - t_peak) * a.inv_tau - t_log, p = id[i] < 0 ? 0.0f : __builtin_amdgcn_exp2f(x * kLog2e);
+        if (!(p <= 0.0f)) loss += p * (x - ((at_id[i] - low) * a.inv_tau - log_low));
+        t[i] = p;
+    }
+    group_reduce<WAVES, false>(loss, count, parts[2]);
+    if (MODE != kBackward && tid == 0) {
+        a.loss[row] = empty ? 0.0f : loss * a.tau * a.tau;
+        if (MODE == kForward) {
+            a.stats[2 * (uint64_t)row] = top;
+            a.stats[2 * (uint64_t)row + 1] = log_total;
+        }
+    }
+    if constexpr (MODE != kForward) {
+        T* dz = static_cast<T*>(a.dz) + (uint64_t)row * a.lddz;
+        const bool counts = !empty && grad != 0.0f;
+        const float g = t_sum != t_sum ? NAN : a.tau * grad;       // a teacher without a value leaves none to any element
+        const float scale = counts ? g * __builtin_amdgcn_exp2f(-log_low * kLog2e) : 0.0f;
+        auto gradient = [&](float v) { return counts ? scale * __builtin_amdgcn_exp2f((v - low) * c) : 0.0f; };
+        // (the reductions' barriers: every z[id] is read where dz is z)
+        if (loose >= 0) dz[loose] = E::store(gradient(z_loose));
+        auto put = [&](uint32_t k, u32x4 w) {
+            float v[IN];
+            R::unpack(w, v);
 #pragma unroll
-    for (uint32_t i0 = 0; i0 < TQ_DISTILL_MAX_TOP; i0 += THREADS, ++k) {
-        const uint32_t i = i0 + tid;
-        named[k] = 0.0f;
-        if (i < a.top && id[i] >= 0 && !empty) {
-            const float x = (prob[i] - peak) * a.inv_tau - log_sum, p = expf(x), zi = E::load(z[id[i]]);
-            if (!(p <= 0.0f)) loss += p * (x - ((zi - low) * a.inv_tau - log_low));
-            named[k] = zi;
+            for (uint32_t j = 0; j < IN; ++j) v[j] = gradient(v[j]);
+            lies.template store<WHOLE>(dz, k, v, a.past_caches);
+        };
+        if constexpr (VECTORS > 0) {
+#pragma unroll
+            for (int i = 0; i < VECTORS; ++i)
+                if (tid + i * THREADS < lies.vectors) {
+                    keep_packed(held[i]);
+                    put(tid + i * THREADS, held[i]);
+                }
+        } else if (counts) {
+#pragma unroll 4
+            for (uint32_t k = tid; k < lies.vectors; k += THREADS) put(k, lies.load(z, k));
+        } else {
+            for (uint32_t k = tid; k < lies.vectors; k += THREADS) put(k, u32x4{0, 0, 0, 0});
         }
-    }
-    if (MODE != kBackward) {
-        loss = group_sum<WAVES>(loss, part);
-        if (tid == 0) {
-            a.loss[row] = empty ? 0.0f : loss * a.tau * a.tau;
-            if (MODE == kForward) {
-                a.stats[2 * (uint64_t)row] = top;
-                a.stats[2 * (uint64_t)row + 1] = log_total;
+        if (!counts) return;
+        __syncthreads();                                           // the elements that the teacher names are written once more
+        for (uint32_t i = tid; i < a.top; i += THREADS)
+            if (id[i] >= 0 && !again[i]) {
+                float p = t[i];
+                if (count != 0.0f)
+                    for (uint32_t j = i + 1; j < a.top; ++j)
+                        if (id[j] == id[i]) p += t[j];
+                dz[id[i]] = E::store(scale * __builtin_amdgcn_exp2f((at_id[i] - low) * c) - g * p);
             }
-        }
     }
-    if (MODE == kForward) return;
+}
 
-    const bool counts = !empty && grad != 0.0f;
-    const float g = sum != sum ? NAN : a.tau * grad;             // a teacher without a value leaves none to any element
-    __syncthreads();                                            // z is read: dz may be z
-    for (uint64_t i = tid; i < a.vocab; i += THREADS) {
-        const float q = counts ? expf((E::load(z[i]) - low) * a.inv_tau - log_low) : 0.0f;
-        dz[i] = E::store(counts ? g * q : 0.0f);
-    }
-    if (!counts) return;
-    __syncthreads();
-    k = 0;
-#pragma unroll
-    for (uint32_t i0 = 0; i0 < TQ_DISTILL_MAX_TOP; i0 += THREADS, ++k) {
-        const uint32_t i = i0 + tid;
-        if (i < a.top && id[i] >= 0) {
-            bool first = true;
-            for (uint32_t j = 0; j < i; ++j) first &= id[j] != id[i];
-            if (first) {
-                float p = 0.0f;
-                for (uint32_t j = i; j < a.top; ++j)
-                    if (id[j] == id[i]) p += expf((prob[j] - peak) * a.inv_tau - log_sum);
-                dz[id[i]] = E::store(g * (expf((named[k] - low) * a.inv_tau - log_low) - p));
-            }
+template <int DTYPE, int MODE, int THREADS, int VECTORS>
+hipError_t launch(const DistillArgs& a, hipStream_t st)
+{
+    dim3 grid;
+    if (!fold_grid(a.rows, THREADS, 1, grid)) return hipErrorInvalidValue;
+    const size_t entries = 16 * (size_t)a.top;
+    if constexpr (MODE != kForward) {
+        const uint64_t size = DTYPE == TQ_F32 ? 4 : 2;
+        if (((reinterpret_cast<uintptr_t>(a.dz) - reinterpret_cast<uintptr_t>(a.z)) | (a.lddz - a.ldz) * size) & 15u) {
+            distill_kernel<DTYPE, MODE, THREADS, VECTORS, false><<<grid, THREADS, entries, st>>>(a);
+            return hipGetLastError();
         }
+    }
+    distill_kernel<DTYPE, MODE, THREADS, VECTORS, true><<<grid, THREADS, entries, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int DTYPE, int MODE>
+hipError_t launch(const DistillArgs& a, hipStream_t st)
+{
+    const uint64_t vectors = (uint64_t)a.vocab / Row<DTYPE>::kIn;
+    if constexpr (MODE == kBackward) {
+        if (vectors <= 256) return launch<DTYPE, MODE, 64, 0>(a, st);
+        return vectors <= 4096 ? launch<DTYPE, MODE, 256, 0>(a, st) : launch<DTYPE, MODE, 1024, 0>(a, st);
+    } else {
+        if (vectors <= 64 * 4) return launch<DTYPE, MODE, 64, 4>(a, st);
+        if (vectors <= 256 * 4) return launch<DTYPE, MODE, 256, 4>(a, st);
+        if (vectors <= 512 * 8) return launch<DTYPE, MODE, 512, 8>(a, st);
+        if (vectors <= 1024 * 8) return launch<DTYPE, MODE, 1024, 8>(a, st);
+        if (vectors <= 1024 * 16) return launch<DTYPE, MODE, 1024, 16>(a, st);
+        return launch<DTYPE, MODE, 1024, 0>(a, st);
     }
 }
 
 template <int MODE>
 hipError_t launch(const DistillArgs& a, int dtype, hipStream_t st)
 {
-    dim3 grid;
-    if (!fold_grid(a.rows, 256, 1, grid)) return hipErrorInvalidValue;
-    if (dtype == TQ_F32) distill_kernel<TQ_F32, MODE, 256><<<grid, 256, 0, st>>>(a);
-    else if (dtype == TQ_BF16) distill_kernel<TQ_BF16, MODE, 256><<<grid, 256, 0, st>>>(a);
-    else distill_kernel<TQ_F16, MODE, 256><<<grid, 256, 0, st>>>(a);
-    return hipGetLastError();
+    if (dtype == TQ_F32) return launch<TQ_F32, MODE>(a, st);
+    return dtype == TQ_BF16 ? launch<TQ_BF16, MODE>(a, st) : launch<TQ_F16, MODE>(a, st);
 }
 
 }  // namespace
@@ -244,6 +368,7 @@ hipError_t tq_launch_distill(const void* z, int dtype, uint64_t rows, uint64_t v
     a.wide_ids = ids_bytes == 8;
     a.tau = temperature;
     a.inv_tau = 1.0f / temperature;
+    a.past_caches = dz && output_past_caches(rows * vocab * (dtype == TQ_F32 ? 4 : 2));
     if (!dz) return launch<kForward>(a, dtype, st);
     return stats_in ? launch<kBackward>(a, dtype, st) : launch<kBoth>(a, dtype, st);
 }
