@@ -64,21 +64,17 @@ struct Row {
     __device__ __forceinline__ void store(T* p, uint32_t k, const float (&v)[kIn], bool past_caches) const
     {
         T* q = p + head + (uint64_t)k * kIn;
-        if constexpr (WHOLE) {
-            u32x4 w;
-            if constexpr (sizeof(T) == 4) {
+        u32x4 w;
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (uint32_t e = 0; e < kIn; ++e) w[e] = __float_as_uint(v[e]);
-            } else {
-#pragma unroll
-                for (uint32_t e = 0; e < kIn / 2; ++e) w[e] = pack2<DTYPE>(v[2 * e], v[2 * e + 1]);
-            }
-            if (past_caches) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(q));
-            else *reinterpret_cast<u32x4*>(q) = w;
+            for (uint32_t e = 0; e < kIn; ++e) w[e] = __float_as_uint(v[e]);
         } else {
 #pragma unroll
-            for (uint32_t e = 0; e < kIn; ++e) q[e] = E::store(v[e]);
+            for (uint32_t e = 0; e < kIn / 2; ++e) w[e] = pack2<DTYPE>(v[2 * e], v[2 * e + 1]);
         }
+        if constexpr (!WHOLE) __builtin_memcpy(q, &w, 16);         // stored at any address
+        else if (past_caches) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(q));
+        else *reinterpret_cast<u32x4*>(q) = w;
     }
 };
 

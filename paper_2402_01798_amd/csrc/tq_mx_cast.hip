@@ -1,4 +1,6 @@
 // Matrices to microscaled 4-bit form and back (tq_mx.h).
+#include <type_traits>
+
 #include "tq_mx_device.h"
 
 namespace tq {
@@ -16,7 +18,7 @@ struct CastArgs {
 
 // Along the rows: a lane takes 8 elements, four lanes a block, 16 lanes a group.  A workgroup is 2^log_lanes lanes along a row
 // times as many rows as fit.
-template <int DTYPE, bool STOCHASTIC, bool VEC>
+template <int DTYPE, bool STOCHASTIC>
 __global__ __launch_bounds__(256) void mx_cast_rows_kernel(CastArgs a)
 {
     using T = typename Element<DTYPE>::type;
@@ -29,7 +31,9 @@ __global__ __launch_bounds__(256) void mx_cast_rows_kernel(CastArgs a)
     if (row >= a.rows || oct >= a.groups * 16) return;           // 16 lanes of a group leave together
     const int n = (int)min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8);
     float v[8];
-    load8<DTYPE, VEC>(static_cast<const T*>(a.x) + row * a.ld + (uint64_t)oct * 8, n, v);
+    const T* x = static_cast<const T*>(a.x);
+    if constexpr (STOCHASTIC) x += round_toward_zero();
+    load8<DTYPE>(x + row * a.ld + (uint64_t)oct * 8, n, v);
     uint32_t draws[4] = {};
     if constexpr (STOCHASTIC) philox4x32_10(oct, (uint32_t)row, a.worker, a.step, a.k0, a.k1, draws);
     uint32_t largest = 0;
@@ -37,7 +41,14 @@ __global__ __launch_bounds__(256) void mx_cast_rows_kernel(CastArgs a)
     for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
     largest = quad_max(largest);
     const uint32_t byte = mx_scale_byte<STOCHASTIC>(largest);
-    const uint32_t w = mx_codes<STOCHASTIC>(v, byte, draws);
+    uint32_t w = 0;
+    if constexpr (STOCHASTIC) {
+#pragma unroll
+        for (int j = 7; j >= 0; --j) w = mx_push(w, v[j], byte, mx_draw(draws[j / 2], j & 1));
+        if (byte == 255) w = 0;
+    } else {
+        w = mx_nearest(v, byte);
+    }
     reinterpret_cast<uint32_t*>(a.codes)[row * (a.groups * 16) + oct] = w;
     if ((oct & 3) == 0) a.scales[((uint64_t)(oct / 16) * a.rows + row) * 4 + (oct / 4 & 3)] = (uint8_t)byte;
 }
@@ -46,7 +57,7 @@ __global__ __launch_bounds__(256) void mx_cast_rows_kernel(CastArgs a)
 // either direction.  Lane 4 c + r of a wavefront holds columns 8 c .. 8 c + 7 of rows 8 r .. 8 r + 7: a row's block is
 // four lanes 4 apart, a column's four neighbouring lanes.  The transposed codes go through LDS, so that a column's 64 bytes are
 // written at once.
-template <int DTYPE, bool STOCHASTIC, bool VEC, bool ROWS>
+template <int DTYPE, bool STOCHASTIC, bool ROWS>
 __global__ __launch_bounds__(256) void mx_cast_tile_kernel(CastArgs a)
 {
     using T = typename Element<DTYPE>::type;
@@ -58,55 +69,85 @@ __global__ __launch_bounds__(256) void mx_cast_tile_kernel(CastArgs a)
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 2, r = lane & 3;
     const uint32_t row0 = ty * 128 + wave * 32 + r * 8, oct = tx * 16 + c;
     const int n = (int)max(min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8), (int64_t)0);
-    float v[8][8];
+    const T* x = static_cast<const T*>(a.x);
+    if constexpr (STOCHASTIC) x += round_toward_zero();
+    Eight<DTYPE> held[8];
+    x += (uint64_t)oct * 8;
+    if (n >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) held[i].load(x + (uint64_t)min(row0 + i, a.rows - 1) * a.ld);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) held[i].load(x + (uint64_t)min(row0 + i, a.rows - 1) * a.ld, n);
+    }
+    if (row0 + 8 > a.rows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (row0 + i >= a.rows) held[i].clear();
+    }
+    uint32_t byte_t[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t row = row0 + i;
-        load8<DTYPE, VEC>(static_cast<const T*>(a.x) + (uint64_t)min(row, a.rows - 1) * a.ld + (uint64_t)oct * 8, row < a.rows ? n : 0, v[i]);
+        float v[8];
+        held[i].unpack(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) byte_t[j] = max(byte_t[j], magnitude_bits(v[j]));
     }
-    uint32_t byte_t[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        uint32_t largest = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude_bits(v[i][j]));
-        byte_t[j] = mx_scale_byte<STOCHASTIC>(quad_max(largest));
+        byte_t[j] = mx_scale_byte<STOCHASTIC>(quad_max(byte_t[j]));
         if (r == 0) scale_t[c * 8 + j][wave] = (uint8_t)byte_t[j];
     }
     uint32_t w_t[8] = {};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    auto along_the_row = [&](int i, const float (&v)[8]) {       // and, rounded stochastically, down the columns
         const uint32_t row = row0 + i;
-        uint32_t draws[4] = {};
-        if constexpr (STOCHASTIC) philox4x32_10(oct, row, a.worker, a.step, a.k0, a.k1, draws);
+        uint32_t byte = 0, w = 0;
         if constexpr (ROWS) {
             uint32_t largest = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[i][j]));
-            const uint32_t byte = mx_scale_byte<STOCHASTIC>(stride4_max(largest));
-            const uint32_t w = mx_codes<STOCHASTIC>(v[i], byte, draws);
+            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
+            byte = mx_scale_byte<STOCHASTIC>(stride4_max(largest));
+        }
+        if constexpr (STOCHASTIC) {
+            uint32_t draws[4], o = oct;
+            asm volatile("" : "+v"(o));                          // not all rows' draws first: they would wait in registers
+            philox4x32_10(o, row, a.worker, a.step, a.k0, a.k1, draws);
+#pragma unroll
+            for (int j = 7; j >= 0; --j) {
+                const uint32_t d = mx_draw(draws[j / 2], j & 1);
+                w_t[j] = mx_push(w_t[j], v[j], byte_t[j], d);
+                if constexpr (ROWS) w = mx_push(w, v[j], byte, d);
+                asm volatile("" : "+v"(w_t[j]));                 // here and not where it is stored, for which what goes into it would
+            }                                                    // have to be kept
+            if (byte == 255) w = 0;
+        } else if constexpr (ROWS) {
+            w = mx_nearest(v, byte);
+        }
+        if constexpr (ROWS) {
             if (row < a.rows) reinterpret_cast<uint32_t*>(a.codes)[(uint64_t)row * (a.groups * 16) + oct] = w;
             if ((c & 3) == 0) scale[wave * 32 + r * 8 + i][c / 4] = (uint8_t)byte;
         }
-        if constexpr (STOCHASTIC) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t d = j & 1 ? draws[j / 2] >> 16 : draws[j / 2] & 0xFFFFu;
-                w_t[j] |= (mx_draw(v[i][j], (int)byte_t[j], d) | (__float_as_uint(v[i][j]) >> 28 & 8u)) << (4 * i);
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    };
+    auto two_rows = [&](auto P) {
+        constexpr int p = decltype(P)::value;
+        float even[8], odd[8];
+        held[2 * p + 1].unpack(odd);
+        along_the_row(2 * p + 1, odd);
+        held[2 * p].unpack(even);
+        along_the_row(2 * p, even);
         if constexpr (!STOCHASTIC) {
-            const float column[8] = {v[0][j], v[1][j], v[2][j], v[3][j], v[4][j], v[5][j], v[6][j], v[7][j]};
-            const uint32_t none[4] = {};
-            w_t[j] = mx_codes<false>(column, byte_t[j], none);
-        } else if (byte_t[j] == 255) {
-            w_t[j] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                w_t[j] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w_t[j], even[j], odd[j], __uint_as_float(byte_t[j] << 23), p);
         }
-        codes_t[c * 8 + j][wave * 4 + r] = w_t[j];
-    }
+        __builtin_amdgcn_sched_barrier(0);                       // one pair after the other: fewer registers
+    };
+    two_rows(std::integral_constant<int, 3>{});                  // downwards: mx_push puts the last one lowest
+    two_rows(std::integral_constant<int, 2>{});
+    two_rows(std::integral_constant<int, 1>{});
+    two_rows(std::integral_constant<int, 0>{});
+#pragma unroll
+    for (int j = 0; j < 8; ++j) codes_t[c * 8 + j][wave * 4 + r] = byte_t[j] == 255 ? 0 : w_t[j];
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -129,7 +170,7 @@ __global__ __launch_bounds__(256) void mx_cast_tile_kernel(CastArgs a)
 }
 
 // Back: a lane takes 8 elements, as in mx_cast_rows_kernel.
-template <int DTYPE, bool VEC>
+template <int DTYPE>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(CastArgs a)
 {
     using T = typename Element<DTYPE>::type;
@@ -156,22 +197,22 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(CastArgs a)
         v[2 * j + 1] = p.y * scale;
     }
     const int n = (int)min((int64_t)a.cols - (int64_t)oct * 8, (int64_t)8);
-    store8<DTYPE, VEC>(static_cast<T*>(const_cast<void*>(a.x)) + row * a.ld + (uint64_t)oct * 8, n, v);
+    store8<DTYPE>(static_cast<T*>(const_cast<void*>(a.x)) + row * a.ld + (uint64_t)oct * 8, n, v);
 }
 
-template <int DTYPE, bool STOCHASTIC, bool VEC>
-void launch_cast(const CastArgs& a, bool rows, bool cols, dim3 grid, hipStream_t st)
+template <int DTYPE, bool STOCHASTIC>
+void launch_cast(const CastArgs& a, dim3 grid, hipStream_t st)
 {
-    if (!cols) mx_cast_rows_kernel<DTYPE, STOCHASTIC, VEC><<<grid, 256, 0, st>>>(a);
-    else if (rows) mx_cast_tile_kernel<DTYPE, STOCHASTIC, VEC, true><<<grid, 256, 0, st>>>(a);
-    else mx_cast_tile_kernel<DTYPE, STOCHASTIC, VEC, false><<<grid, 256, 0, st>>>(a);
+    if (!a.codes_t) mx_cast_rows_kernel<DTYPE, STOCHASTIC><<<grid, 256, 0, st>>>(a);
+    else if (a.codes) mx_cast_tile_kernel<DTYPE, STOCHASTIC, true><<<grid, 256, 0, st>>>(a);
+    else mx_cast_tile_kernel<DTYPE, STOCHASTIC, false><<<grid, 256, 0, st>>>(a);
 }
 
 template <int DTYPE>
-void launch_cast(const CastArgs& a, bool stochastic, bool vec, bool rows, bool cols, dim3 grid, hipStream_t st)
+void launch_cast(const CastArgs& a, bool stochastic, dim3 grid, hipStream_t st)
 {
-    if (stochastic) vec ? launch_cast<DTYPE, true, true>(a, rows, cols, grid, st) : launch_cast<DTYPE, true, false>(a, rows, cols, grid, st);
-    else vec ? launch_cast<DTYPE, false, true>(a, rows, cols, grid, st) : launch_cast<DTYPE, false, false>(a, rows, cols, grid, st);
+    if (stochastic) launch_cast<DTYPE, true>(a, grid, st);
+    else launch_cast<DTYPE, false>(a, grid, st);
 }
 
 // Lanes along a row and workgroups of the kernels that go along the rows.
@@ -183,12 +224,6 @@ bool rows_grid(CastArgs& a, uint64_t octs, dim3& grid)
     const uint64_t per = 256u >> a.log_lanes;
     a.tiles = a.tiles_x * ((a.rows + per - 1) / per);
     return fold_grid(a.tiles, 256, 1, grid);
-}
-
-bool whole_lines(const void* p, uint64_t ld, int dtype)
-{
-    const uint64_t size = dtype == TQ_F32 ? 4 : 2;
-    return ((reinterpret_cast<uintptr_t>(p) | ld * size) & 15u) == 0;
 }
 
 }  // namespace
@@ -222,10 +257,10 @@ hipError_t tq_launch_mx_quantize(const void* x, int dtype, uint64_t rows, uint64
     } else if (!rows_grid(a, (uint64_t)a.groups * 16, grid)) {
         return hipErrorInvalidValue;
     }
-    const bool vec = whole_lines(x, ld, dtype), stochastic = rounding == TQ_MX_STOCHASTIC;
-    if (dtype == TQ_F32) launch_cast<TQ_F32>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
-    else if (dtype == TQ_BF16) launch_cast<TQ_BF16>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
-    else launch_cast<TQ_F16>(a, stochastic, vec, codes != nullptr, codes_t != nullptr, grid, st);
+    const bool stochastic = rounding == TQ_MX_STOCHASTIC;
+    if (dtype == TQ_F32) launch_cast<TQ_F32>(a, stochastic, grid, st);
+    else if (dtype == TQ_BF16) launch_cast<TQ_BF16>(a, stochastic, grid, st);
+    else launch_cast<TQ_F16>(a, stochastic, grid, st);
     return hipGetLastError();
 }
 
@@ -243,8 +278,7 @@ hipError_t tq_launch_mx_dequantize(const void* codes, const void* scales, uint64
     a.groups = (uint32_t)((cols + kMxGroup - 1) / kMxGroup);
     dim3 grid;
     if (!rows_grid(a, (cols + 7) / 8, grid)) return hipErrorInvalidValue;
-    const bool vec = whole_lines(out, ldo, dtype);
-    if (dtype == TQ_F32) vec ? mx_dequantize_kernel<TQ_F32, true><<<grid, 256, 0, st>>>(a) : mx_dequantize_kernel<TQ_F32, false><<<grid, 256, 0, st>>>(a);
-    else vec ? mx_dequantize_kernel<TQ_BF16, true><<<grid, 256, 0, st>>>(a) : mx_dequantize_kernel<TQ_BF16, false><<<grid, 256, 0, st>>>(a);
+    if (dtype == TQ_F32) mx_dequantize_kernel<TQ_F32><<<grid, 256, 0, st>>>(a);
+    else mx_dequantize_kernel<TQ_BF16><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }

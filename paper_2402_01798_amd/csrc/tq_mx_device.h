@@ -64,21 +64,18 @@ __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b)
     }
 }
 
-// 8 consecutive elements, `n` of them there (the rest 0).  VEC: the address is 16-byte aligned.
-template <int DTYPE, bool VEC>
+// 8 consecutive elements, `n` of them there (the rest 0).  Whole ones are fetched 16 bytes at a time from any address: the memory
+// unit takes addresses that are no multiple of 16 (rows of an odd length) at little more than the cost of aligned ones.
+template <int DTYPE>
 __device__ __forceinline__ void load8(const typename Element<DTYPE>::type* p, int n, float (&v)[8])
 {
     using E = Element<DTYPE>;
-    if (VEC && n >= 8) {
+    if (n >= 8) {
         if constexpr (DTYPE == TQ_F32) {
-            const float4_native a = *reinterpret_cast<const float4_native*>(p), b = *reinterpret_cast<const float4_native*>(p + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = a[j];
-                v[4 + j] = b[j];
-            }
+            __builtin_memcpy(v, p, 32);
         } else {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+            u32x4 w;
+            __builtin_memcpy(&w, p, 16);
 #pragma unroll
             for (int j = 0; j < 4; ++j) unpack2<DTYPE>(w[j], v[2 * j], v[2 * j + 1]);
         }
@@ -88,19 +85,53 @@ __device__ __forceinline__ void load8(const typename Element<DTYPE>::type* p, in
     }
 }
 
-template <int DTYPE, bool VEC>
+// The same, left as they are in memory.  `unpack` makes fp32 values of them, and new ones each time: kept from one use to the
+// next they would take twice the registers.
+template <int DTYPE>
+struct Eight {
+    u32x4 w[DTYPE == TQ_F32 ? 2 : 1];
+
+    __device__ __forceinline__ void load(const typename Element<DTYPE>::type* p) { __builtin_memcpy(w, p, sizeof(w)); }
+    __device__ __forceinline__ void load(const typename Element<DTYPE>::type* p, int n)      // n < 8 of them
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const typename Element<DTYPE>::type v = j < n ? p[j] : 0;
+            if constexpr (DTYPE == TQ_F32) w[j / 4][j % 4] = __float_as_uint(v);
+            else w[0][j / 2] = j & 1 ? w[0][j / 2] | (uint32_t)v << 16 : (uint32_t)v;
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (DTYPE == TQ_F32) w[1] = w[0];
+    }
+    __device__ __forceinline__ void unpack(float (&v)[8])
+    {
+        asm volatile("" : "+v"(w[0]));
+        if constexpr (DTYPE == TQ_F32) {
+            asm volatile("" : "+v"(w[1]));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j / 4][j % 4]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpack2<DTYPE>(w[0][j], v[2 * j], v[2 * j + 1]);
+        }
+    }
+};
+
+template <int DTYPE>
 __device__ __forceinline__ void store8(typename Element<DTYPE>::type* p, int n, const float (&v)[8])
 {
     using E = Element<DTYPE>;
-    if (VEC && n >= 8) {
+    if (n >= 8) {
         if constexpr (DTYPE == TQ_F32) {
-            reinterpret_cast<float4_native*>(p)[0] = float4_native{v[0], v[1], v[2], v[3]};
-            reinterpret_cast<float4_native*>(p)[1] = float4_native{v[4], v[5], v[6], v[7]};
+            __builtin_memcpy(p, v, 32);
         } else {
             u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = pack2<DTYPE>(v[2 * j], v[2 * j + 1]);
-            *reinterpret_cast<u32x4*>(p) = w;
+            __builtin_memcpy(p, &w, 16);
         }
     } else {
 #pragma unroll
@@ -118,33 +149,37 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest)
     return largest >= 0x7F800000u ? 255u : (uint32_t)max(e, 0);
 }
 
-// The magnitude code 0..7 of |v| <= 6 * 2^(byte - 127), rounded stochastically by the 16 bits r.  k is the magnitude in units of
-// 2^-17 of the scale, so that a step of the grid is 2^16 units below 2, 2^17 below 4 and 2^18 above.
-__device__ __forceinline__ uint32_t mx_draw(float v, int byte, uint32_t r)
+// Stochastic rounding.  A magnitude t (in units of the scale, at most 6) times 2^-126 has, as an fp32 number, the grid's own
+// structure: below 1 it is subnormal and a step of 0.5 is 2^22 units in the last place, above it has one bit of the mantissa above
+// those 22.  So its bits, 16 random bits added where the fraction begins, are the code << 22 and what is dropped.  The product
+// has to be cut off, not rounded, where it is subnormal: round_toward_zero.  5 instructions an element and form, 11 as
+// comparisons and shifts of a fixed-point number.
+__device__ __forceinline__ uint32_t round_toward_zero()
 {
-    const uint32_t k = (uint32_t)__builtin_amdgcn_ldexpf(fabsf(v), 144 - byte);
-    const uint32_t s = min(k >> 18, 2u);
-    return (((k >> s) + r) >> 16) + 2 * s;
+    // bits 0 and 1 of the wavefront's mode: fp32 arithmetic.  Gives 0: what is loaded from an address that it is added to comes after.
+    uint32_t zero = 0;
+    asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 0, 2), 3" : "+s"(zero));
+    return zero;
+}
+// The element's 16 bits of a word of draws, as high as mx_push wants them.
+__device__ __forceinline__ uint32_t mx_draw(uint32_t word, bool high) { return high ? (word >> 16) << 12 : (word & 0xFFFFu) << 12; }
+// The word's codes, one to the left, and this element's.
+__device__ __forceinline__ uint32_t mx_push(uint32_t w, float v, uint32_t byte, uint32_t draw)
+{
+    const uint32_t bits = __float_as_uint(__builtin_amdgcn_ldexpf(fabsf(v), 1 - (int)byte));
+    const uint32_t x = (bits << 6) + draw;                              // the magnitude's code in bits 28..30
+    return __builtin_amdgcn_alignbit(w, (x & 0x7FFFFFFFu) | (__float_as_uint(v) & 0x80000000u), 28);
 }
 
 // 8 codes in a word, the first element's lowest.
-template <bool STOCHASTIC>
-__device__ __forceinline__ uint32_t mx_codes(const float (&v)[8], uint32_t byte, const uint32_t (&draws)[4])
+__device__ __forceinline__ uint32_t mx_nearest(const float (&v)[8], uint32_t byte)
 {
+    const float scale = __uint_as_float(byte << 23);                    // the instruction takes the exponent field alone
     uint32_t w = 0;
-    if constexpr (STOCHASTIC) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t r = j & 1 ? draws[j / 2] >> 16 : draws[j / 2] & 0xFFFFu;
-            w |= (mx_draw(v[j], (int)byte, r) | (__float_as_uint(v[j]) >> 28 & 8u)) << (4 * j);
-        }
-    } else {
-        const float scale = __uint_as_float(byte << 23);                // the instruction takes the exponent field alone
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
-    }
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
     return byte == 255 ? 0u : w;
 }
 

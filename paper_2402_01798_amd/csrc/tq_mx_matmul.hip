@@ -225,8 +225,8 @@ constexpr uint32_t kFewRowsInForm = 16, kFewRows = 32;
 __host__ __device__ constexpr uint64_t few_row_bytes(uint64_t groups) { return groups * 64 + 16; }
 __host__ __device__ constexpr uint64_t few_bytes(uint64_t m, uint64_t groups) { return kFewRing + m * (few_row_bytes(groups) + groups * 4); }
 
-// X: the type of g.x, or -1 for rows in 4-bit form.  VEC: rows of x are 16-byte aligned.
-template <int DTYPE, int X, bool VEC>
+// X: the type of g.x, or -1 for rows in 4-bit form.
+template <int DTYPE, int X>
 __global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArgs g)
 {
     extern __shared__ char lds[];
@@ -276,13 +276,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArg
         for (uint32_t i = threadIdx.x; i < g.m * octs; i += kFewWaves * 64) {
             const uint32_t row = i / octs, oct = i - row * octs;
             float v[8];
-            load8<X, VEC>(static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
+            load8<X>(static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
             uint32_t largest = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
             const uint32_t byte = mx_scale_byte<false>(quad_max(largest));
-            const uint32_t none[4] = {};
-            *reinterpret_cast<uint32_t*>(codes + row * row_bytes + oct * 4) = mx_codes<false>(v, byte, none);
+            *reinterpret_cast<uint32_t*>(codes + row * row_bytes + oct * 4) = mx_nearest(v, byte);
             if ((oct & 3) == 0) scales[row * octs / 4 + oct / 4] = (char)byte;
         }
     }
@@ -352,9 +351,7 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
     dim3 grid;
     if (!fold_grid(g.tiles, kFewWaves * 64, 1, grid)) return hipErrorInvalidValue;
     const uint32_t bytes = (uint32_t)few_bytes(g.m, g.groups);
-    const bool vec = X >= 0 && ((reinterpret_cast<uintptr_t>(g.x) | g.ldx * (X == TQ_F32 ? 4 : 2)) & 15u) == 0;
-    if (vec) mx_matmul_few_kernel<DTYPE, X, true><<<grid, kFewWaves * 64, bytes, st>>>(g);
-    else mx_matmul_few_kernel<DTYPE, X, false><<<grid, kFewWaves * 64, bytes, st>>>(g);
+    mx_matmul_few_kernel<DTYPE, X><<<grid, kFewWaves * 64, bytes, st>>>(g);
     return hipGetLastError();
 }
 
