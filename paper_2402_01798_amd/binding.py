@@ -14,7 +14,7 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 try:
     from . import _tq_marshal
-    if getattr(_tq_marshal, "interface", 0) != 1:
+    if getattr(_tq_marshal, "interface", 0) != 3:
         raise ImportError("built from other sources than this file's")
 except ImportError as e:                # the loops below do the same, slower
     _tq_marshal = None
@@ -113,7 +113,7 @@ def lib():
         for f in (L.tq_mx_quantize, L.tq_mx_dequantize, L.tq_mx_matmul, L.tq_mx_linear, L.tq_distill_forward,
                   L.tq_distill_backward, L.tq_distill):
             f.restype = i32
-        for name in _NATIVE:
+        for name in (*_NATIVE, *_NATIVE_LEARN):
             f = getattr(L, name)
             f.address = C.cast(f, C.c_void_p).value
         _lib = L
@@ -128,6 +128,26 @@ _NATIVE = {"tq_stats": "stats", "tq_stats_multi": "stats_multi", "tq_params": "p
            "tq_stats_segments": "stats_segments", "tq_stats_segments_multi": "stats_segments_multi",
            "tq_compress_segments": "compress_segments", "tq_compress_segments_multi": "compress_segments_multi",
            "tq_decompress_aggregate_segments": "aggregate_segments"}
+
+
+# The same for the calls of tq_mx.h and tq_distill.h.
+_NATIVE_LEARN = {"tq_mx_quantize": "mx_quantize", "tq_mx_dequantize": "mx_dequantize", "tq_mx_matmul": "mx_matmul",
+                 "tq_mx_linear": "mx_linear", "tq_distill_forward": "distill_forward", "tq_distill_backward": "distill_backward",
+                 "tq_distill": "distill"}
+_native_calls = {}
+
+
+def _native_learn(name, *args):
+    """As _native."""
+    call = _native_calls.get(name)
+    if call is None:
+        if _tq_marshal is None:
+            return False
+        call = _native_calls[name] = (getattr(_tq_marshal, _NATIVE_LEARN[name]), getattr(lib(), name).address)
+    rc = call[0](call[1], *args)
+    if rc:
+        raise TqError(rc, name)
+    return rc is not None
 
 
 def _native(name, *args):
@@ -565,11 +585,17 @@ class MxMatrix:
     def args(self):
         return self.codes.data_ptr(), self.scales.data_ptr()
 
+    def all(self):
+        return self.codes, self.scales, self.rows, self.cols
+
 
 def alloc_mx(rows, cols, device="cuda"):
     groups = -(-cols // 128)
     return MxMatrix(torch.empty((rows, 64 * groups), dtype=torch.uint8, device=device),
                     torch.empty((groups, rows, 4), dtype=torch.uint8, device=device), rows, cols)
+
+
+_NO_FORM = (None, None, None, None)
 
 
 def mx_matmul_workspace_bytes(m, n, k):
@@ -586,18 +612,22 @@ def _scratch(workspace):
 
 def tq_mx_quantize(x, form, form_t=None, rounding=MX_NEAREST, seed=0, worker=0, step=0):
     """``form`` takes x [rows, cols], ``form_t`` its transpose; either may be None."""
+    if _native_learn("tq_mx_quantize", x, *(_NO_FORM if form is None else form.all()),
+                     *(_NO_FORM if form_t is None else form_t.all()), rounding, seed, worker, step):
+        return form, form_t
     px, code, rows, cols, ld = _matrix(x, "x")
     if form is not None and (form.rows != rows or form.cols != cols):
         raise ValueError("form must be [%d, %d]" % (rows, cols))
     if form_t is not None and (form_t.rows != cols or form_t.cols != rows):
         raise ValueError("form_t must be [%d, %d]" % (cols, rows))
-    none = (None, None)
-    _check(lib().tq_mx_quantize(px, code, rows, cols, ld, rounding, seed, worker, step, *(none if form is None else form.args()),
-                                *(none if form_t is None else form_t.args()), _stream()), "tq_mx_quantize")
+    _check(lib().tq_mx_quantize(px, code, rows, cols, ld, rounding, seed, worker, step, *(_NO_FORM[:2] if form is None else form.args()),
+                                *(_NO_FORM[:2] if form_t is None else form_t.args()), _stream()), "tq_mx_quantize")
     return form, form_t
 
 
 def tq_mx_dequantize(form, out):
+    if _native_learn("tq_mx_dequantize", *form.all(), out):
+        return out
     po, code, rows, cols, ld = _matrix(out, "out")
     if (rows, cols) != (form.rows, form.cols):
         raise ValueError("out must be [%d, %d]" % (form.rows, form.cols))
@@ -607,6 +637,8 @@ def tq_mx_dequantize(form, out):
 
 def tq_mx_matmul(a, b, out, workspace=None, add=None):
     """out [m, n] = a [m, k] b [n, k]^T (+ add, float32, which may be out)."""
+    if _native_learn("tq_mx_matmul", *a.all(), *b.all(), out, workspace, add):
+        return out
     po, code, m, n, ld = _matrix(out, "out")
     if a.cols != b.cols or a.rows != m or b.rows != n:
         raise ValueError("[%d, %d] times [%d, %d]^T does not fit out [%d, %d]" % (a.rows, a.cols, b.rows, b.cols, m, n))
@@ -622,6 +654,8 @@ def tq_mx_matmul(a, b, out, workspace=None, add=None):
 
 def tq_mx_linear(x, w, out, workspace=None):
     """out [m, n] = Q(x [m, k]) w [n, k]^T, Q the nearest rounding to 4-bit form."""
+    if _native_learn("tq_mx_linear", x, *w.all(), out, workspace):
+        return out
     px, code, m, k, ldx = _matrix(x, "x")
     po, ocode, om, n, ldo = _matrix(out, "out")
     if w.cols != k or w.rows != n or om != m:
@@ -658,6 +692,8 @@ def _gradient(z, dz):
 
 def tq_distill_forward(z, ids, t, loss, stats, temperature=1.0):
     """``stats`` [rows, 2]: what tq_distill_backward needs of the row."""
+    if _native_learn("tq_distill_forward", z, ids, t, loss, stats, temperature):
+        return loss, stats
     args, out = _distill_args(z, ids, t, temperature, loss=loss, stats=stats)
     _check(lib().tq_distill_forward(*args, *out, _stream()), "tq_distill_forward")
     return loss, stats
@@ -665,6 +701,8 @@ def tq_distill_forward(z, ids, t, loss, stats, temperature=1.0):
 
 def tq_distill_backward(z, ids, t, stats, grad, dz, temperature=1.0):
     """``dz`` may be ``z``."""
+    if _native_learn("tq_distill_backward", z, ids, t, stats, grad, dz, temperature):
+        return dz
     args, rows = _distill_args(z, ids, t, temperature, stats=stats, grad=grad)
     _check(lib().tq_distill_backward(*args, *rows, *_gradient(z, dz), _stream()), "tq_distill_backward")
     return dz
@@ -672,6 +710,8 @@ def tq_distill_backward(z, ids, t, stats, grad, dz, temperature=1.0):
 
 def tq_distill(z, ids, t, grad, loss, dz, temperature=1.0):
     """Loss and gradient in one call; ``dz`` may be ``z``."""
+    if _native_learn("tq_distill", z, ids, t, grad, loss, dz, temperature):
+        return loss, dz
     args, rows = _distill_args(z, ids, t, temperature, grad=grad, loss=loss)
     _check(lib().tq_distill(*args, *rows, *_gradient(z, dz), _stream()), "tq_distill")
     return loss, dz

@@ -76,7 +76,7 @@ def build_marshal(force: bool = False, verbose: bool = False) -> str:
     from torch.utils import cpp_extension
 
     src = os.path.join(CSRC, "tq_marshal.cpp")
-    if force or _stale(MARSHAL, [src, os.path.join(ROOT, "include", "tq.h"), __file__]):
+    if force or _stale(MARSHAL, [src, *(os.path.join(ROOT, "include", h) for h in ("tq.h", "tq_mx.h", "tq_distill.h")), __file__]):
         lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
         tmp = MARSHAL + ".tmp.%d" % os.getpid()
         cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wno-attributes",

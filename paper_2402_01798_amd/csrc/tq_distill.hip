@@ -16,7 +16,7 @@ struct DistillArgs {
     float *loss, *stats;
     void* dz;
     uint64_t ldz, lddz;
-    uint32_t rows, vocab, top;
+    uint32_t rows, vocab, top, pieces;                             // workgroups of a row (kBackward)
     int wide_ids, past_caches;
     float tau, inv_tau;
 };
@@ -45,9 +45,20 @@ struct Row {
         if (tid >= kIn && tid - kIn < tail) return (int64_t)head + (uint64_t)vectors * kIn + (tid - kIn);
         return -1;
     }
+    // Whether element `at` is in the vectors k0 .. k1 - 1, or a loose one where k0 is 0.
+    __device__ __forceinline__ bool within(uint32_t at, uint32_t k0, uint32_t k1) const
+    {
+        const uint32_t k = (at - head) / kIn;
+        return at < head || k >= vectors ? k0 == 0 : k >= k0 && k < k1;
+    }
+    // NEAR: the row is short of 4 GiB, so that a vector's place in it is a 32-bit number beside the row's address, which all
+    // threads share.
+    template <bool NEAR>
     __device__ __forceinline__ u32x4 load(const T* p, uint32_t k) const
     {
-        return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p + head) + (uint64_t)k * 16);
+        const char* q = reinterpret_cast<const char*>(p + head);
+        if constexpr (NEAR) return *reinterpret_cast<const u32x4*>(q + k * 16u);
+        else return *reinterpret_cast<const u32x4*>(q + (uint64_t)k * 16);
     }
     static __device__ __forceinline__ void unpack(u32x4 w, float (&v)[kIn])
     {
@@ -60,10 +71,10 @@ struct Row {
         }
     }
     // Vector k of the gradient, which begins at p and lies as the row does (WHOLE) or not.
-    template <bool WHOLE>
+    template <bool NEAR, bool WHOLE>
     __device__ __forceinline__ void store(T* p, uint32_t k, const float (&v)[kIn], bool past_caches) const
     {
-        T* q = p + head + (uint64_t)k * kIn;
+        T* q = NEAR ? p + head + k * kIn : p + head + (uint64_t)k * kIn;
         u32x4 w;
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -104,6 +115,13 @@ __device__ __forceinline__ void group_reduce(float& x, float& y, float (*part)[2
     }
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;                                                       // fmaxf would first rewrite each operand, lest it be a signalling NaN
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
 // Running maximum and sum of exp((z - maximum) / tau) of a thread's elements.
 struct Softmax {
     float m = -INFINITY, s = 0.0f;
@@ -142,10 +160,13 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     float* t = reinterpret_cast<float*>(id + a.top);
     float* at_id = t + a.top;
     int* again = reinterpret_cast<int*>(at_id + a.top);
-    const uint32_t row = linear_block(), tid = threadIdx.x;
+    const uint32_t block = linear_block(), tid = threadIdx.x, row = MODE == kBackward ? block / a.pieces : block;
     if (row >= a.rows) return;
     const T* z = static_cast<const T*>(a.z) + (uint64_t)row * a.ldz;
     const R lies(z, a.vocab);
+    // this workgroup's vectors of the row, and with the first of them the loose elements
+    const uint32_t piece = MODE == kBackward ? block - row * a.pieces : 0, per = MODE == kBackward ? (lies.vectors + a.pieces - 1) / a.pieces : 0;
+    const uint32_t k_first = piece * per, k_end = MODE == kBackward ? min(k_first + per, lies.vectors) : lies.vectors;
     const float grad = MODE == kForward ? 0.0f : a.grad[row];
     const float c = a.inv_tau * kLog2e;
 
@@ -153,9 +174,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
 #pragma unroll
     for (int i = 0; i < VECTORS; ++i) {
         held[i] = u32x4{R::kNothing, R::kNothing, R::kNothing, R::kNothing};
-        if (tid + i * THREADS < lies.vectors) held[i] = lies.load(z, tid + i * THREADS);
+        if (tid + i * THREADS < lies.vectors) held[i] = lies.template load<true>(z, tid + i * THREADS);
     }
-    const int64_t loose = lies.loose(tid);
+    const int64_t loose = piece == 0 ? lies.loose(tid) : -1;
     const float z_loose = loose >= 0 ? E::load(z[loose]) : -INFINITY;
 
     float t_peak = -INFINITY;
@@ -168,7 +189,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         id[i] = there ? (int)w : -1;
         t[i] = v;
         again[i] = 0;
-        at_id[i] = there ? E::load(z[w]) : 0.0f;
+        // (another piece's elements may be gradients by now, where dz is z)
+        at_id[i] = there && (MODE != kBackward || lies.within((uint32_t)w, k_first, k_end)) ? E::load(z[w]) : 0.0f;
         if (there) {
             t_peak = fmaxf(t_peak, v);
             bad |= !(v < INFINITY);
@@ -196,7 +218,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
             float v[IN];
             R::unpack(held[i], v);
 #pragma unroll
-            for (uint32_t j = 0; j < IN; ++j) top = fmaxf(top, v[j]);
+            for (uint32_t j = 0; j < IN; j += 2) top = max3(top, v[j], v[j + 1]);
         }
     } else if constexpr (MODE != kBackward) {
         const float first[1] = {z_loose};
@@ -204,7 +226,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
 #pragma unroll 4
         for (uint32_t k = tid; k < lies.vectors; k += THREADS) {
             float v[IN];
-            R::unpack(lies.load(z, k), v);
+            R::unpack(lies.template load<false>(z, k), v);
             q.take(v, c);
         }
         top = q.m;
@@ -214,34 +236,31 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     for (uint32_t i = tid; i < a.top; i += THREADS)
         if (id[i] >= 0) t_sum += __builtin_amdgcn_exp2f((t[i] - t_peak) * c);
     if (bad) t_sum = NAN;
-    if constexpr (MODE != kBackward) {
-        const float low = top == -INFINITY ? 0.0f : top;
-        if constexpr (VECTORS > 0) {
-            total = __builtin_amdgcn_exp2f((z_loose - low) * c);
+    if constexpr (MODE == kBackward) {
+        top = a.stats_in[2 * (uint64_t)row];
+        log_total = a.stats_in[2 * (uint64_t)row + 1];
+    }
+    const float low = top == -INFINITY ? 0.0f : top;               // -inf - -inf has no value
+    auto power = [&](float v) { return __builtin_amdgcn_exp2f((v - low) * c); };
+    if constexpr (MODE != kBackward && VECTORS > 0) {
+        total = power(z_loose);
 #pragma unroll
-            for (int i = 0; i < VECTORS; ++i) {
-                float v[IN];
-                keep_packed(held[i]);
-                R::unpack(held[i], v);
+        for (int i = 0; i < VECTORS; ++i) {
+            float v[IN];
+            keep_packed(held[i]);
+            R::unpack(held[i], v);
 #pragma unroll
-                for (uint32_t j = 0; j < IN; ++j) total += __builtin_amdgcn_exp2f((v[j] - low) * c);
-            }
-        } else {
-            total = q.m == -INFINITY ? q.s : q.s * __builtin_amdgcn_exp2f((q.m - low) * c);
+            for (uint32_t j = 0; j < IN; ++j) total += power(v[j]);
         }
+    } else if constexpr (MODE != kBackward) {
+        total = q.m == -INFINITY ? q.s : q.s * power(q.m);
     }
     group_reduce<WAVES, false>(t_sum, total, parts[1]);
     const bool empty = t_sum == 0.0f;
     const float t_log = empty ? 0.0f : logf(t_sum);
-    if constexpr (MODE == kBackward) {
-        top = a.stats_in[2 * (uint64_t)row];
-        log_total = a.stats_in[2 * (uint64_t)row + 1];
-    } else {
-        log_total = logf(total);
-    }
-    // where nothing is left of the row every z is -inf and q is 0: any finite numbers do
-    const bool none = log_total == -INFINITY;
-    const float low = none || top == -INFINITY ? 0.0f : top, log_low = none ? 0.0f : log_total;
+    if constexpr (MODE != kBackward) log_total = logf(total);
+    // where nothing is left of the row every z is -inf and q is 0: any finite number does
+    const float log_low = log_total == -INFINITY ? 0.0f : log_total;
 
     float loss = 0.0f, count = twice ? 1.0f : 0.0f;
     for (uint32_t i = tid; i < a.top; i += THREADS) {
@@ -262,38 +281,41 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         const bool counts = !empty && grad != 0.0f;
         const float g = t_sum != t_sum ? NAN : a.tau * grad;       // a teacher without a value leaves none to any element
         const float scale = counts ? g * __builtin_amdgcn_exp2f(-log_low * kLog2e) : 0.0f;
-        auto gradient = [&](float v) { return counts ? scale * __builtin_amdgcn_exp2f((v - low) * c) : 0.0f; };
         // (the reductions' barriers: every z[id] is read where dz is z)
-        if (loose >= 0) dz[loose] = E::store(gradient(z_loose));
+        if (loose >= 0) dz[loose] = E::store(counts ? scale * power(z_loose) : 0.0f);
+        const float from = counts ? low : 0.0f;                    // of a row that does not count zeros are left: 0 * 2^0
         auto put = [&](uint32_t k, u32x4 w) {
             float v[IN];
             R::unpack(w, v);
 #pragma unroll
-            for (uint32_t j = 0; j < IN; ++j) v[j] = gradient(v[j]);
-            lies.template store<WHOLE>(dz, k, v, a.past_caches);
+            for (uint32_t j = 0; j < IN; ++j) v[j] = scale * __builtin_amdgcn_exp2f((v[j] - from) * c);
+            lies.template store<(VECTORS > 0), WHOLE>(dz, k, v, a.past_caches);
         };
         if constexpr (VECTORS > 0) {
+            if (!counts) {
 #pragma unroll
-            for (int i = 0; i < VECTORS; ++i)
-                if (tid + i * THREADS < lies.vectors) {
-                    keep_packed(held[i]);
-                    put(tid + i * THREADS, held[i]);
-                }
+                for (int i = 0; i < VECTORS; ++i) held[i] = u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int i = 0; i < VECTORS; ++i) {
+                keep_packed(held[i]);
+                if (tid + i * THREADS < lies.vectors) put(tid + i * THREADS, held[i]);
+            }
         } else if (counts) {
 #pragma unroll 4
-            for (uint32_t k = tid; k < lies.vectors; k += THREADS) put(k, lies.load(z, k));
+            for (uint32_t k = k_first + tid; k < k_end; k += THREADS) put(k, lies.template load<false>(z, k));
         } else {
-            for (uint32_t k = tid; k < lies.vectors; k += THREADS) put(k, u32x4{0, 0, 0, 0});
+            for (uint32_t k = k_first + tid; k < k_end; k += THREADS) put(k, u32x4{0, 0, 0, 0});
         }
         if (!counts) return;
         __syncthreads();                                           // the elements that the teacher names are written once more
         for (uint32_t i = tid; i < a.top; i += THREADS)
-            if (id[i] >= 0 && !again[i]) {
+            if (id[i] >= 0 && !again[i] && lies.within(id[i], k_first, k_end)) {
                 float p = t[i];
                 if (count != 0.0f)
                     for (uint32_t j = i + 1; j < a.top; ++j)
                         if (id[j] == id[i]) p += t[j];
-                dz[id[i]] = E::store(scale * __builtin_amdgcn_exp2f((at_id[i] - low) * c) - g * p);
+                dz[id[i]] = E::store(scale * power(at_id[i]) - g * p);
             }
     }
 }
@@ -302,7 +324,7 @@ template <int DTYPE, int MODE, int THREADS, int VECTORS>
 hipError_t launch(const DistillArgs& a, hipStream_t st)
 {
     dim3 grid;
-    if (!fold_grid(a.rows, THREADS, 1, grid)) return hipErrorInvalidValue;
+    if (!fold_grid((uint64_t)a.rows * a.pieces, THREADS, 1, grid)) return hipErrorInvalidValue;
     const size_t entries = 16 * (size_t)a.top;
     if constexpr (MODE != kForward) {
         const uint64_t size = DTYPE == TQ_F32 ? 4 : 2;
@@ -316,24 +338,33 @@ hipError_t launch(const DistillArgs& a, hipStream_t st)
 }
 
 template <int DTYPE, int MODE>
-hipError_t launch(const DistillArgs& a, hipStream_t st)
+hipError_t launch(DistillArgs& a, hipStream_t st)
 {
     const uint64_t vectors = (uint64_t)a.vocab / Row<DTYPE>::kIn;
-    if constexpr (MODE == kBackward) {
-        if (vectors <= 256) return launch<DTYPE, MODE, 64, 0>(a, st);
-        return vectors <= 4096 ? launch<DTYPE, MODE, 256, 0>(a, st) : launch<DTYPE, MODE, 1024, 0>(a, st);
-    } else {
+    if constexpr (MODE == kForward) {
+        if (vectors <= 64 * 4) return launch<DTYPE, MODE, 64, 4>(a, st);
+        if (vectors <= 256 * 4) return launch<DTYPE, MODE, 256, 4>(a, st);
+        if (vectors <= 512 * 8) return launch<DTYPE, MODE, 512, 8>(a, st);
+        return launch<DTYPE, MODE, 1024, 0>(a, st);
+    } else if constexpr (MODE == kBoth) {
         if (vectors <= 64 * 4) return launch<DTYPE, MODE, 64, 4>(a, st);
         if (vectors <= 256 * 4) return launch<DTYPE, MODE, 256, 4>(a, st);
         if (vectors <= 512 * 8) return launch<DTYPE, MODE, 512, 8>(a, st);
         if (vectors <= 1024 * 8) return launch<DTYPE, MODE, 1024, 8>(a, st);
         if (vectors <= 1024 * 16) return launch<DTYPE, MODE, 1024, 16>(a, st);
         return launch<DTYPE, MODE, 1024, 0>(a, st);
+    } else {
+        if (vectors <= 256) return launch<DTYPE, MODE, 64, 0>(a, st);
+        const uint64_t wanted = 1024 / a.rows, most = vectors / 1024;      // a few workgroups for each compute unit, 4 vectors a thread
+        a.pieces = (uint32_t)(most < wanted ? most : wanted);
+        if (a.pieces < 1) a.pieces = 1;
+        if (vectors <= 4096 || a.pieces > 1) return launch<DTYPE, MODE, 256, 0>(a, st);
+        return launch<DTYPE, MODE, 1024, 0>(a, st);
     }
 }
 
 template <int MODE>
-hipError_t launch(const DistillArgs& a, int dtype, hipStream_t st)
+hipError_t launch(DistillArgs& a, int dtype, hipStream_t st)
 {
     if (dtype == TQ_F32) return launch<TQ_F32, MODE>(a, st);
     return dtype == TQ_BF16 ? launch<TQ_BF16, MODE>(a, st) : launch<TQ_F16, MODE>(a, st);
@@ -361,6 +392,7 @@ hipError_t tq_launch_distill(const void* z, int dtype, uint64_t rows, uint64_t v
     a.rows = (uint32_t)rows;
     a.vocab = (uint32_t)vocab;
     a.top = (uint32_t)top;
+    a.pieces = 1;
     a.wide_ids = ids_bytes == 8;
     a.tau = temperature;
     a.inv_tau = 1.0f / temperature;

@@ -14,6 +14,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "tq.h"
+#include "tq_distill.h"
+#include "tq_mx.h"
 
 namespace {
 
@@ -483,6 +485,187 @@ PyObject* call_aggregate_segments(Args in)
                   bits, accumulate, out);
 }
 
+// ---- the calls of tq_mx.h and tq_distill.h
+
+// A matrix of floating-point numbers whose rows may be apart: address, type, rows, columns, row length.
+struct Dense {
+    void* p = nullptr;
+    int dtype = -1;
+    uint64_t rows = 0, cols = 0, ld = 0;
+
+    Dense(Args& in, Py_ssize_t i)
+    {
+        if (!in.ok || !THPVariable_CheckExact(in.a[i])) { in.ok = false; return; }
+        const at::Tensor& t = THPVariable_Unpack(in.a[i]);
+        const at::ScalarType type = t.scalar_type();
+        dtype = type == at::kFloat ? TQ_F32 : type == at::kBFloat16 ? TQ_BF16 : type == at::kHalf ? TQ_F16 : -1;
+        if (dtype < 0 || !t.is_cuda() || t.dim() != 2) { in.ok = false; return; }
+        const int64_t r = t.size(0), c = t.size(1), step = t.stride(1);
+        int64_t length = t.stride(0);
+        if (r < 1 || c < 1 || (step != 1 && c > 1)) { in.ok = false; return; }
+        if (r == 1 && length < c) length = c;
+        if (length < c) { in.ok = false; return; }
+        p = t.data_ptr();
+        rows = (uint64_t)r;
+        cols = (uint64_t)c;
+        ld = (uint64_t)length;
+    }
+};
+
+// A matrix in 4-bit form: codes, scales, rows, columns, as the binding's MxMatrix holds them; all None where one is not wanted.
+struct Form {
+    void *codes = nullptr, *scales = nullptr;
+    uint64_t rows = 0, cols = 0;
+
+    Form(Args& in, Py_ssize_t i, bool wanted = true)
+    {
+        if (!in.ok || (!wanted && in.a[i] == Py_None)) return;
+        rows = in.u64(i + 2, INT32_MAX);
+        cols = in.u64(i + 3, INT32_MAX);
+        const long long groups = (long long)((cols + 127) / 128), n = (long long)rows * groups;
+        codes = in.address(i, n * 64, n * 64);
+        scales = in.address(i + 1, n * 4, n * 4);
+        if (in.ok && (byte(in, i) || byte(in, i + 1))) in.ok = false;
+    }
+    static bool byte(const Args& in, Py_ssize_t i) { return THPVariable_Unpack(in.a[i]).scalar_type() != at::kByte; }
+};
+
+// Scratch memory, or None.
+struct Scratch {
+    void* p = nullptr;
+    uint64_t bytes = 0;
+
+    Scratch(Args& in, Py_ssize_t i)
+    {
+        if (!in.ok || in.a[i] == Py_None) return;
+        const at::Tensor* t = in.tensor(i);
+        if (!t) return;
+        p = t->data_ptr();
+        bytes = (uint64_t)t->nbytes();
+    }
+};
+
+// x, form (4), form_t (4), rounding, seed, worker, step
+PyObject* call_mx_quantize(Args in)
+{
+    const auto f = in.entry<decltype(&tq_mx_quantize)>();
+    const Dense x(in, 1);
+    const Form form(in, 2, false), form_t(in, 6, false);
+    const int rounding = in.i32(10);
+    const uint64_t seed = in.u64(11);
+    const uint32_t worker = in.u32(12), step = in.u32(13);
+    if (form.codes && (form.rows != x.rows || form.cols != x.cols)) in.ok = false;
+    if (form_t.codes && (form_t.rows != x.cols || form_t.cols != x.rows)) in.ok = false;
+    return finish(in, f, x.p, x.dtype, x.rows, x.cols, x.ld, rounding, seed, worker, step, form.codes, form.scales, form_t.codes,
+                  form_t.scales);
+}
+
+// form (4), out
+PyObject* call_mx_dequantize(Args in)
+{
+    const auto f = in.entry<decltype(&tq_mx_dequantize)>();
+    const Form form(in, 1);
+    const Dense out(in, 5);
+    if (out.rows != form.rows || out.cols != form.cols) in.ok = false;
+    return finish(in, f, form.codes, form.scales, form.rows, form.cols, out.p, out.dtype, out.ld);
+}
+
+// a (4), b (4), out, workspace, add
+PyObject* call_mx_matmul(Args in)
+{
+    const auto f = in.entry<decltype(&tq_mx_matmul)>();
+    const Form a(in, 1), b(in, 5);
+    const Dense out(in, 9);
+    const Scratch ws(in, 10);
+    const float* add = nullptr;
+    uint64_t lda = 0;
+    if (in.ok && in.a[11] != Py_None) {
+        const Dense d(in, 11);
+        if (d.dtype != TQ_F32 || d.rows != out.rows || d.cols != out.cols) in.ok = false;
+        add = (const float*)d.p;
+        lda = d.ld;
+    }
+    if (a.cols != b.cols || a.rows != out.rows || b.rows != out.cols) in.ok = false;
+    return finish(in, f, a.codes, a.scales, b.codes, b.scales, out.rows, out.cols, a.cols, add, lda, out.p, out.dtype, out.ld, ws.p, ws.bytes);
+}
+
+// x, w (4), out, workspace
+PyObject* call_mx_linear(Args in)
+{
+    const auto f = in.entry<decltype(&tq_mx_linear)>();
+    const Dense x(in, 1);
+    const Form w(in, 2);
+    const Dense out(in, 6);
+    const Scratch ws(in, 7);
+    if (w.cols != x.cols || w.rows != out.cols || out.rows != x.rows) in.ok = false;
+    return finish(in, f, x.p, x.dtype, x.rows, x.ld, w.codes, w.scales, w.rows, w.cols, out.p, out.dtype, out.ld, ws.p, ws.bytes);
+}
+
+// z, ids, t and the temperature of a distillation call, whose arguments begin at 1; the temperature is argument `last`.
+struct Teacher {
+    const void* ids = nullptr;
+    const float* t = nullptr;
+    int id_bytes = 0;
+    uint64_t top = 0;
+    float temperature = 0.0f;
+
+    Teacher(Args& in, const Dense& z, Py_ssize_t last)
+    {
+        const at::Tensor *i = in.tensor(2), *p = in.tensor(3);
+        temperature = in.f32(last);
+        if (!in.ok) return;
+        id_bytes = i->scalar_type() == at::kInt ? 4 : i->scalar_type() == at::kLong ? 8 : 0;
+        if (id_bytes == 0 || p->scalar_type() != at::kFloat || i->dim() != 2 || p->dim() != 2 || i->size(0) != (int64_t)z.rows ||
+            p->size(0) != i->size(0) || p->size(1) != i->size(1)) {
+            in.ok = false;
+            return;
+        }
+        ids = i->data_ptr();
+        t = (const float*)p->data_ptr();
+        top = (uint64_t)i->size(1);
+    }
+};
+
+bool alike(const Dense& z, const Dense& dz) { return z.rows == dz.rows && z.cols == dz.cols && z.dtype == dz.dtype; }
+
+// z, ids, t, loss, stats, temperature
+PyObject* call_distill_forward(Args in)
+{
+    const auto f = in.entry<decltype(&tq_distill_forward)>();
+    const Dense z(in, 1);
+    const Teacher e(in, z, 6);
+    const long long rows = (long long)z.rows;
+    auto *loss = (float*)in.floats(4, rows, rows), *stats = (float*)in.floats(5, 2 * rows, 2 * rows);
+    return finish(in, f, z.p, z.dtype, z.rows, z.cols, z.ld, e.ids, e.id_bytes, e.t, e.top, e.temperature, loss, stats);
+}
+
+// z, ids, t, stats, grad, dz, temperature
+PyObject* call_distill_backward(Args in)
+{
+    const auto f = in.entry<decltype(&tq_distill_backward)>();
+    const Dense z(in, 1);
+    const Teacher e(in, z, 7);
+    const long long rows = (long long)z.rows;
+    auto *stats = (const float*)in.floats(4, 2 * rows, 2 * rows), *grad = (const float*)in.floats(5, rows, rows);
+    const Dense dz(in, 6);
+    if (!alike(z, dz)) in.ok = false;
+    return finish(in, f, z.p, z.dtype, z.rows, z.cols, z.ld, e.ids, e.id_bytes, e.t, e.top, e.temperature, stats, grad, dz.p, dz.ld);
+}
+
+// z, ids, t, grad, loss, dz, temperature
+PyObject* call_distill(Args in)
+{
+    const auto f = in.entry<decltype(&tq_distill)>();
+    const Dense z(in, 1);
+    const Teacher e(in, z, 7);
+    const long long rows = (long long)z.rows;
+    auto* grad = (const float*)in.floats(4, rows, rows);
+    auto* loss = (float*)in.floats(5, rows, rows);
+    const Dense dz(in, 6);
+    if (!alike(z, dz)) in.ok = false;
+    return finish(in, f, z.p, z.dtype, z.rows, z.cols, z.ld, e.ids, e.id_bytes, e.t, e.top, e.temperature, grad, loss, dz.p, dz.ld);
+}
+
 template <PyObject* (*CALL)(Args), int ARGS>
 PyObject* take(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -516,6 +699,13 @@ PyMethodDef methods[] = {
     method<call_compress_segments, 11>("compress_segments"),
     method<call_compress_segments_multi, 11>("compress_segments_multi"),
     method<call_aggregate_segments, 10>("aggregate_segments"),
+    method<call_mx_quantize, 14>("mx_quantize"),
+    method<call_mx_dequantize, 6>("mx_dequantize"),
+    method<call_mx_matmul, 12>("mx_matmul"),
+    method<call_mx_linear, 8>("mx_linear"),
+    method<call_distill_forward, 7>("distill_forward"),
+    method<call_distill_backward, 8>("distill_backward"),
+    method<call_distill, 8>("distill"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tq_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -526,6 +716,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tq_marshal", nullptr, -1, methods
 PyMODINIT_FUNC PyInit__tq_marshal()
 {
     PyObject* m = PyModule_Create(&module);
-    if (m && PyModule_AddIntConstant(m, "interface", 1) != 0) Py_CLEAR(m);
+    if (m && PyModule_AddIntConstant(m, "interface", 3) != 0) Py_CLEAR(m);
     return m;
 }

@@ -46,8 +46,8 @@ struct Element<TQ_F16> {
 template <int DTYPE>
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
-    if constexpr (DTYPE == TQ_BF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-    else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+    if constexpr (DTYPE == TQ_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
 }
 
 // The same two values back.
