@@ -36,7 +36,6 @@ __device__ __forceinline__ void store_one(const MatmulArgs& g, uint32_t row, uin
 {
     using E = Element<DTYPE>;
     if (row >= g.m || col >= g.n) return;
-    if (g.add) v += g.add[row * g.lda + col];
     static_cast<typename E::type*>(g.out)[row * g.ldo + col] = E::store(v);
 }
 
@@ -144,6 +143,18 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
 
     const uint32_t ra = wm * S::kFragsM * 32 + r, rb = BM + wn * S::kFragsN * 32 + r;
     f32x16 acc[S::kFragsM][S::kFragsN] = {};
+    if (g.add && part == 0) {                                      // requested first, so that it is there when the sums begin
+#pragma unroll
+        for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t row = row0 + (wm * S::kFragsM + i) * 32 + (e / 4) * 8 + half * 4 + e % 4;
+                    const uint32_t col = col0 + (wn * S::kFragsN + j) * 32 + r;
+                    acc[i][j][e] = g.add[min(row, g.m - 1) * g.lda + min(col, g.n - 1)];
+                }
+    }
 #pragma unroll
     for (uint32_t t = 0; t < STAGES - 1; ++t)
         if (t < trips) fetch(t, t);
@@ -328,6 +339,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArg
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) v += sums[(w * 32 + row) * 33 + col];
+        if (g.add && col0 + col < g.n) v += g.add[row * g.lda + col0 + col];
         store_one<DTYPE>(g, row, col0 + col, v);
     }
 }
