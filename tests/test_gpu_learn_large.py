@@ -1,0 +1,134 @@
+"""4-bit matrices and distillation at sizes that choose the large tiles, and where offsets pass 32 bits."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import learn_common as LC
+from paper_2402_01798_amd import binding as B
+from test_gpu_mx import random_form, scratch
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def on_device(values):
+    return torch.from_numpy(values).cuda()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(2049, 2047, 129), (2100, 2000, 1000), (3713, 3701, 300), (3900, 3800, 1), (4096, 4096, 640), (1300, 7000, 2050)])
+def test_product_in_large_tiles(m, n, k, out):
+    (a, va), (b, vb) = random_form(m, k, 1, 118, 122), random_form(n, k, 2, 118, 122)
+    va, vb = on_device(va), on_device(vb)
+    ref, size = va @ vb.t().contiguous(), va.abs() @ vb.abs().t().contiguous()
+    ws = scratch(B.mx_matmul_workspace_bytes(m, n, k))
+    add = torch.randn(m, n + 4, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    wide = torch.full((m, n + 3), 7.0, dtype=LC.TYPES[out], device="cuda")
+    for o, extra in ((torch.empty(m, n, dtype=LC.TYPES[out], device="cuda"), None), (wide[:, :n], add[:, 1:n + 1])):
+        B.tq_mx_matmul(a, b, o, ws, add=extra)
+        want = ref if extra is None else ref + extra.double()
+        bound = (k + 1) * 2.0 ** -23 * (size if extra is None else size + extra.double().abs()) + 1.001 * LC.HALF_ULP[out] * want.abs() \
+            + (2.0 ** -25 if out == "f16" else 0.0)
+        assert ((o.double() - want).abs() <= bound).all()
+    assert (wide[:, n:] == 7).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(2100, 2000, 700), (3800, 3800, 400)])
+def test_blocks_without_a_value_in_large_tiles(m, n, k):
+    (a, _), (b, _) = random_form(m, k, 3), random_form(n, k, 4)
+    a.scales[1, 1500, 2] = 255
+    b.scales[2, 7, 0] = 255
+    out = torch.empty(m, n, device="cuda")
+    B.tq_mx_matmul(a, b, out, scratch(B.mx_matmul_workspace_bytes(m, n, k)))
+    want = torch.zeros(m, n, dtype=torch.bool, device="cuda")
+    want[1500], want[:, 7] = True, True
+    assert torch.equal(torch.isnan(out), want)
+
+
+def test_cast_past_32_bits():
+    """4.6e9 elements: the last rows of both forms, and of the way back."""
+    rows, cols = 70_000, 65_664                             # cols: 513 groups of 128
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x[-40:] = torch.randn(40, cols, generator=g, device="cuda").bfloat16()
+    x[:, -40:] = torch.randn(rows, 40, generator=g, device="cuda").bfloat16()
+    f, ft = B.alloc_mx(rows, cols), B.alloc_mx(cols, rows)
+    B.tq_mx_quantize(x, f, ft)
+    last = x[-33:].double().cpu().numpy()
+    got = f.codes[-33:, -64:].cpu().numpy()
+    want, want_scales = LC.mx_form(last[:, -128:])
+    assert (got == want).all() and (f.scales[-1:, -33:].cpu().numpy() == want_scales).all()
+    first = rows // 128 * 128                               # the last, short group of the columns
+    want, want_scales = LC.mx_form(x[first:, -33:].double().cpu().numpy().T)
+    assert (ft.codes[-33:, -64:].cpu().numpy() == want).all() and (ft.scales[-1:, -33:].cpu().numpy() == want_scales).all()
+    rows_only = B.alloc_mx(rows, cols)
+    B.tq_mx_quantize(x, rows_only)
+    assert torch.equal(rows_only.codes[-33:], f.codes[-33:]) and torch.equal(rows_only.scales[:, -33:], f.scales[:, -33:])
+    del rows_only, ft
+    B.tq_mx_dequantize(f, x)
+    assert np.array_equal(x[-33:, -128:].double().cpu().numpy(), LC.mx_values(*LC.mx_form(last[:, -128:]), 128))
+
+
+def test_product_past_32_bits():
+    """An output of 4.6e9 elements, and operands with more than 2^32 codes."""
+    (a, va), (b, vb) = random_form(70_000, 32, 5), random_form(66_000, 32, 6)
+    out = torch.empty(70_000, 66_000, dtype=torch.bfloat16, device="cuda")
+    B.tq_mx_matmul(a, b, out, scratch(B.mx_matmul_workspace_bytes(70_000, 66_000, 32)))
+    for rows, cols in ((slice(0, 50), slice(0, 50)), (slice(-300, None), slice(-300, None)), (slice(65_500, 65_600), slice(-50, None))):
+        ref = va[rows] @ vb[cols].T
+        assert (np.abs(out[rows, cols].double().cpu().numpy() - ref) <= LC.product_bound(va[rows], vb[cols], 32, "bf16", ref)).all()
+    del out
+    rows, k = 9_000, 600_064                                # 5.4e9 codes, 2.7e9 bytes
+    a = B.alloc_mx(rows, k)
+    a.codes.zero_()
+    a.scales.fill_(127)
+    a.codes[-1, -1] = 0x22                                  # 1 and 1
+    a.codes[-2, 0] = 0x04                                   # 2 and 0
+    b = B.alloc_mx(3, k)
+    b.codes.fill_(0x22)
+    b.scales.fill_(128)                                     # every element 2
+    out = torch.empty(rows, 3, device="cuda")
+    B.tq_mx_matmul(a, b, out, scratch(B.mx_matmul_workspace_bytes(rows, 3, k)))
+    assert (out[:-2] == 0).all() and (out[-1] == 4).all() and (out[-2] == 4).all()
+
+
+def test_distillation_past_32_bits():
+    """5.2e9 logits: the last rows."""
+    rows, vocab, top = 40_000, 131_001, 16
+    z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    z[-3:] = (3 * torch.randn(3, vocab, generator=g, device="cuda")).bfloat16()
+    ids = torch.randint(0, vocab, (rows, top), generator=g, device="cuda")
+    ids[-1, 0] = vocab - 1
+    t = torch.randn(rows, top, generator=g, device="cuda")
+    grad = torch.ones(rows, device="cuda")
+    last = [v[-3:].contiguous() for v in (z, ids, t, grad)]
+    want_loss, want_dz = torch.empty(3, device="cuda"), torch.empty_like(last[0])
+    B.tq_distill(last[0], last[1], last[2], last[3], want_loss, want_dz)
+    loss, stats = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    B.tq_distill_forward(z, ids, t, loss, stats)
+    kept = z[-3:].clone()
+    B.tq_distill_backward(z, ids, t, stats, grad, z)
+    assert torch.allclose(loss[-3:], want_loss, rtol=1e-5) and torch.allclose(z[-3:].float(), want_dz.float(), rtol=2 ** -7, atol=1e-12)
+    z[-3:] = kept
+    B.tq_distill(z[-3:], ids[-3:], t[-3:], grad[-3:], loss[-3:], z[-3:])
+    assert torch.allclose(z[-3:].float(), want_dz.float(), rtol=2 ** -7, atol=1e-12)
+    # rows of zeros: q = 1 / vocab, less the teacher's share
+    share = torch.softmax(t[5].double(), 0)
+    assert abs(float(z[5].double().sum())) < 0.02 and abs(float(z[5, int(ids[5, 0])]) - (1 / vocab - float(share[ids[5] == ids[5, 0]].sum()))) < 2 ** -8
+
+
+def test_with_a_folded_grid():
+    """Launches beyond one grid dimension are folded; a child process lowers the fold point and runs the parity tests again."""
+    from paper_2402_01798_amd import build
+    assert os.path.exists(build.FOLD_TEST_LIB), "build it first: python -m paper_2402_01798_amd.build"
+    env = dict(os.environ, TQ_TEST_MAX_GRID_X="40", TQ_LIBRARY_PATH=build.FOLD_TEST_LIB)
+    cmd = [sys.executable, "-m", "pytest", "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider", "tests/test_gpu_mx.py::test_cast",
+           "tests/test_gpu_mx.py::test_product", "tests/test_gpu_mx.py::test_linear", "tests/test_gpu_learn_large.py::test_product_in_large_tiles",
+           "tests/test_gpu_learn_calls.py::test_rows_in_pieces_write_what_one_workgroup_writes"]
+    r = subprocess.run(cmd, cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
