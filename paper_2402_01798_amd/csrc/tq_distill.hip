@@ -17,9 +17,11 @@ struct DistillArgs {
     void* dz;
     uint64_t ldz, lddz;
     uint32_t rows, vocab, top, pieces;                             // workgroups of a row (kBackward)
-    int wide_ids, past_caches;
+    int wide_ids;
     float tau, inv_tau;
 };
+
+constexpr uint32_t kSeenBits = 32768;                              // a set of ids, by their low bits
 
 enum { kForward = 0, kBackward = 1, kBoth = 2 };
 
@@ -72,7 +74,7 @@ struct Row {
     }
     // Vector k of the gradient, which begins at p and lies as the row does (WHOLE) or not.
     template <bool NEAR, bool WHOLE>
-    __device__ __forceinline__ void store(T* p, uint32_t k, const float (&v)[kIn], bool past_caches) const
+    __device__ __forceinline__ void store(T* p, uint32_t k, const float (&v)[kIn]) const
     {
         T* q = NEAR ? p + head + k * kIn : p + head + (uint64_t)k * kIn;
         u32x4 w;
@@ -84,21 +86,36 @@ struct Row {
             for (uint32_t e = 0; e < kIn / 2; ++e) w[e] = pack2<DTYPE>(v[2 * e], v[2 * e + 1]);
         }
         if constexpr (!WHOLE) __builtin_memcpy(q, &w, 16);         // stored at any address
-        else if (past_caches) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(q));
         else *reinterpret_cast<u32x4*>(q) = w;
     }
 };
 
-// Sums and maxima of two values over the workgroup, in a fixed order.  `part` holds two values per wavefront and is used once.
+template <int CTRL>
+__device__ __forceinline__ float dpp_float(float v) { return __uint_as_float(dpp_move<CTRL>(__float_as_uint(v))); }
+
+// The sum or the maximum of a wavefront's values, the same bits in every lane, by moves inside the vector unit (through LDS each of
+// the six steps takes some hundred clocks, and a short row has six such reductions).
+template <bool MAX>
+__device__ __forceinline__ float wave_reduce(float v)
+{
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+    v = op(v, dpp_float<0xB1>(v));          // lanes 1 0 3 2
+    v = op(v, dpp_float<0x4E>(v));          // lanes 2 3 0 1
+    v = op(v, dpp_float<0x141>(v));         // mirrored within 8
+    v = op(v, dpp_float<0x140>(v));         // within 16
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Of two values over the workgroup, in a fixed order.  `part` holds two values per wavefront and is used once.
 template <int WAVES, bool MAX>
 __device__ __forceinline__ void group_reduce(float& x, float& y, float (*part)[2])
 {
     auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        x = op(x, __shfl_xor(x, d));
-        y = op(y, __shfl_xor(y, d));
-    }
+    x = wave_reduce<MAX>(x);
+    y = wave_reduce<MAX>(y);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) {
             part[threadIdx.x >> 6][0] = x;
@@ -155,11 +172,11 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     constexpr int WAVES = THREADS / 64;
     constexpr uint32_t IN = R::kIn;
     __shared__ float parts[3][WAVES][2];
-    extern __shared__ char entries[];                              // the teacher's: id, logit and then probability, z, whether
-    int* id = reinterpret_cast<int*>(entries);                     // an earlier one has the id
+    extern __shared__ char entries[];                              // the teacher's: id, logit and then probability, z
+    int* id = reinterpret_cast<int*>(entries);
     float* t = reinterpret_cast<float*>(id + a.top);
     float* at_id = t + a.top;
-    int* again = reinterpret_cast<int*>(at_id + a.top);
+    __shared__ uint32_t seen[MODE == kForward ? 1 : kSeenBits / 32];
     const uint32_t block = linear_block(), tid = threadIdx.x, row = MODE == kBackward ? block / a.pieces : block;
     if (row >= a.rows) return;
     const T* z = static_cast<const T*>(a.z) + (uint64_t)row * a.ldz;
@@ -179,6 +196,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     const int64_t loose = piece == 0 ? lies.loose(tid) : -1;
     const float z_loose = loose >= 0 ? E::load(z[loose]) : -INFINITY;
 
+    if constexpr (MODE != kForward) {
+        for (uint32_t i = tid; i < kSeenBits / 32; i += THREADS) seen[i] = 0;
+    }
     float t_peak = -INFINITY;
     bool bad = false, twice = false;
     for (uint32_t i = tid; i < a.top; i += THREADS) {
@@ -188,7 +208,6 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         const bool there = w >= 0 && w < (int64_t)a.vocab && v != -INFINITY;
         id[i] = there ? (int)w : -1;
         t[i] = v;
-        again[i] = 0;
         // (another piece's elements may be gradients by now, where dz is z)
         at_id[i] = there && (MODE != kBackward || lies.within((uint32_t)w, k_first, k_end)) ? E::load(z[w]) : 0.0f;
         if (there) {
@@ -196,18 +215,11 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
             bad |= !(v < INFINITY);
         }
     }
-    if constexpr (MODE != kForward) {                              // each pair of entries once, spread over the threads
+    if constexpr (MODE != kForward) {                              // whether an id occurs twice: those whose bit was set look closer
         __syncthreads();
-        const uint32_t slices = a.top < THREADS ? THREADS / a.top : 1, slice = tid / a.top, step = a.top < THREADS ? a.top : THREADS;
-        if (slice < slices || a.top >= THREADS)
-            for (uint32_t i = a.top < THREADS ? tid - slice * a.top : tid; i < a.top; i += step) {
-                const int mine = id[i];
-                for (uint32_t j = a.top < THREADS ? slice : 0; mine >= 0 && j < i; j += slices)
-                    if (id[j] == mine) {
-                        again[i] = 1;
-                        twice = true;
-                    }
-            }
+        for (uint32_t i = tid; i < a.top; i += THREADS)
+            if (id[i] >= 0 && (atomicOr(&seen[(id[i] & (kSeenBits - 1)) / 32], 1u << (id[i] & 31)) >> (id[i] & 31) & 1u))
+                for (uint32_t j = 0; j < a.top; ++j) twice |= j != i && id[j] == id[i];
     }
 
     float top = z_loose, log_total = 0.0f;                         // the row's largest logit, ln sum exp((z - top) / tau)
@@ -289,7 +301,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
             R::unpack(w, v);
 #pragma unroll
             for (uint32_t j = 0; j < IN; ++j) v[j] = scale * __builtin_amdgcn_exp2f((v[j] - from) * c);
-            lies.template store<(VECTORS > 0), WHOLE>(dz, k, v, a.past_caches);
+            lies.template store<(VECTORS > 0), WHOLE>(dz, k, v);
         };
         if constexpr (VECTORS > 0) {
             if (!counts) {
@@ -310,11 +322,17 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         if (!counts) return;
         __syncthreads();                                           // the elements that the teacher names are written once more
         for (uint32_t i = tid; i < a.top; i += THREADS)
-            if (id[i] >= 0 && !again[i] && lies.within(id[i], k_first, k_end)) {
+            if (id[i] >= 0 && lies.within(id[i], k_first, k_end)) {
                 float p = t[i];
-                if (count != 0.0f)
-                    for (uint32_t j = i + 1; j < a.top; ++j)
-                        if (id[j] == id[i]) p += t[j];
+                if (count != 0.0f) {                               // an id's first entry takes the probabilities of all
+                    bool first = true;
+                    for (uint32_t j = 0; j < a.top; ++j)
+                        if (j != i && id[j] == id[i]) {
+                            first &= j > i;
+                            p += t[j];
+                        }
+                    if (!first) continue;
+                }
                 dz[id[i]] = E::store(scale * power(at_id[i]) - g * p);
             }
     }
@@ -325,7 +343,7 @@ hipError_t launch(const DistillArgs& a, hipStream_t st)
 {
     dim3 grid;
     if (!fold_grid((uint64_t)a.rows * a.pieces, THREADS, 1, grid)) return hipErrorInvalidValue;
-    const size_t entries = 16 * (size_t)a.top;
+    const size_t entries = 12 * (size_t)a.top;
     if constexpr (MODE != kForward) {
         const uint64_t size = DTYPE == TQ_F32 ? 4 : 2;
         if (((reinterpret_cast<uintptr_t>(a.dz) - reinterpret_cast<uintptr_t>(a.z)) | (a.lddz - a.ldz) * size) & 15u) {
@@ -396,7 +414,6 @@ hipError_t tq_launch_distill(const void* z, int dtype, uint64_t rows, uint64_t v
     a.wide_ids = ids_bytes == 8;
     a.tau = temperature;
     a.inv_tau = 1.0f / temperature;
-    a.past_caches = dz && output_past_caches(rows * vocab * (dtype == TQ_F32 ? 4 : 2));
     if (!dz) return launch<kForward>(a, dtype, st);
     return stats_in ? launch<kBackward>(a, dtype, st) : launch<kBoth>(a, dtype, st);
 }

@@ -201,6 +201,22 @@ __device__ __forceinline__ uint32_t stride4_max(uint32_t v)
     return max(v, dpp_move<0x124>(v));     // by 4
 }
 
+// The largest of 16 neighbouring lanes, in each of them.
+__device__ __forceinline__ uint32_t row16_max(uint32_t v)
+{
+    v = quad_max(v);
+    v = max(v, dpp_move<0x141>(v));        // mirrored within 8
+    return max(v, dpp_move<0x140>(v));     // within 16
+}
+// The largest of the lanes 16 apart (l, l + 16, l + 32, l + 48), in each of them.
+__device__ __forceinline__ uint32_t stride16_max(uint32_t v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(b[0], b[1]);
+}
+
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 }  // namespace tq
