@@ -72,7 +72,7 @@ struct Tile {
     static constexpr int kRing = STAGES * kStage;
     static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
     static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
-    static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % kRows == 0, "every wavefront requests the same");
+    static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % (kRows * kWaves) == 0, "every wavefront requests the same");
 };
 
 // Waits until the requests of all but the newest `newer` stages (at most N) are there.
