@@ -86,29 +86,24 @@ __global__ __launch_bounds__(256) void mx_cast_tile_kernel(CastArgs a)
         for (int i = 0; i < 8; ++i)
             if (row0 + i >= a.rows) held[i].clear();
     }
-    uint32_t byte_t[8] = {};
+    uint32_t byte_t[8], most[Eight<DTYPE>::kWords] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float v[8];
-        held[i].unpack(v);
+    for (int i = 0; i < 8; ++i) held[i].largest_of_columns(most);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) byte_t[j] = max(byte_t[j], magnitude_bits(v[j]));
+    for (int j = 0; j < Eight<DTYPE>::kWords; ++j) {             // of four neighbouring lanes
+        most[j] = Eight<DTYPE>::larger(most[j], dpp_move<0xB1>(most[j]));
+        most[j] = Eight<DTYPE>::larger(most[j], dpp_move<0x4E>(most[j]));
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        byte_t[j] = mx_scale_byte<STOCHASTIC>(quad_max(byte_t[j]));
+        byte_t[j] = mx_scale_byte<STOCHASTIC>(Eight<DTYPE>::bits(most[j * Eight<DTYPE>::kWords / 8], j & 1));
         if (r == 0) scale_t[c * 8 + j][wave] = (uint8_t)byte_t[j];
     }
     uint32_t w_t[8] = {};
     auto along_the_row = [&](int i, const float (&v)[8]) {       // and, rounded stochastically, down the columns
         const uint32_t row = row0 + i;
         uint32_t byte = 0, w = 0;
-        if constexpr (ROWS) {
-            uint32_t largest = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
-            byte = mx_scale_byte<STOCHASTIC>(stride4_max(largest));
-        }
+        if constexpr (ROWS) byte = mx_scale_byte<STOCHASTIC>(stride4_max(held[i].largest()));
         if constexpr (STOCHASTIC) {
             uint32_t draws[4], o = oct;
             asm volatile("" : "+v"(o));                          // not all rows' draws first: they would wait in registers

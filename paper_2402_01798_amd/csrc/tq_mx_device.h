@@ -13,6 +13,7 @@ constexpr uint32_t kMxGroup = 128;         // elements of a row that are kept to
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -106,6 +107,34 @@ struct Eight {
         w[0] = u32x4{0, 0, 0, 0};
         if constexpr (DTYPE == TQ_F32) w[1] = w[0];
     }
+    // Largest magnitudes, of 16-bit types two at a time: as integers they order like their values.  `most` is one of the columns' words.
+    static constexpr int kWords = DTYPE == TQ_F32 ? 8 : 4;
+    __device__ __forceinline__ void largest_of_columns(uint32_t (&most)[kWords]) const
+    {
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) most[j] = larger(most[j], word(j));
+    }
+    __device__ __forceinline__ uint32_t largest() const                 // of the eight, as fp32 bits
+    {
+        uint32_t m = word(0);
+#pragma unroll
+        for (int j = 1; j < kWords; ++j) m = larger(m, word(j));
+        return DTYPE == TQ_F32 ? m : max(bits(m, 0), bits(m, 1));
+    }
+    static __device__ __forceinline__ uint32_t bits(uint32_t m, int half)      // one half of a word of magnitudes as fp32 bits
+    {
+        if constexpr (DTYPE == TQ_F32) return m;
+        else return __float_as_uint(Element<DTYPE>::load((uint16_t)(half ? m >> 16 : m)));
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        if constexpr (DTYPE == TQ_F32) return max(a, b);
+        else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    __device__ __forceinline__ uint32_t word(int j) const
+    {
+        return DTYPE == TQ_F32 ? w[j / 4][j % 4] & 0x7FFFFFFFu : w[0][j % 4] & 0x7FFF7FFFu;
+    }
     __device__ __forceinline__ void unpack(float (&v)[8])
     {
         asm volatile("" : "+v"(w[0]));
@@ -168,7 +197,9 @@ __device__ __forceinline__ uint32_t mx_push(uint32_t w, float v, uint32_t byte, 
 {
     const uint32_t bits = __float_as_uint(__builtin_amdgcn_ldexpf(fabsf(v), 1 - (int)byte));
     const uint32_t x = (bits << 6) + draw;                              // the magnitude's code in bits 28..30
-    return __builtin_amdgcn_alignbit(w, (x & 0x7FFFFFFFu) | (__float_as_uint(v) & 0x80000000u), 28);
+    uint32_t code;                                                      // and v's sign above it, in one instruction
+    asm("v_bfi_b32 %0, %1, %2, %3" : "=v"(code) : "s"(0x7FFFFFFFu), "v"(x), "v"(v));
+    return __builtin_amdgcn_alignbit(w, code, 28);
 }
 
 // 8 codes in a word, the first element's lowest.
