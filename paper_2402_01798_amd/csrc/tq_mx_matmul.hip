@@ -6,6 +6,10 @@
 namespace tq {
 namespace {
 
+constexpr uint64_t kUnits = 256;                                   // compute units
+constexpr uint64_t kSplitGroups = 16;                              // of a workgroup at least, where k is split over several
+constexpr uint64_t kSplitSaves = 40;
+
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -18,7 +22,9 @@ struct MatmulArgs {
     uint64_t ldx, lda, ldo;
     uint32_t m, n, k, groups;
     uint32_t tiles_x;
-    uint64_t tiles;
+    uint64_t tiles;                // of the output, times `splits`
+    float* partial;                // [splits][m][n]: sums over parts of k that different workgroups take
+    uint32_t splits;
 };
 
 // 32 x 32 outputs += 64 elements of k.  Lane l holds row l % 32 and block l / 32 of both operands: 32 codes and their scale, a byte
@@ -44,11 +50,14 @@ typedef __attribute__((address_space(3))) void lds_bytes;
 
 // Which tile this workgroup takes.  Workgroups go to the 8 dies in turn; each die takes a run of tiles, which goes down 4 tiles and
 // then on to the next column, so that the tiles at work on a die at a time share their rows in its cache.
-__device__ __forceinline__ bool find_tile(const MatmulArgs& g, uint32_t& ty, uint32_t& tx)
+__device__ __forceinline__ bool find_tile(const MatmulArgs& g, uint32_t& ty, uint32_t& tx, uint32_t& split)
 {
-    const uint32_t block = linear_block(), per = (uint32_t)(g.tiles + 7) / 8, tile = (block & 7) * per + (block >> 3);
+    const uint32_t block = linear_block(), per = (uint32_t)(g.tiles + 7) / 8;
+    uint32_t tile = (block & 7) * per + (block >> 3);
     if (block >= 8 * per || tile >= g.tiles) return false;
-    const uint32_t tiles_y = (uint32_t)(g.tiles / g.tiles_x);
+    const uint32_t of_a_split = (uint32_t)g.tiles / g.splits, tiles_y = of_a_split / g.tiles_x;
+    split = tile / of_a_split;
+    tile -= split * of_a_split;
     const uint32_t band = tile / (4 * g.tiles_x), rows = min(4u, tiles_y - band * 4), in = tile - band * 4 * g.tiles_x;
     ty = band * 4 + in % rows;
     tx = in / rows;
@@ -90,8 +99,8 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
 {
     using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
     extern __shared__ char lds[];
-    uint32_t ty, tx;
-    if (!find_tile(g, ty, tx)) return;
+    uint32_t ty, tx, split;
+    if (!find_tile(g, ty, tx, split)) return;
     const uint32_t lane = threadIdx.x & 63, wave_in_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t part = wave_in_all / S::kWaves, wave = wave_in_all % S::kWaves;
     const uint32_t r = lane & 31, half = lane >> 5, wm = wave / WN, wn = wave % WN;
@@ -117,9 +126,11 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
         const uint32_t row = c % ((BM + BN) / 64) * 64 + lane;
         scale_row[i] = row < BM ? min(row0 + row, g.m - 1) : min(col0 + row - BM, g.n - 1);
     }
-    // this part of k, in trips of GROUPS groups; `most` is the longest part's
-    const uint32_t all = (g.groups + GROUPS - 1) / GROUPS, most = (all + KS - 1) / KS, first_trip = part * most;
-    const uint32_t trips = KS == 1 ? all : first_trip < all ? min(most, all - first_trip) : 0;
+    // this part of k, in trips of GROUPS groups, up to `end`; `most` is the longest part's
+    const uint32_t all = (g.groups + GROUPS - 1) / GROUPS, of_a_split = KS == 1 ? all : (all + g.splits - 1) / g.splits;
+    const uint32_t begin = KS == 1 ? 0 : split * of_a_split, end = min(begin + of_a_split, all);
+    const uint32_t most = (of_a_split + KS - 1) / KS, first_trip = begin + part * most;
+    const uint32_t trips = KS == 1 ? all : first_trip < end ? min(most, end - first_trip) : 0;
     char* ring = lds + part * S::kRing;
     auto fetch = [&](uint32_t t, uint32_t stage) {
         char* base = ring + stage * S::kStage;
@@ -143,7 +154,7 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
 
     const uint32_t ra = wm * S::kFragsM * 32 + r, rb = BM + wn * S::kFragsN * 32 + r;
     f32x16 acc[S::kFragsM][S::kFragsN] = {};
-    if (g.add && part == 0) {                                      // requested first, so that it is there when the sums begin
+    if (g.add && part == 0 && split == 0) {                                      // requested first, so that it is there when the sums begin
 #pragma unroll
         for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
@@ -212,7 +223,8 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
             float v = 0.0f;
 #pragma unroll
             for (int q = 0; q < KS; ++q) v += sums[(q * BM + row) * (BN + 1) + col];
-            store_one<DTYPE>(g, row0 + row, col0 + col, v);
+            if (g.splits == 1) store_one<DTYPE>(g, row0 + row, col0 + col, v);
+            else if (row0 + row < g.m && col0 + col < g.n) g.partial[((uint64_t)split * g.m + row0 + row) * g.n + col0 + col] = v;
         }
         return;
     }
@@ -344,12 +356,24 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArg
     }
 }
 
+// The splits' sums, joined in their order.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void mx_join_kernel(MatmulArgs g)
+{
+    const uint64_t at = (uint64_t)linear_block() * 256 + threadIdx.x, size = (uint64_t)g.m * g.n;
+    if (at >= size) return;
+    float v = g.partial[at];
+#pragma unroll 8
+    for (uint32_t s = 1; s < g.splits; ++s) v += g.partial[s * size + at];
+    store_one<DTYPE>(g, (uint32_t)(at / g.n), (uint32_t)(at % g.n), v);
+}
+
 template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
 hipError_t launch_tile(MatmulArgs& g, hipStream_t st)
 {
     using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
     g.tiles_x = (g.n + BN - 1) / BN;
-    g.tiles = (uint64_t)g.tiles_x * ((g.m + BM - 1) / BM);
+    g.tiles = (uint64_t)g.tiles_x * ((g.m + BM - 1) / BM) * g.splits;
     dim3 grid;
     if (!fold_grid((g.tiles + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
     mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES><<<grid, S::kThreads, S::kBytes, st>>>(g);
@@ -381,23 +405,58 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 //   128 x 8192 x 8192   54.8   25.8   18.0   12.7
 //   784 x 1000 x 64      8.1    4.8    3.9    4.6              nothing to part
 //   1 x 8192 x 8192     57.5   28.1   19.9    9.7    7.4
+// Few tiles and a long k: k is split over workgroups too, where at least 40 groups (5 steps of a workgroup, the second launch's
+// price) are saved.  Not split / split, us: 64 x 64 x 8192 9.8 / 7.8, x 32768 28 / 9.5, x 131072 119 / 12, 256 x 256 x 32768 29 / 12,
+// 700 x 700 x 32768 35 / 26; with fewer saved it loses (500 x 500 x 4096 7.3 / 8.6).
+enum Shape { kFew, k256, k128, k64, k64InParts };
+
+uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side) { return (m + side - 1) / side * ((n + side - 1) / side); }
+
+Shape shape(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (m <= kFewRowsInForm && few_bytes(m, groups) <= kFewBytes) return kFew;
+    const uint64_t of_256 = tiles_of(m, n, 256), of_128 = tiles_of(m, n, 128), of_64 = tiles_of(m, n, 64);
+    // A round of tiles of 256, one on each compute unit, takes as long as 820 tiles of 128.
+    if ((of_256 + kUnits - 1) / kUnits * 820 <= of_128) return k256;
+    if (of_128 >= kUnits) return k128;
+    return of_64 > kUnits || groups < 4 ? k64 : k64InParts;
+}
+
+uint32_t splits(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (shape(m, n, groups) != k64InParts) return 1;
+    const uint64_t most = kUnits / tiles_of(m, n, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
+    return s > 1 && groups - groups / s >= kSplitSaves ? (uint32_t)s : 1;
+}
+
 template <int DTYPE>
 hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
 {
-    if (g.m <= kFewRowsInForm && few_bytes(g.m, g.groups) <= kFewBytes) return launch_few<DTYPE, -1>(g, st);
-    auto tiles = [&](uint64_t side) { return (g.m + side - 1) / side * ((g.n + side - 1) / side); };
-    const uint64_t of_256 = tiles(256), of_128 = tiles(128), of_64 = tiles(64), units = 256;
-    // A round of tiles of 256, one on each compute unit, takes as long as 820 tiles of 128.
-    if ((of_256 + units - 1) / units * 820 <= of_128) return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
-    if (of_128 >= units) return launch_tile<DTYPE, 128, 128, 2, 4, 1, 1, 3>(g, st);
-    if (of_64 > units || g.groups < 4) return launch_tile<DTYPE, 64, 64, 2, 2, 1, 1, 3>(g, st);
-    return launch_tile<DTYPE, 64, 64, 2, 2, 4, 2, 2>(g, st);
+    g.splits = 1;
+    switch (shape(g.m, g.n, g.groups)) {
+        case kFew: return launch_few<DTYPE, -1>(g, st);
+        case k256: return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
+        case k128: return launch_tile<DTYPE, 128, 128, 2, 4, 1, 1, 3>(g, st);
+        case k64: return launch_tile<DTYPE, 64, 64, 2, 2, 1, 1, 3>(g, st);
+        case k64InParts: break;
+    }
+    g.splits = splits(g.m, g.n, g.groups);
+    const hipError_t e = launch_tile<DTYPE, 64, 64, 2, 2, 4, 2, 2>(g, st);
+    if (e != hipSuccess || g.splits == 1) return e;
+    dim3 grid;
+    if (!fold_grid(((uint64_t)g.m * g.n + 255) / 256, 256, 1, grid)) return hipErrorInvalidValue;
+    mx_join_kernel<DTYPE><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
 }  // namespace
 }  // namespace tq
 
-uint64_t tq_mx_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k) { return 0; }
+uint64_t tq_mx_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint32_t s = tq::splits(m, n, (k + tq::kMxGroup - 1) / tq::kMxGroup);
+    return s == 1 ? 0 : s * m * n * sizeof(float);
+}
 
 hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, const void* sb, uint64_t m, uint64_t n, uint64_t k,
                                const float* add, uint64_t lda, void* out, int dtype, uint64_t ldo, void* workspace, hipStream_t st)
@@ -416,6 +475,7 @@ hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, con
     g.n = (uint32_t)n;
     g.k = (uint32_t)k;
     g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
+    g.partial = static_cast<float*>(workspace);
     if (dtype == TQ_F32) return launch_matmul<TQ_F32>(g, st);
     return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
 }

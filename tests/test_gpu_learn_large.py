@@ -49,6 +49,44 @@ def test_blocks_without_a_value_in_large_tiles(m, n, k):
     assert torch.equal(torch.isnan(out), want)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(64, 64, 8192), (70, 130, 8100), (17, 33, 20001), (300, 500, 16384), (1, 40, 200_000), (129, 65, 65_665)])
+def test_product_over_a_long_axis(m, n, k, out):
+    """k in parts over workgroups, joined in a second launch, whatever the workspace held."""
+    (a, va), (b, vb) = random_form(m, k, 7, 118, 122), random_form(n, k, 8, 118, 122)
+    nbytes = B.mx_matmul_workspace_bytes(m, n, k)
+    assert nbytes > 0 and nbytes % (4 * m * n) == 0
+    add = torch.randn(m, n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    for extra in (None, add):
+        got = []
+        for fill in (0x00, 0xFF):                           # 0xFF: NaN
+            ws = torch.full((nbytes,), fill, dtype=torch.uint8, device="cuda")
+            got.append(B.tq_mx_matmul(a, b, torch.full((m, n + 2), 5.0, dtype=LC.TYPES[out], device="cuda")[:, 1:n + 1], ws, extra))
+        assert torch.equal(got[0], got[1])
+        want = va @ vb.T + (0 if extra is None else extra.double().cpu().numpy())
+        bound = LC.product_bound(va, vb, k + 1, out, want) + (0 if extra is None else (k + 1) * 2.0 ** -23 * np.abs(extra.cpu().numpy()))
+        assert (np.abs(got[0].double().cpu().numpy() - want) <= bound).all()
+    with pytest.raises(B.TqError) as e:
+        B.tq_mx_matmul(a, b, torch.empty(m, n, device="cuda"), torch.empty(nbytes - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == B.EINVAL
+
+
+@pytest.mark.parametrize("m,k,in_one", [(1, 177_280, True), (1, 177_281, False), (16, 11_000, True), (32, 5_000, True), (32, 6_000, False),
+                                        (33, 100, False)])
+def test_linear_on_both_sides_of_what_lds_holds(m, k, in_one):
+    n = 70
+    w, vw = random_form(n, k, 9, 118, 122)
+    nbytes = B.mx_linear_workspace_bytes(m, n, k)
+    assert (nbytes == 0) == in_one
+    x = torch.randn(m, k, generator=torch.Generator(device="cuda").manual_seed(m), device="cuda").bfloat16()
+    out = B.tq_mx_linear(x, w, torch.empty(m, n, device="cuda"), scratch(nbytes))
+    f = B.alloc_mx(m, k)
+    B.tq_mx_quantize(x, f)
+    vx = LC.mx_values(f.codes.cpu().numpy(), f.scales.cpu().numpy(), k)
+    ref = vx @ vw.T
+    assert (np.abs(out.double().cpu().numpy() - ref) <= LC.product_bound(vx, vw, k, "f32", ref)).all()
+
+
 def test_cast_past_32_bits():
     """4.6e9 elements: the last rows of both forms, and of the way back."""
     rows, cols = 70_000, 65_664                             # cols: 513 groups of 128
