@@ -170,3 +170,20 @@ def test_with_a_folded_grid():
            "tests/test_gpu_learn_calls.py::test_rows_in_pieces_write_what_one_workgroup_writes"]
     r = subprocess.run(cmd, cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m,n,k", [(2, 40, 128), (40, 40, 128), (200, 140, 900), (64, 64, 8192), (2100, 2000, 128)])
+@pytest.mark.parametrize("sa,sb", [(254, 254), (254, 127), (254, 0), (200, 200), (0, 254), (60, 60), (10, 100), (0, 0)])
+def test_scales_at_the_ends_of_their_range(m, n, k, sa, sb):
+    """A product that passes the range ends at infinity, one below it at its subnormal or zero; codes that meet zeros stay zero."""
+    a, b = B.alloc_mx(m, k), B.alloc_mx(n, k)
+    for f, scale in ((a, sa), (b, sb)):
+        f.codes.zero_()
+        f.scales.fill_(scale)
+    a.codes[:, 0], b.codes[:, 1] = 0x07, 0x70  # 6 in columns 0 and 3: they meet zeros
+    a.codes[1, 8] = b.codes[1, 8] = 0x02  # 1 in column 16 of one row of each: they meet
+    out = torch.empty(m, n, device="cuda")
+    B.tq_mx_matmul(a, b, out, scratch(B.mx_matmul_workspace_bytes(m, n, k)))
+    want = torch.zeros(m, n)
+    want[1, 1] = torch.tensor(2.0 ** (sa + sb - 254), dtype=torch.float64).float()
+    assert torch.equal(out.cpu(), want)
