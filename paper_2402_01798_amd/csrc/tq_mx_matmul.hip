@@ -75,13 +75,14 @@ struct Tile {
     static constexpr int kRows = 64 / kPieces;                     // that one request of a wavefront covers
     static constexpr int kScales = (BM + BN) * kRow;               // where a buffer's scales begin
     static constexpr int kStage = kScales + (BM + BN) * 4 * GROUPS;
-    static constexpr int kLoads = (BM + BN) / kRows / kWaves;      // requests of codes, by every wavefront
+    static constexpr int kRequests = (BM + BN) / kRows;            // of codes, shared by the wavefronts; some make one a second time
+    static constexpr int kLoads = (kRequests + kWaves - 1) / kWaves;
     static constexpr int kScaleLoads = ((BM + BN) * GROUPS / 64 + kWaves - 1) / kWaves;
     static constexpr int kPerStage = kLoads + kScaleLoads;
     static constexpr int kRing = STAGES * kStage;
     static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
     static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
-    static_assert(BM % 64 == 0 && BN % 64 == 0 && (BM + BN) % (kRows * kWaves) == 0, "every wavefront requests the same");
+    static_assert(BM % 64 == 0 && BN % 64 == 0 && kBytes <= 160 << 10, "requests of scales are of 64 rows");
 };
 
 // Waits until the requests of all but the newest `newer` stages (at most N) are there.
@@ -94,8 +95,10 @@ __device__ __forceinline__ void wait_for_stages(uint32_t newer)
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER * N) : "memory");
 }
 
+// Two workgroups of 4 wavefronts at least on a compute unit: given all its registers the compiler keeps sums in those that only the
+// matrix instructions reach, and moves the addend there before anything else is requested.
 template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
-__global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(MatmulArgs g)
+__global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void mx_matmul_tile_kernel(MatmulArgs g)
 {
     using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
     extern __shared__ char lds[];
@@ -111,11 +114,12 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
     constexpr auto turn = [](uint32_t n) { return GROUPS == 1 ? n >> 2 & 3 : n >> 1 & 7; };
     const uint8_t* from[S::kLoads];                                // rows past the end repeat the last
     uint32_t scale_row[S::kScaleLoads];
-    static_assert(S::kRows * S::kWaves % 16 == 0, "turn, of period 16, is the same in each of a wavefront's requests");
+    static_assert(S::kRows * S::kWaves % 16 == 0 && (S::kRequests % S::kWaves == 0 || S::kRows == 16),
+                  "turn, of period 16, is the same in each of a wavefront's requests");
     const uint32_t piece = (lane % S::kPieces) ^ turn(wave * S::kRows + lane / S::kPieces);
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
-        const uint32_t c = i * S::kWaves + wave;                   // A's rows first
+        const uint32_t c = (i * S::kWaves + wave) % S::kRequests;  // A's rows first
         const bool is_a = c < BM / S::kRows;
         const uint32_t row = (is_a ? c : c - BM / S::kRows) * S::kRows + lane / S::kPieces;
         from[i] = (is_a ? g.a : g.b) + (uint64_t)(is_a ? min(row0 + row, g.m - 1) : min(col0 + row, g.n - 1)) * g.groups * 64;
@@ -139,7 +143,7 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
         const uint32_t at = (GROUPS == 1 || first + 1 < g.groups ? piece : piece & 3) * 16;
 #pragma unroll
         for (int i = 0; i < S::kLoads; ++i) {
-            const uint32_t c = i * S::kWaves + wave;
+            const uint32_t c = (i * S::kWaves + wave) % S::kRequests;
             __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)first * 64 + at), (lds_bytes*)(base + c * 1024), 16, 0, 0);
         }
 #pragma unroll
@@ -154,17 +158,34 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
 
     const uint32_t ra = wm * S::kFragsM * 32 + r, rb = BM + wn * S::kFragsN * 32 + r;
     f32x16 acc[S::kFragsM][S::kFragsN] = {};
-    if (g.add && part == 0 && split == 0) {                                      // requested first, so that it is there when the sums begin
+    // Of 32 x 32 outputs a lane holds 16: with its row of B first in the instruction, of one row 4 columns of every 8, which make
+    // whole 16-byte stores of 16-bit elements (bf16 2056 x 1000 x 1999 9.4 -> 8.7 us); else of one column 4 rows of every 8, 32 lanes
+    // with 128 bytes of fp32 in a row (fp32 with an addend, the same size, 13.2 -> 10.0 us).
+    constexpr bool kAlongRow = KS == 1 && DTYPE != TQ_F32;
+    if (g.add && part == 0 && split == 0) {                        // requested first, so that it is there when the sums begin
+        const bool whole = col0 + BN <= g.n;                       // no test between two requests
 #pragma unroll
         for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::kFragsN; ++j)
+            for (int j = 0; j < S::kFragsN; ++j) {
+                const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
+                if (kAlongRow && whole) {
+                    const float* from_row = g.add + min(row + r, g.m - 1) * g.lda + col + half * 4;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t row = row0 + (wm * S::kFragsM + i) * 32 + (e / 4) * 8 + half * 4 + e % 4;
-                    const uint32_t col = col0 + (wn * S::kFragsN + j) * 32 + r;
-                    acc[i][j][e] = g.add[min(row, g.m - 1) * g.lda + min(col, g.n - 1)];
+                    for (int q = 0; q < 4; ++q) {
+                        float v[4];
+                        __builtin_memcpy(v, from_row + q * 8, 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][q * 4 + e] = v[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t at = (e / 4) * 8 + half * 4 + e % 4;
+                        acc[i][j][e] = g.add[min(row + (kAlongRow ? r : at), g.m - 1) * g.lda + min(col + (kAlongRow ? at : r), g.n - 1)];
+                    }
                 }
+            }
     }
 #pragma unroll
     for (uint32_t t = 0; t < STAGES - 1; ++t)
@@ -198,11 +219,13 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
 #pragma unroll
             for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
-                for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = mfma32<0>(a[0][i], b[0][j], acc[i][j], sa[i], sb[j]);
+                for (int j = 0; j < S::kFragsN; ++j)
+                    acc[i][j] = kAlongRow ? mfma32<0>(b[0][j], a[0][i], acc[i][j], sb[j], sa[i]) : mfma32<0>(a[0][i], b[0][j], acc[i][j], sa[i], sb[j]);
 #pragma unroll
             for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
-                for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = mfma32<2>(a[1][i], b[1][j], acc[i][j], sa[i], sb[j]);
+                for (int j = 0; j < S::kFragsN; ++j)
+                    acc[i][j] = kAlongRow ? mfma32<2>(b[1][j], a[1][i], acc[i][j], sb[j], sa[i]) : mfma32<2>(a[1][i], b[1][j], acc[i][j], sa[i], sb[j]);
         }
         free_stage = stage;
         stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -228,14 +251,33 @@ __global__ __launch_bounds__(WM * WN * KS * 64) void mx_matmul_tile_kernel(Matmu
         }
         return;
     }
+    uint32_t me = threadIdx.x & 63;
+    asm volatile("" : "+v"(me));                                   // places in the output are found here, not kept through the loop
 #pragma unroll
     for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
-        for (int j = 0; j < S::kFragsN; ++j)
+        for (int j = 0; j < S::kFragsN; ++j) {
+            const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
+            if constexpr (kAlongRow) {                             // 4 columns changed for 4 with the other half make 8 in a row
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                store_one<DTYPE>(g, row0 + (wm * S::kFragsM + i) * 32 + (e / 4) * 8 + half * 4 + e % 4,
-                                 col0 + (wn * S::kFragsN + j) * 32 + r, acc[i][j][e]);
+                for (int q = 0; q < 2; ++q) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 8 + e]),
+                                                                        __float_as_uint(acc[i][j][q * 8 + 4 + e]), false, false);
+                        v[e] = __uint_as_float(w[0]);
+                        v[4 + e] = __uint_as_float(w[1]);
+                    }
+                    const uint32_t to_row = row + (me & 31), to_col = col + q * 16 + (me >> 5) * 8;
+                    if (to_row < g.m && to_col < g.n)
+                        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), acc[i][j][e]);
+            }
+        }
 }
 
 // Few rows of A (at most 32) against 32 rows of B, 8 wavefronts over parts of k: serving, where B is read once and bounds it.  The
@@ -391,41 +433,63 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
-// Which kernel.  Times in us, in turn, replayed from a graph; `256`, `128`, `64` are tiles of that side (16, 8 and 4 wavefronts),
-// `64/4` tiles of 64 with k in 4 parts (16 wavefronts), `few` the kernel for few rows:
-//   m x n x k            256    128     64   64/4    few
-//   8192 x 8192 x 8192   309    405    647    629              large tiles move least through the caches
-//   4096 x 4096 x 4096  45.2   56.0   85.4    102
-//   1037 x 8192 x 4096  37.7   38.6   46.6   57.7
-//   2048 x 2048 x 2048  20.9   11.6   13.7   18.0              256 leaves three quarters of the device without a tile
-//   4096 x 1000 x 784   14.5    8.9    9.4   15.3
-//   2056 x 1000 x 1999  20.5   10.4    9.9   13.7
-//   512 x 4096 x 4096   32.0   15.2   12.0   13.0
-//   256 x 4096 x 4096   31.8   14.7   10.6    7.6              64 too: the parts of k run beside each other
-//   128 x 8192 x 8192   54.8   25.8   18.0   12.7
-//   784 x 1000 x 64      8.1    4.8    3.9    4.6              nothing to part
-//   1 x 8192 x 8192     57.5   28.1   19.9    9.7    7.4
+// Which kernel.  Times in us of bf16 products, in turn, replayed from a graph, 64 x 64 outputs to a wavefront but in tiles of 128 and 64;
+// `64/4` are tiles of 64 with k in 4 parts, `few` is the kernel for few rows:
+//   m x n x k            256  256x128  128x320   192    128     64   64/4    few
+//   8192 x 8192 x 8192   301    325      360     372    390    459    645          large tiles move least through the caches
+//   4096 x 4096 x 4096  48.4   54.0     62.9    62.4   62.3   72.4    113
+//   5000 x 5000 x 3000  64.6   67.2     71.2    70.1   73.7   80.5    143
+//   2000 x 6000 x 4096  40.4   41.3     54.6    51.1   42.3   49.5   80.7          the others leave a last round with few tiles
+//   1037 x 8192 x 4096  38.3   40.2     34.1    52.4   39.6   39.3   63.0
+//   3000 x 3000 x 4096  37.2   39.0     34.2    32.0   39.1   39.5   62.2
+//   1500 x 4000 x 8192  58.6   44.3     51.3    48.5   47.9   52.0   68.4
+//   2048 x 2048 x 2048  20.2   14.2     16.5    16.1   11.7   11.4   20.0          256 leaves three quarters of the device without a tile
+//   4096 x 1000 x 784   12.3    9.4     10.3    10.4    7.9    8.3   16.5
+//   600 x 5000 x 3000   25.3   17.8     20.9    20.6   13.9   14.5   24.4
+//   2056 x 1000 x 1999  18.3   12.6     15.2    14.7    9.8    8.6   15.2
+//   512 x 4096 x 4096   31.5   20.7     25.8    25.0   15.5   11.4   14.5
+//   256 x 4096 x 4096   30.3   19.9     25.0    24.0   14.4    9.0    8.1          64 too: the parts of k run beside each other
+//   128 x 8192 x 8192   53.8   35.0     45.9    42.5   25.7   18.8   13.2
+//   784 x 1000 x 64      6.1    4.4      5.2     5.2    3.7    3.2    4.7          nothing to part
+//   1 x 8192 x 8192     51.7   34.5     43.6    41.5   24.2   17.6   11.3    7.3
+// Enough tiles of 128 for every compute unit: the shape whose rounds take least.  Where the sides leave little over this is 256.
 // Few tiles and a long k: k is split over workgroups too, where at least 40 groups (5 steps of a workgroup, the second launch's
 // price) are saved.  Not split / split, us: 64 x 64 x 8192 9.8 / 7.8, x 32768 28 / 9.5, x 131072 119 / 12, 256 x 256 x 32768 29 / 12,
 // 700 x 700 x 32768 35 / 26; with fewer saved it loses (500 x 500 x 4096 7.3 / 8.6).
-enum Shape { kFew, k256, k128, k64, k64InParts };
+enum Shape { kFew, k256, k256x128, k128x320, k192, k128, k64, k64InParts };
 
-uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side) { return (m + side - 1) / side * ((n + side - 1) / side); }
+// A tile's sides, and the time in ns that 128 elements of k took while 1, 2, .. of them, as many as fit, were at work on every
+// compute unit.
+struct Pace {
+    Shape shape;
+    uint64_t bm, bn;
+    uint32_t ns[3];
+};
+constexpr Pace kPaces[] = {{k256, 256, 256, {1070, 0, 0}}, {k256x128, 256, 128, {580, 1090, 0}}, {k128x320, 128, 320, {860, 0, 0}},
+                           {k192, 192, 192, {740, 0, 0}},  {k128, 128, 128, {400, 700, 1080}}};
+
+uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
+
+uint64_t pace(const Pace& p, uint64_t m, uint64_t n)
+{
+    const uint64_t fit = p.ns[2] ? 3 : p.ns[1] ? 2 : 1, each = (tiles_of(m, n, p.bm, p.bn) + kUnits - 1) / kUnits;
+    return each / fit * p.ns[fit - 1] + (each % fit ? p.ns[each % fit - 1] : 0);
+}
 
 Shape shape(uint64_t m, uint64_t n, uint64_t groups)
 {
     if (m <= kFewRowsInForm && few_bytes(m, groups) <= kFewBytes) return kFew;
-    const uint64_t of_256 = tiles_of(m, n, 256), of_128 = tiles_of(m, n, 128), of_64 = tiles_of(m, n, 64);
-    // A round of tiles of 256, one on each compute unit, takes as long as 820 tiles of 128.
-    if ((of_256 + kUnits - 1) / kUnits * 820 <= of_128) return k256;
-    if (of_128 >= kUnits) return k128;
-    return of_64 > kUnits || groups < 4 ? k64 : k64InParts;
+    if (tiles_of(m, n, 128, 128) < kUnits) return tiles_of(m, n, 64, 64) > kUnits || groups < 4 ? k64 : k64InParts;
+    const Pace* best = kPaces;
+    for (const Pace& p : kPaces)
+        if (pace(p, m, n) < pace(*best, m, n)) best = &p;
+    return best->shape;
 }
 
 uint32_t splits(uint64_t m, uint64_t n, uint64_t groups)
 {
     if (shape(m, n, groups) != k64InParts) return 1;
-    const uint64_t most = kUnits / tiles_of(m, n, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
+    const uint64_t most = kUnits / tiles_of(m, n, 64, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
     return s > 1 && groups - groups / s >= kSplitSaves ? (uint32_t)s : 1;
 }
 
@@ -436,8 +500,11 @@ hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
     switch (shape(g.m, g.n, g.groups)) {
         case kFew: return launch_few<DTYPE, -1>(g, st);
         case k256: return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
+        case k256x128: return launch_tile<DTYPE, 256, 128, 4, 2, 1, 1, 3>(g, st);
+        case k128x320: return launch_tile<DTYPE, 128, 320, 2, 5, 1, 1, 3>(g, st);
+        case k192: return launch_tile<DTYPE, 192, 192, 3, 3, 1, 1, 3>(g, st);
         case k128: return launch_tile<DTYPE, 128, 128, 2, 4, 1, 1, 3>(g, st);
-        case k64: return launch_tile<DTYPE, 64, 64, 2, 2, 1, 1, 3>(g, st);
+        case k64: return launch_tile<DTYPE, 64, 64, 2, 2, 1, 2, 2>(g, st);
         case k64InParts: break;
     }
     g.splits = splits(g.m, g.n, g.groups);

@@ -187,3 +187,20 @@ def test_scales_at_the_ends_of_their_range(m, n, k, sa, sb):
     want = torch.zeros(m, n)
     want[1, 1] = torch.tensor(2.0 ** (sa + sb - 254), dtype=torch.float64).float()
     assert torch.equal(out.cpu(), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(2051, 2045, 300), (2901, 2950, 200), (1037, 8192, 130), (1111, 8001, 130), (1500, 4001, 300), (5001, 1203, 500),
+                                   (700, 1301, 300), (2047, 2040, 513), (3713, 3701, 520)])
+@pytest.mark.parametrize("out,offset", [("f32", 0), ("bf16", 0), ("bf16", 3), ("f16", 1)])
+def test_product_in_tiles_of_every_shape(m, n, k, out, offset):
+    """Rows of the output begin at any element, and what lies between them is left alone."""
+    (a, va), (b, vb) = random_form(m, k, 11, 118, 122), random_form(n, k, 12, 118, 122)
+    va, vb = on_device(va), on_device(vb)
+    add = torch.randn(m, n + 5, generator=torch.Generator(device="cuda").manual_seed(13), device="cuda")[:, 2:n + 2]
+    ref, size = va @ vb.t().contiguous() + add.double(), va.abs() @ vb.abs().t().contiguous() + add.double().abs()
+    wide = torch.full((m, n + 2 * offset + 1), 7.0, dtype=LC.TYPES[out], device="cuda")
+    o = wide[:, offset:offset + n]
+    B.tq_mx_matmul(a, b, o, scratch(B.mx_matmul_workspace_bytes(m, n, k)), add=add)
+    bound = (k + 1) * 2.0 ** -23 * size + 1.001 * LC.HALF_ULP[out] * ref.abs() + (2.0 ** -25 if out == "f16" else 0.0)
+    assert ((o.double() - ref).abs() <= bound).all()
+    assert (wide[:, :offset] == 7).all() and (wide[:, offset + n:] == 7).all()
