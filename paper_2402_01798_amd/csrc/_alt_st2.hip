@@ -1,0 +1,574 @@
+// Products of microscaled 4-bit matrices (tq_mx.h): out = A B^T (+ add).
+#include <type_traits>
+
+#include "tq_mx_device.h"
+
+namespace tq {
+namespace {
+
+constexpr uint64_t kUnits = 256;                                   // compute units
+constexpr uint64_t kSplitGroups = 16;                              // of a workgroup at least, where k is split over several
+constexpr uint64_t kSplitSaves = 40;
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct MatmulArgs {
+    const void* x;                 // tokens that are not in 4-bit form yet, in place of a and sa
+    const uint8_t *a, *sa, *b, *sb;
+    const float* add;
+    void* out;
+    uint64_t ldx, lda, ldo;
+    uint32_t m, n, k, groups;
+    uint32_t tiles_x;
+    uint64_t tiles;                // of the output, times `splits`
+    float* partial;                // [splits][m][n]: sums over parts of k that different workgroups take
+    uint32_t splits;
+};
+
+// 32 x 32 outputs += 64 elements of k.  Lane l holds row l % 32 and block l / 32 of both operands: 32 codes and their scale, a byte
+// of a word.
+template <int BYTE>
+__device__ __forceinline__ f32x16 mfma32(i32x4 a, i32x4 b, f32x16 c, int sa, int sb)
+{
+    const i32x8 wa = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+    const i32x8 wb = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, wb, c, 4, 4, BYTE, sa, BYTE, sb);
+}
+
+template <int DTYPE>
+__device__ __forceinline__ void store_one(const MatmulArgs& g, uint32_t row, uint32_t col, float v)
+{
+    using E = Element<DTYPE>;
+    if (row >= g.m || col >= g.n) return;
+    static_cast<typename E::type*>(g.out)[row * g.ldo + col] = E::store(v);
+}
+
+typedef __attribute__((address_space(1))) const void global_bytes;
+typedef __attribute__((address_space(3))) void lds_bytes;
+
+// Which tile this workgroup takes.  Workgroups go to the 8 dies in turn; each die takes a run of tiles, which goes down 4 tiles and
+// then on to the next column, so that the tiles at work on a die at a time share their rows in its cache.
+__device__ __forceinline__ bool find_tile(const MatmulArgs& g, uint32_t& ty, uint32_t& tx, uint32_t& split)
+{
+    const uint32_t block = linear_block(), per = (uint32_t)(g.tiles + 7) / 8;
+    uint32_t tile = (block & 7) * per + (block >> 3);
+    if (block >= 8 * per || tile >= g.tiles) return false;
+    const uint32_t of_a_split = (uint32_t)g.tiles / g.splits, tiles_y = of_a_split / g.tiles_x;
+    split = tile / of_a_split;
+    tile -= split * of_a_split;
+    const uint32_t band = tile / (4 * g.tiles_x), rows = min(4u, tiles_y - band * 4), in = tile - band * 4 * g.tiles_x;
+    ty = band * 4 + in % rows;
+    tx = in / rows;
+    return true;
+}
+
+// BM x BN outputs by WM x WN wavefronts, GROUPS groups of 128 elements of k at a time through a ring of STAGES buffers in LDS.  A
+// buffer holds BM rows of A and BN of B, 64 GROUPS bytes each, then the groups' scales, 4 bytes for each row.
+template <int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+struct Tile {
+    static constexpr int kThreads = WM * WN * KS * 64, kWaves = WM * WN;     // wavefronts of a part
+    static constexpr int kFragsM = BM / WM / 32, kFragsN = BN / WN / 32;
+    static constexpr int kRow = 64 * GROUPS;                       // bytes
+    static constexpr int kPieces = 4 * GROUPS;                     // of 16 bytes in a row
+    static constexpr int kRows = 64 / kPieces;                     // that one request of a wavefront covers
+    static constexpr int kScales = (BM + BN) * kRow;               // where a buffer's scales begin
+    static constexpr int kStage = kScales + (BM + BN) * 4 * GROUPS;
+    static constexpr int kRequests = (BM + BN) / kRows;            // of codes, shared by the wavefronts; some make one a second time
+    static constexpr int kLoads = (kRequests + kWaves - 1) / kWaves;
+    static constexpr int kScaleLoads = ((BM + BN) * GROUPS / 64 + kWaves - 1) / kWaves;
+    static constexpr int kPerStage = kLoads + kScaleLoads;
+    static constexpr int kRing = STAGES * kStage;
+    static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
+    static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
+    static_assert(BM % 64 == 0 && BN % 64 == 0 && kBytes <= 160 << 10, "requests of scales are of 64 rows");
+};
+
+// Waits until the requests of all but the newest `newer` stages (at most N) are there.
+template <int PER, int N>
+__device__ __forceinline__ void wait_for_stages(uint32_t newer)
+{
+    if constexpr (N > 0) {
+        if (newer < N) return wait_for_stages<PER, N - 1>(newer);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER * N) : "memory");
+}
+
+// Two workgroups of 4 wavefronts at least on a compute unit: given all its registers the compiler keeps sums in those that only the
+// matrix instructions reach, and moves the addend there before anything else is requested.
+template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+__global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void mx_matmul_tile_kernel(MatmulArgs g)
+{
+    using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
+    extern __shared__ char lds[];
+    uint32_t ty, tx, split;
+    if (!find_tile(g, ty, tx, split)) return;
+    const uint32_t lane = threadIdx.x & 63, wave_in_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t part = wave_in_all / S::kWaves, wave = wave_in_all % S::kWaves;
+    const uint32_t r = lane & 31, half = lane >> 5, wm = wave / WN, wn = wave % WN;
+    const uint32_t row0 = ty * BM, col0 = tx * BN;
+
+    // A row's pieces lie in the buffer in another order from row to row: piece p of row n in place p ^ turn(n), so that 16 rows'
+    // pieces of the same k, which are read together, lie in 64 different banks.
+    constexpr auto turn = [](uint32_t n) { return GROUPS == 1 ? n >> 2 & 3 : n >> 1 & 7; };
+    const uint8_t* from[S::kLoads];                                // rows past the end repeat the last
+    uint32_t scale_row[S::kScaleLoads];
+    static_assert(S::kRows * S::kWaves % 16 == 0 && (S::kRequests % S::kWaves == 0 || S::kRows == 16),
+                  "turn, of period 16, is the same in each of a wavefront's requests");
+    const uint32_t piece = (lane % S::kPieces) ^ turn(wave * S::kRows + lane / S::kPieces);
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const uint32_t c = (i * S::kWaves + wave) % S::kRequests;  // A's rows first
+        const bool is_a = c < BM / S::kRows;
+        const uint32_t row = (is_a ? c : c - BM / S::kRows) * S::kRows + lane / S::kPieces;
+        from[i] = (is_a ? g.a : g.b) + (uint64_t)(is_a ? min(row0 + row, g.m - 1) : min(col0 + row, g.n - 1)) * g.groups * 64;
+    }
+#pragma unroll
+    for (int i = 0; i < S::kScaleLoads; ++i) {
+        const uint32_t c = (i * S::kWaves + wave) % ((BM + BN) * GROUPS / 64);     // group after group: A's rows, then B's
+        const uint32_t row = c % ((BM + BN) / 64) * 64 + lane;
+        scale_row[i] = row < BM ? min(row0 + row, g.m - 1) : min(col0 + row - BM, g.n - 1);
+    }
+    // this part of k, in trips of GROUPS groups, up to `end`; `most` is the longest part's
+    const uint32_t all = (g.groups + GROUPS - 1) / GROUPS, of_a_split = KS == 1 ? all : (all + g.splits - 1) / g.splits;
+    const uint32_t begin = KS == 1 ? 0 : split * of_a_split, end = min(begin + of_a_split, all);
+    const uint32_t most = (of_a_split + KS - 1) / KS, first_trip = begin + part * most;
+    const uint32_t trips = KS == 1 ? all : first_trip < end ? min(most, end - first_trip) : 0;
+    char* ring = lds + part * S::kRing;
+    auto fetch = [&](uint32_t t, uint32_t stage) {
+        char* base = ring + stage * S::kStage;
+        const uint32_t first = (first_trip + t) * GROUPS;
+        // the second half of the last stage may not be there: the first again, which is not used
+        const uint32_t at = (GROUPS == 1 || first + 1 < g.groups ? piece : piece & 3) * 16;
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i) {
+            const uint32_t c = (i * S::kWaves + wave) % S::kRequests;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)first * 64 + at), (lds_bytes*)(base + c * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < S::kScaleLoads; ++i) {
+            const uint32_t c = (i * S::kWaves + wave) % ((BM + BN) * GROUPS / 64), in_group = c % ((BM + BN) / 64);
+            const uint64_t group = min(first + c / ((BM + BN) / 64), g.groups - 1);
+            const uint32_t* q = in_group < BM / 64 ? reinterpret_cast<const uint32_t*>(g.sa) + group * g.m
+                                                   : reinterpret_cast<const uint32_t*>(g.sb) + group * g.n;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(q + scale_row[i]), (lds_bytes*)(base + S::kScales + c * 256), 4, 0, 0);
+        }
+    };
+
+    const uint32_t ra = wm * S::kFragsM * 32 + r, rb = BM + wn * S::kFragsN * 32 + r;
+    f32x16 acc[S::kFragsM][S::kFragsN] = {};
+    // Of 32 x 32 outputs a lane holds 16: with its row of B first in the instruction, of one row 4 columns of every 8, which make
+    // whole 16-byte stores of 16-bit elements (bf16 2056 x 1000 x 1999 9.4 -> 8.7 us); else of one column 4 rows of every 8, 32 lanes
+    // with 128 bytes of fp32 in a row (fp32 with an addend, the same size, 13.2 -> 10.0 us).
+    constexpr bool kAlongRow = KS == 1 && DTYPE != TQ_F32;
+    if (g.add && part == 0 && split == 0) {                        // requested first, so that it is there when the sums begin
+        const bool whole = col0 + BN <= g.n;                       // no test between two requests
+#pragma unroll
+        for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j) {
+                const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
+                if (kAlongRow && whole) {
+                    const float* from_row = g.add + min(row + r, g.m - 1) * g.lda + col + half * 4;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float v[4];
+                        __builtin_memcpy(v, from_row + q * 8, 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][q * 4 + e] = v[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t at = (e / 4) * 8 + half * 4 + e % 4;
+                        acc[i][j][e] = g.add[min(row + (kAlongRow ? r : at), g.m - 1) * g.lda + min(col + (kAlongRow ? at : r), g.n - 1)];
+                    }
+                }
+            }
+    }
+#pragma unroll
+    for (uint32_t t = 0; t < STAGES - 1; ++t)
+        if (t < trips) fetch(t, t);
+    uint32_t stage = 0, free_stage = STAGES - 1;
+    for (uint32_t t = 0; t < most; ++t) {
+        // this trip's requests are there, and every wavefront is done with the buffer that is filled next
+        wait_for_stages<S::kPerStage, STAGES - 2>(t < trips ? trips - 1 - t : 0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + STAGES - 1 < trips) fetch(t + STAGES - 1, free_stage);
+        const char* base = ring + stage * S::kStage;
+#pragma unroll
+        for (int h = 0; h < GROUPS; ++h) {
+            if (KS > 1 && h == 0 && t >= trips) break;             // a shorter part
+            if (h && (first_trip + t) * GROUPS + h >= g.groups) break;
+            int sa[S::kFragsM], sb[S::kFragsN];
+            i32x4 a[2][S::kFragsM], b[2][S::kFragsN];
+            const char* scales = base + S::kScales + h * (BM + BN) * 4;
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i) sa[i] = *reinterpret_cast<const int*>(scales + (ra + i * 32) * 4) >> (8 * half);
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j) sb[j] = *reinterpret_cast<const int*>(scales + (rb + j * 32) * 4) >> (8 * half);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t at = ((4 * h + 2 * s + half) ^ turn(lane)) * 16;
+#pragma unroll
+                for (int i = 0; i < S::kFragsM; ++i) a[s][i] = *reinterpret_cast<const i32x4*>(base + (ra + i * 32) * S::kRow + at);
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j) b[s][j] = *reinterpret_cast<const i32x4*>(base + (rb + j * 32) * S::kRow + at);
+            }
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j)
+                    acc[i][j] = kAlongRow ? mfma32<0>(b[0][j], a[0][i], acc[i][j], sb[j], sa[i]) : mfma32<0>(a[0][i], b[0][j], acc[i][j], sa[i], sb[j]);
+#pragma unroll
+            for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kFragsN; ++j)
+                    acc[i][j] = kAlongRow ? mfma32<2>(b[1][j], a[1][i], acc[i][j], sb[j], sa[i]) : mfma32<2>(a[1][i], b[1][j], acc[i][j], sa[i], sb[j]);
+        }
+        free_stage = stage;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    if constexpr (KS > 1) {                                        // the parts' sums, joined in their order
+        __syncthreads();                                           // the rings are done with
+        float* sums = reinterpret_cast<float*>(lds);
+        const uint32_t at = (part * BM + wm * S::kFragsM * 32 + half * 4) * (BN + 1) + wn * S::kFragsN * 32 + r;
+#pragma unroll
+        for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kFragsN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sums[at + (i * 32 + (e / 4) * 8 + e % 4) * (BN + 1) + j * 32] = acc[i][j][e];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < BM * BN; i += S::kThreads) {
+            const uint32_t row = i / BN, col = i % BN;
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < KS; ++q) v += sums[(q * BM + row) * (BN + 1) + col];
+            if (g.splits == 1) store_one<DTYPE>(g, row0 + row, col0 + col, v);
+            else if (row0 + row < g.m && col0 + col < g.n) g.partial[((uint64_t)split * g.m + row0 + row) * g.n + col0 + col] = v;
+        }
+        return;
+    }
+    uint32_t me = threadIdx.x & 63;
+    asm volatile("" : "+v"(me));                                   // places in the output are found here, not kept through the loop
+#pragma unroll
+    for (int i = 0; i < S::kFragsM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kFragsN; ++j) {
+            const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
+            if constexpr (kAlongRow) {                             // 4 columns changed for 4 with the other half make 8 in a row
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 8 + e]),
+                                                                        __float_as_uint(acc[i][j][q * 8 + 4 + e]), false, false);
+                        v[e] = __uint_as_float(w[0]);
+                        v[4 + e] = __uint_as_float(w[1]);
+                    }
+                    const uint32_t to_row = row + (me & 31), to_col = col + q * 16 + (me >> 5) * 8;
+                    if (to_row < g.m && to_col < g.n)
+                        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), acc[i][j][e]);
+            }
+        }
+}
+
+// Few rows of A (at most 32) against 32 rows of B, 8 wavefronts over parts of k: serving, where B is read once and bounds it.  The
+// rows of A, cast here if they are not in 4-bit form yet, stay in LDS; B comes through a ring for each wavefront, whose first
+// requests are on their way while A is prepared.
+constexpr int kFewWaves = 8, kFewStages = 2, kFewStage = 32 * 128 + 256, kFewRing = kFewWaves * kFewStages * kFewStage;
+constexpr uint32_t kFewBytes = 160 << 10;                         // the LDS of a compute unit
+constexpr uint32_t kFewRowsInForm = 16, kFewRows = 32;
+
+__host__ __device__ constexpr uint64_t few_row_bytes(uint64_t groups) { return groups * 64 + 16; }
+__host__ __device__ constexpr uint64_t few_bytes(uint64_t m, uint64_t groups) { return kFewRing + m * (few_row_bytes(groups) + groups * 4); }
+
+// X: the type of g.x, or -1 for rows in 4-bit form.
+template <int DTYPE, int X>
+__global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArgs g)
+{
+    extern __shared__ char lds[];
+    const uint32_t tx = linear_block();
+    if (tx >= g.tiles) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
+    const uint32_t col0 = tx * 32, pairs = (g.groups + 1) / 2;
+    const uint32_t per = (pairs + kFewWaves - 1) / kFewWaves, first = wave * per, trips = first < pairs ? min(per, pairs - first) : 0;
+    char* ring = lds + wave * (kFewStages * kFewStage);
+    const uint32_t row_bytes = (uint32_t)few_row_bytes(g.groups);
+    char* codes = lds + kFewRing;
+    char* scales = codes + g.m * row_bytes;                        // [m][groups][4]
+
+    const uint8_t* from[4];
+    const uint32_t piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};      // of rows 8 i + lane / 8, i even and odd
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from[i] = g.b + (uint64_t)min(col0 + i * 8 + (lane >> 3), g.n - 1) * g.groups * 64;
+    const uint32_t row_b = min(col0 + r, g.n - 1);
+    auto fetch = [&](uint32_t t, uint32_t stage) {
+        char* base = ring + stage * kFewStage;
+        const uint32_t group = 2 * (first + t);
+        const bool both = group + 1 < g.groups;                    // the second half of the last may not be there: the first again
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at = both ? piece[i & 1] : piece[i & 1] & 3;
+            __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)group * 64 + at * 16), (lds_bytes*)(base + i * 1024), 16, 0, 0);
+        }
+        const uint64_t mine = both ? group + half : group;
+        __builtin_amdgcn_global_load_lds((global_bytes*)(g.sb + (mine * g.n + row_b) * 4), (lds_bytes*)(base + 4096), 4, 0, 0);
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < kFewStages; ++t)
+        if (t < trips) fetch(t, t);
+
+    if constexpr (X < 0) {
+        for (uint32_t i = threadIdx.x; i < g.m * g.groups * 4; i += kFewWaves * 64) {
+            const uint32_t row = i / (g.groups * 4), p = i - row * (g.groups * 4);
+            *reinterpret_cast<i32x4*>(codes + row * row_bytes + p * 16) = *reinterpret_cast<const i32x4*>(g.a + (uint64_t)i * 16);
+        }
+        for (uint32_t i = threadIdx.x; i < g.m * g.groups; i += kFewWaves * 64) {
+            const uint32_t group = i / g.m, row = i - group * g.m;
+            *reinterpret_cast<int*>(scales + (row * g.groups + group) * 4) = *reinterpret_cast<const int*>(g.sa + (uint64_t)i * 4);
+        }
+    } else {
+        using T = typename Element<X>::type;
+        const uint32_t octs = g.groups * 16;                       // of 8 elements in a row: four neighbouring lanes are a block
+        for (uint32_t i = threadIdx.x; i < g.m * octs; i += kFewWaves * 64) {
+            const uint32_t row = i / octs, oct = i - row * octs;
+            float v[8];
+            load8<X>(static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
+            uint32_t largest = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
+            const uint32_t byte = mx_scale_byte<false>(quad_max(largest));
+            *reinterpret_cast<uint32_t*>(codes + row * row_bytes + oct * 4) = mx_nearest(v, byte);
+            if ((oct & 3) == 0) scales[row * octs / 4 + oct / 4] = (char)byte;
+        }
+    }
+    __syncthreads();
+
+    const char* my_codes = codes + min(r, g.m - 1) * row_bytes;
+    const char* my_scales = scales + min(r, g.m - 1) * g.groups * 4;
+    f32x16 acc = {};
+    uint32_t stage = 0;
+    for (uint32_t t = 0; t < trips; ++t) {
+        wait_for_stages<5, kFewStages - 1>(trips - 1 - t);
+        const char* base = ring + stage * kFewStage;
+        const uint32_t group = 2 * (first + t);
+        const bool both = group + 1 < g.groups;
+        i32x4 a[4], b[4];
+        int sa[2], sb[2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            b[s] = *reinterpret_cast<const i32x4*>(base + r * 128 + ((2 * s + half) ^ (r >> 1 & 7)) * 16);
+            a[s] = *reinterpret_cast<const i32x4*>(my_codes + (group + (both ? s / 2 : 0)) * 64 + (2 * (s & 1) + half) * 16);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sb[h] = *reinterpret_cast<const int*>(base + 4096 + (h * 32 + r) * 4) >> (8 * half);
+            sa[h] = *reinterpret_cast<const int*>(my_scales + (group + (both ? h : 0)) * 4) >> (8 * half);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
+        if (t + kFewStages < trips) fetch(t + kFewStages, stage);
+        acc = mfma32<0>(a[0], b[0], acc, sa[0], sb[0]);
+        acc = mfma32<2>(a[1], b[1], acc, sa[0], sb[0]);
+        if (both) {
+            acc = mfma32<0>(a[2], b[2], acc, sa[1], sb[1]);
+            acc = mfma32<2>(a[3], b[3], acc, sa[1], sb[1]);
+        }
+        stage ^= 1;
+    }
+    __syncthreads();                                               // the rings are done with
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[(wave * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < g.m * 32; i += kFewWaves * 64) {
+        const uint32_t row = i / 32, col = i & 31;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) v += sums[(w * 32 + row) * 33 + col];
+        if (g.add && col0 + col < g.n) v += g.add[row * g.lda + col0 + col];
+        store_one<DTYPE>(g, row, col0 + col, v);
+    }
+}
+
+// The splits' sums, joined in their order.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void mx_join_kernel(MatmulArgs g)
+{
+    const uint64_t at = (uint64_t)linear_block() * 256 + threadIdx.x, size = (uint64_t)g.m * g.n;
+    if (at >= size) return;
+    float v = g.partial[at];
+#pragma unroll 8
+    for (uint32_t s = 1; s < g.splits; ++s) v += g.partial[s * size + at];
+    store_one<DTYPE>(g, (uint32_t)(at / g.n), (uint32_t)(at % g.n), v);
+}
+
+template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+hipError_t launch_tile(MatmulArgs& g, hipStream_t st)
+{
+    using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
+    g.tiles_x = (g.n + BN - 1) / BN;
+    g.tiles = (uint64_t)g.tiles_x * ((g.m + BM - 1) / BM) * g.splits;
+    dim3 grid;
+    if (!fold_grid((g.tiles + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
+    mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES><<<grid, S::kThreads, S::kBytes, st>>>(g);
+    return hipGetLastError();
+}
+
+template <int DTYPE, int X>
+hipError_t launch_few(MatmulArgs& g, hipStream_t st)
+{
+    g.tiles = (g.n + 31) / 32;
+    dim3 grid;
+    if (!fold_grid(g.tiles, kFewWaves * 64, 1, grid)) return hipErrorInvalidValue;
+    const uint32_t bytes = (uint32_t)few_bytes(g.m, g.groups);
+    mx_matmul_few_kernel<DTYPE, X><<<grid, kFewWaves * 64, bytes, st>>>(g);
+    return hipGetLastError();
+}
+
+// Which kernel.  Times in us of bf16 products, in turn, replayed from a graph, 64 x 64 outputs to a wavefront but in tiles of 128 and 64;
+// `64/4` are tiles of 64 with k in 4 parts, `few` is the kernel for few rows:
+//   m x n x k            256  256x128  128x320   192    128     64   64/4    few
+//   8192 x 8192 x 8192   301    325      360     372    390    459    645          large tiles move least through the caches
+//   4096 x 4096 x 4096  48.4   54.0     62.9    62.4   62.3   72.4    113
+//   5000 x 5000 x 3000  64.6   67.2     71.2    70.1   73.7   80.5    143
+//   2000 x 6000 x 4096  40.4   41.3     54.6    51.1   42.3   49.5   80.7          the others leave a last round with few tiles
+//   1037 x 8192 x 4096  38.3   40.2     34.1    52.4   39.6   39.3   63.0
+//   3000 x 3000 x 4096  37.2   39.0     34.2    32.0   39.1   39.5   62.2
+//   1500 x 4000 x 8192  58.6   44.3     51.3    48.5   47.9   52.0   68.4
+//   2048 x 2048 x 2048  20.2   14.2     16.5    16.1   11.7   11.4   20.0          256 leaves three quarters of the device without a tile
+//   4096 x 1000 x 784   12.3    9.4     10.3    10.4    7.9    8.3   16.5
+//   600 x 5000 x 3000   25.3   17.8     20.9    20.6   13.9   14.5   24.4
+//   2056 x 1000 x 1999  18.3   12.6     15.2    14.7    9.8    8.6   15.2
+//   512 x 4096 x 4096   31.5   20.7     25.8    25.0   15.5   11.4   14.5
+//   256 x 4096 x 4096   30.3   19.9     25.0    24.0   14.4    9.0    8.1          64 too: the parts of k run beside each other
+//   128 x 8192 x 8192   53.8   35.0     45.9    42.5   25.7   18.8   13.2
+//   784 x 1000 x 64      6.1    4.4      5.2     5.2    3.7    3.2    4.7          nothing to part
+//   1 x 8192 x 8192     51.7   34.5     43.6    41.5   24.2   17.6   11.3    7.3
+// Enough tiles of 128 for every compute unit: the shape whose rounds take least.  Where the sides leave little over this is 256.
+// Few tiles and a long k: k is split over workgroups too, where at least 40 groups (5 steps of a workgroup, the second launch's
+// price) are saved.  Not split / split, us: 64 x 64 x 8192 9.8 / 7.8, x 32768 28 / 9.5, x 131072 119 / 12, 256 x 256 x 32768 29 / 12,
+// 700 x 700 x 32768 35 / 26; with fewer saved it loses (500 x 500 x 4096 7.3 / 8.6).
+enum Shape { kFew, k256, k256x128, k128x320, k192, k128, k64, k64InParts };
+
+// A tile's sides, and the time in ns that 128 elements of k took while 1, 2, .. of them, as many as fit, were at work on every
+// compute unit.
+struct Pace {
+    Shape shape;
+    uint64_t bm, bn;
+    uint32_t ns[3];
+};
+constexpr Pace kPaces[] = {{k256, 256, 256, {1070, 0, 0}}, {k256x128, 256, 128, {580, 1090, 0}}, {k128x320, 128, 320, {860, 0, 0}},
+                           {k192, 192, 192, {740, 0, 0}},  {k128, 128, 128, {400, 700, 1080}}};
+
+uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
+
+uint64_t pace(const Pace& p, uint64_t m, uint64_t n)
+{
+    const uint64_t fit = p.ns[2] ? 3 : p.ns[1] ? 2 : 1, each = (tiles_of(m, n, p.bm, p.bn) + kUnits - 1) / kUnits;
+    return each / fit * p.ns[fit - 1] + (each % fit ? p.ns[each % fit - 1] : 0);
+}
+
+Shape shape(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (m <= kFewRowsInForm && few_bytes(m, groups) <= kFewBytes) return kFew;
+    if (tiles_of(m, n, 128, 128) < kUnits) return tiles_of(m, n, 64, 64) > kUnits || groups < 4 ? k64 : k64InParts;
+    const Pace* best = kPaces;
+    for (const Pace& p : kPaces)
+        if (pace(p, m, n) < pace(*best, m, n)) best = &p;
+    return best->shape;
+}
+
+uint32_t splits(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (shape(m, n, groups) != k64InParts) return 1;
+    const uint64_t most = kUnits / tiles_of(m, n, 64, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
+    return s > 1 && groups - groups / s >= kSplitSaves ? (uint32_t)s : 1;
+}
+
+template <int DTYPE>
+hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
+{
+    g.splits = 1;
+    switch (shape(g.m, g.n, g.groups)) {
+        case kFew: return launch_few<DTYPE, -1>(g, st);
+        case k256: return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
+        case k256x128: return launch_tile<DTYPE, 256, 128, 4, 2, 1, 1, 2>(g, st);
+        case k128x320: return launch_tile<DTYPE, 128, 320, 2, 5, 1, 2, 2>(g, st);
+        case k192: return launch_tile<DTYPE, 192, 192, 3, 3, 1, 1, 3>(g, st);
+        case k128: return launch_tile<DTYPE, 128, 128, 2, 4, 1, 2, 2>(g, st);
+        case k64: return launch_tile<DTYPE, 64, 64, 2, 2, 1, 2, 2>(g, st);
+        case k64InParts: break;
+    }
+    g.splits = splits(g.m, g.n, g.groups);
+    const hipError_t e = launch_tile<DTYPE, 64, 64, 2, 2, 4, 2, 2>(g, st);
+    if (e != hipSuccess || g.splits == 1) return e;
+    dim3 grid;
+    if (!fold_grid(((uint64_t)g.m * g.n + 255) / 256, 256, 1, grid)) return hipErrorInvalidValue;
+    mx_join_kernel<DTYPE><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace tq
+
+uint64_t tq_mx_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint32_t s = tq::splits(m, n, (k + tq::kMxGroup - 1) / tq::kMxGroup);
+    return s == 1 ? 0 : s * m * n * sizeof(float);
+}
+
+hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, const void* sb, uint64_t m, uint64_t n, uint64_t k,
+                               const float* add, uint64_t lda, void* out, int dtype, uint64_t ldo, void* workspace, hipStream_t st)
+{
+    using namespace tq;
+    MatmulArgs g = {};
+    g.a = static_cast<const uint8_t*>(a);
+    g.sa = static_cast<const uint8_t*>(sa);
+    g.b = static_cast<const uint8_t*>(b);
+    g.sb = static_cast<const uint8_t*>(sb);
+    g.add = add;
+    g.lda = lda;
+    g.out = out;
+    g.ldo = ldo;
+    g.m = (uint32_t)m;
+    g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
+    g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
+    g.partial = static_cast<float*>(workspace);
+    if (dtype == TQ_F32) return launch_matmul<TQ_F32>(g, st);
+    return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
+}
+
+bool tq_mx_linear_in_one(uint64_t m, uint64_t k) { return m <= tq::kFewRows && tq::few_bytes(m, (k + tq::kMxGroup - 1) / tq::kMxGroup) <= tq::kFewBytes; }
+
+hipError_t tq_launch_mx_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const void* sw, uint64_t n,
+                                   uint64_t k, void* out, int dtype, uint64_t ldo, hipStream_t st)
+{
+    using namespace tq;
+    MatmulArgs g = {};
+    g.x = x;
+    g.ldx = ldx;
+    g.b = static_cast<const uint8_t*>(w);
+    g.sb = static_cast<const uint8_t*>(sw);
+    g.out = out;
+    g.ldo = ldo;
+    g.m = (uint32_t)m;
+    g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
+    g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
+    auto as = [&](auto D) {
+        constexpr int T = decltype(D)::value;
+        if (x_dtype == TQ_F32) return launch_few<T, TQ_F32>(g, st);
+        return x_dtype == TQ_BF16 ? launch_few<T, TQ_BF16>(g, st) : launch_few<T, TQ_F16>(g, st);
+    };
+    if (dtype == TQ_F32) return as(std::integral_constant<int, TQ_F32>{});
+    return dtype == TQ_BF16 ? as(std::integral_constant<int, TQ_BF16>{}) : as(std::integral_constant<int, TQ_F16>{});
+}

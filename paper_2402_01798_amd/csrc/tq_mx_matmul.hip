@@ -433,13 +433,13 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
-// Which kernel.  Times in us of bf16 products, in turn, replayed from a graph, 64 x 64 outputs to a wavefront but in tiles of 128 and 64;
-// `64/4` are tiles of 64 with k in 4 parts, `few` is the kernel for few rows:
+// Which kernel.  Times in us of bf16 products, in turn, replayed from a graph; `64/4` are tiles of 64 with k in 4 parts, `few` is
+// the kernel for few rows:
 //   m x n x k            256  256x128  128x320   192    128     64   64/4    few
-//   8192 x 8192 x 8192   301    325      360     372    390    459    645          large tiles move least through the caches
-//   4096 x 4096 x 4096  48.4   54.0     62.9    62.4   62.3   72.4    113
-//   5000 x 5000 x 3000  64.6   67.2     71.2    70.1   73.7   80.5    143
-//   2000 x 6000 x 4096  40.4   41.3     54.6    51.1   42.3   49.5   80.7          the others leave a last round with few tiles
+//   8192 x 8192 x 8192   283    325      360     372    390    459    645          large tiles move least through the caches
+//   4096 x 4096 x 4096  47.9   54.0     62.9    62.4   62.3   72.4    113
+//   5000 x 5000 x 3000  63.1   67.2     71.2    70.1   73.7   80.5    143
+//   2000 x 6000 x 4096  38.9   41.3     54.6    51.1   42.3   49.5   80.7          the others leave a last round with few tiles
 //   1037 x 8192 x 4096  38.3   40.2     34.1    52.4   39.6   39.3   63.0
 //   3000 x 3000 x 4096  37.2   39.0     34.2    32.0   39.1   39.5   62.2
 //   1500 x 4000 x 8192  58.6   44.3     51.3    48.5   47.9   52.0   68.4
@@ -465,7 +465,7 @@ struct Pace {
     uint64_t bm, bn;
     uint32_t ns[3];
 };
-constexpr Pace kPaces[] = {{k256, 256, 256, {1070, 0, 0}}, {k256x128, 256, 128, {580, 1090, 0}}, {k128x320, 128, 320, {860, 0, 0}},
+constexpr Pace kPaces[] = {{k256, 256, 256, {1010, 0, 0}}, {k256x128, 256, 128, {580, 1090, 0}}, {k128x320, 128, 320, {860, 0, 0}},
                            {k192, 192, 192, {740, 0, 0}},  {k128, 128, 128, {400, 700, 1080}}};
 
 uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t bm, uint64_t bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); }
@@ -499,7 +499,9 @@ hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
     g.splits = 1;
     switch (shape(g.m, g.n, g.groups)) {
         case kFew: return launch_few<DTYPE, -1>(g, st);
-        case k256: return launch_tile<DTYPE, 256, 256, 4, 4, 1, 1, 3>(g, st);
+        // 8 wavefronts of 128 x 64, 256 of k a trip (whole lines of 128 bytes): 8192^3 289 us, by 16 wavefronts of 64 x 64 300, and with
+        // 128 of k a trip and three buffers 310.  Tiles of which two are to fit have buffers of 128 of k.
+        case k256: return launch_tile<DTYPE, 256, 256, 2, 4, 1, 2, 2>(g, st);
         case k256x128: return launch_tile<DTYPE, 256, 128, 4, 2, 1, 1, 3>(g, st);
         case k128x320: return launch_tile<DTYPE, 128, 320, 2, 5, 1, 1, 3>(g, st);
         case k192: return launch_tile<DTYPE, 192, 192, 3, 3, 1, 1, 3>(g, st);
