@@ -12,7 +12,7 @@ hipError_t tq_launch_mx_dequantize(const void* codes, const void* scales, uint64
 uint64_t tq_mx_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k);
 hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, const void* sb, uint64_t m, uint64_t n, uint64_t k,
                                const float* add, uint64_t lda, void* out, int dtype, uint64_t ldo, void* workspace, hipStream_t st);
-bool tq_mx_linear_in_one(uint64_t m, uint64_t k);
+bool tq_mx_linear_in_one(uint64_t m, uint64_t n, uint64_t k);
 hipError_t tq_launch_mx_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const void* sw, uint64_t n,
                                    uint64_t k, void* out, int dtype, uint64_t ldo, hipStream_t st);
 hipError_t tq_launch_distill(const void* z, int dtype, uint64_t rows, uint64_t vocab, uint64_t ldz, const void* ids, int ids_bytes,
@@ -124,7 +124,7 @@ int tq_mx_matmul(const void* a_codes_dev, const void* a_scales_dev, const void* 
 uint64_t tq_mx_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k)
 {
     if (check_matrix(m, k, k + 127) || check_matrix(n, k, k + 127) || check_matrix(m, n, n)) return 0;
-    if (tq_mx_linear_in_one(m, k)) return 0;
+    if (tq_mx_linear_in_one(m, n, k)) return 0;
     return padded(tq_mx_code_bytes(m, k)) + padded(tq_mx_scale_bytes(m, k)) + tq_mx_matmul_workspace_bytes_impl(m, n, k);
 }
 
@@ -138,7 +138,7 @@ int tq_mx_linear(const void* x_dev, int dtype, uint64_t m, uint64_t ldx, const v
         (rc = check_workspace(workspace_dev, workspace_bytes, tq_mx_linear_workspace_bytes(m, n, k))))
         return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (tq_mx_linear_in_one(m, k))
+    if (tq_mx_linear_in_one(m, n, k))
         return from_hip(tq_launch_mx_linear_few(x_dev, dtype, m, ldx, w_codes_dev, w_scales_dev, n, k, out_dev, out_dtype, ldo, st));
     char* codes = static_cast<char*>(workspace_dev);
     char* scales = codes + padded(tq_mx_code_bytes(m, k));

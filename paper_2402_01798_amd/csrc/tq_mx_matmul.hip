@@ -6,7 +6,7 @@
 namespace tq {
 namespace {
 
-constexpr uint64_t kUnits = 256;                                   // compute units
+constexpr uint64_t kUnits = 256, kLds = 160 << 10;                 // compute units, and the LDS of one in bytes
 constexpr uint64_t kSplitGroups = 16;                              // of a workgroup at least, where k is split over several
 constexpr uint64_t kSplitSaves = 40;
 
@@ -82,7 +82,7 @@ struct Tile {
     static constexpr int kRing = STAGES * kStage;
     static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
     static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
-    static_assert(BM % 64 == 0 && BN % 64 == 0 && kBytes <= 160 << 10, "requests of scales are of 64 rows");
+    static_assert(BM % 64 == 0 && BN % 64 == 0 && kBytes <= kLds, "requests of scales are of 64 rows");
 };
 
 // Waits until the requests of all but the newest `newer` stages (at most N) are there.
@@ -280,119 +280,168 @@ __global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void 
         }
 }
 
-// Few rows of A (at most 32) against 32 rows of B, 8 wavefronts over parts of k: serving, where B is read once and bounds it.  The
-// rows of A, cast here if they are not in 4-bit form yet, stay in LDS; B comes through a ring for each wavefront, whose first
-// requests are on their way while A is prepared.
-constexpr int kFewWaves = 8, kFewStages = 2, kFewStage = 32 * 128 + 256, kFewRing = kFewWaves * kFewStages * kFewStage;
-constexpr uint32_t kFewBytes = 160 << 10;                         // the LDS of a compute unit
-constexpr uint32_t kFewRowsInForm = 16, kFewRows = 32;
+// Few rows of A, FRAGS x 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds
+// it.  B comes through a ring of STAGES buffers for each wavefront, 256 of k at a time, and rows of A in 4-bit form (X < 0) with it.
+// Others, of type X, are cast here by every workgroup and stay in LDS; the rings' first requests are on their way meanwhile.
+template <int X, int FRAGS, int WAVES, int STAGES>
+struct Few {
+    static constexpr int kRowsA = X < 0 ? FRAGS * 32 : 0;          // in a buffer, before the 32 of B
+    static constexpr int kScales = (kRowsA + 32) * 128;            // then two groups' scales of 32 rows at a time
+    static constexpr int kStage = kScales + (kRowsA + 32) * 8;
+    static constexpr int kPerStage = 5 * (kRowsA + 32) / 32;       // requests: 4 of codes and one of scales for 32 rows
+    static constexpr int kRing = WAVES * STAGES * kStage;
+    static constexpr int kSums = WAVES * FRAGS * 32 * 33 * 4;
+    static_assert(kRing <= kLds && kRing >= kSums, "the sums take the rings' place");
+};
+constexpr int kFewWaves = 8, kFewStages = 2;                       // where A is cast
+using FewCast = Few<0, 1, kFewWaves, kFewStages>;
 
 __host__ __device__ constexpr uint64_t few_row_bytes(uint64_t groups) { return groups * 64 + 16; }
-__host__ __device__ constexpr uint64_t few_bytes(uint64_t m, uint64_t groups) { return kFewRing + m * (few_row_bytes(groups) + groups * 4); }
+__host__ __device__ constexpr uint64_t few_bytes(uint64_t m, uint64_t groups) { return FewCast::kRing + m * (few_row_bytes(groups) + groups * 4); }
 
 // X: the type of g.x, or -1 for rows in 4-bit form.
-template <int DTYPE, int X>
-__global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_kernel(MatmulArgs g)
+template <int DTYPE, int X, int FRAGS, int WAVES, int STAGES>
+__global__ __launch_bounds__(WAVES * 64) void mx_matmul_few_kernel(MatmulArgs g)
 {
+    using S = Few<X, FRAGS, WAVES, STAGES>;
+    static_assert(X < 0 || FRAGS == 1, "rows that are cast here");
+    constexpr int kBlocksA = S::kRowsA / 32;                       // blocks of 32 rows in a buffer, A's before B's
     extern __shared__ char lds[];
     const uint32_t tx = linear_block();
     if (tx >= g.tiles) return;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
     const uint32_t col0 = tx * 32, pairs = (g.groups + 1) / 2;
-    const uint32_t per = (pairs + kFewWaves - 1) / kFewWaves, first = wave * per, trips = first < pairs ? min(per, pairs - first) : 0;
-    char* ring = lds + wave * (kFewStages * kFewStage);
+    const uint32_t per = (pairs + WAVES - 1) / WAVES, first = wave * per, trips = first < pairs ? min(per, pairs - first) : 0;
+    char* ring = lds + wave * (STAGES * S::kStage);
     const uint32_t row_bytes = (uint32_t)few_row_bytes(g.groups);
-    char* codes = lds + kFewRing;
+    char* codes = lds + S::kRing;                                  // of rows cast here
     char* scales = codes + g.m * row_bytes;                        // [m][groups][4]
 
-    const uint8_t* from[4];
+    const uint8_t* from[4 * (kBlocksA + 1)];
     const uint32_t piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};      // of rows 8 i + lane / 8, i even and odd
+    uint32_t scale_row[kBlocksA + 1];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) from[i] = g.b + (uint64_t)min(col0 + i * 8 + (lane >> 3), g.n - 1) * g.groups * 64;
-    const uint32_t row_b = min(col0 + r, g.n - 1);
+    for (int i = 0; i < 4 * (kBlocksA + 1); ++i) {
+        const uint32_t row = i % 4 * 8 + (lane >> 3);
+        from[i] = i < 4 * kBlocksA ? g.a + (uint64_t)min(i / 4 * 32 + row, g.m - 1) * g.groups * 64
+                                   : g.b + (uint64_t)min(col0 + row, g.n - 1) * g.groups * 64;
+    }
+#pragma unroll
+    for (int i = 0; i <= kBlocksA; ++i) scale_row[i] = i < kBlocksA ? min(i * 32 + r, g.m - 1) : min(col0 + r, g.n - 1);
     auto fetch = [&](uint32_t t, uint32_t stage) {
-        char* base = ring + stage * kFewStage;
+        char* base = ring + stage * S::kStage;
         const uint32_t group = 2 * (first + t);
         const bool both = group + 1 < g.groups;                    // the second half of the last may not be there: the first again
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4 * (kBlocksA + 1); ++i) {
             const uint32_t at = both ? piece[i & 1] : piece[i & 1] & 3;
             __builtin_amdgcn_global_load_lds((global_bytes*)(from[i] + (uint64_t)group * 64 + at * 16), (lds_bytes*)(base + i * 1024), 16, 0, 0);
         }
         const uint64_t mine = both ? group + half : group;
-        __builtin_amdgcn_global_load_lds((global_bytes*)(g.sb + (mine * g.n + row_b) * 4), (lds_bytes*)(base + 4096), 4, 0, 0);
+#pragma unroll
+        for (int i = 0; i <= kBlocksA; ++i) {
+            const uint8_t* q = i < kBlocksA ? g.sa + (mine * g.m + scale_row[i]) * 4 : g.sb + (mine * g.n + scale_row[i]) * 4;
+            __builtin_amdgcn_global_load_lds((global_bytes*)q, (lds_bytes*)(base + S::kScales + i * 256), 4, 0, 0);
+        }
     };
 #pragma unroll
-    for (uint32_t t = 0; t < kFewStages; ++t)
+    for (uint32_t t = 0; t < STAGES; ++t)
         if (t < trips) fetch(t, t);
 
-    if constexpr (X < 0) {
-        for (uint32_t i = threadIdx.x; i < g.m * g.groups * 4; i += kFewWaves * 64) {
-            const uint32_t row = i / (g.groups * 4), p = i - row * (g.groups * 4);
-            *reinterpret_cast<i32x4*>(codes + row * row_bytes + p * 16) = *reinterpret_cast<const i32x4*>(g.a + (uint64_t)i * 16);
-        }
-        for (uint32_t i = threadIdx.x; i < g.m * g.groups; i += kFewWaves * 64) {
-            const uint32_t group = i / g.m, row = i - group * g.m;
-            *reinterpret_cast<int*>(scales + (row * g.groups + group) * 4) = *reinterpret_cast<const int*>(g.sa + (uint64_t)i * 4);
-        }
-    } else {
+    if constexpr (X >= 0) {
         using T = typename Element<X>::type;
-        const uint32_t octs = g.groups * 16;                       // of 8 elements in a row: four neighbouring lanes are a block
-        for (uint32_t i = threadIdx.x; i < g.m * octs; i += kFewWaves * 64) {
-            const uint32_t row = i / octs, oct = i - row * octs;
-            float v[8];
-            load8<X>(static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
+        const uint32_t octs = g.groups * 16, all = g.m * octs;     // of 8 elements in a row: four neighbouring lanes are a block
+        auto from_x = [&](uint32_t i, uint32_t& row, uint32_t& oct) {
+            row = i / octs;
+            oct = i - row * octs;
+            return static_cast<const T*>(g.x) + row * g.ldx + (uint64_t)oct * 8;
+        };
+        auto put = [&](uint32_t row, uint32_t oct, const float (&v)[8]) {
             uint32_t largest = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) largest = max(largest, magnitude_bits(v[j]));
             const uint32_t byte = mx_scale_byte<false>(quad_max(largest));
             *reinterpret_cast<uint32_t*>(codes + row * row_bytes + oct * 4) = mx_nearest(v, byte);
             if ((oct & 3) == 0) scales[row * octs / 4 + oct / 4] = (char)byte;
+        };
+        uint32_t i = threadIdx.x, row, oct;
+        if (g.k % kMxGroup == 0) {                                 // 4 requests of a thread are on their way together
+            for (; i + 3 * WAVES * 64 < all; i += 4 * WAVES * 64) {
+                Eight<X> w[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) w[u].load(from_x(i + u * WAVES * 64, row, oct));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float v[8];
+                    w[u].unpack(v);
+                    from_x(i + u * WAVES * 64, row, oct);
+                    put(row, oct, v);
+                }
+            }
         }
+        for (; i < all; i += WAVES * 64) {
+            float v[8];
+            const T* p = from_x(i, row, oct);
+            load8<X>(p, (int)min((int64_t)g.k - (int64_t)oct * 8, (int64_t)8), v);
+            put(row, oct, v);
+        }
+        __syncthreads();
     }
-    __syncthreads();
 
     const char* my_codes = codes + min(r, g.m - 1) * row_bytes;
     const char* my_scales = scales + min(r, g.m - 1) * g.groups * 4;
-    f32x16 acc = {};
+    f32x16 acc[FRAGS] = {};
     uint32_t stage = 0;
     for (uint32_t t = 0; t < trips; ++t) {
-        wait_for_stages<5, kFewStages - 1>(trips - 1 - t);
-        const char* base = ring + stage * kFewStage;
+        wait_for_stages<S::kPerStage, STAGES - 1>(trips - 1 - t);
+        const char* base = ring + stage * S::kStage;
         const uint32_t group = 2 * (first + t);
         const bool both = group + 1 < g.groups;
-        i32x4 a[4], b[4];
-        int sa[2], sb[2];
+        i32x4 a[FRAGS][4], b[4];
+        int sa[FRAGS][2], sb[2];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            b[s] = *reinterpret_cast<const i32x4*>(base + r * 128 + ((2 * s + half) ^ (r >> 1 & 7)) * 16);
-            a[s] = *reinterpret_cast<const i32x4*>(my_codes + (group + (both ? s / 2 : 0)) * 64 + (2 * (s & 1) + half) * 16);
+            const uint32_t at = r * 128 + ((2 * s + half) ^ (r >> 1 & 7)) * 16;
+            b[s] = *reinterpret_cast<const i32x4*>(base + kBlocksA * 4096 + at);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f)
+                a[f][s] = *reinterpret_cast<const i32x4*>(X < 0 ? base + f * 4096 + at
+                                                                : my_codes + (group + (both ? s / 2 : 0)) * 64 + (2 * (s & 1) + half) * 16);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            sb[h] = *reinterpret_cast<const int*>(base + 4096 + (h * 32 + r) * 4) >> (8 * half);
-            sa[h] = *reinterpret_cast<const int*>(my_scales + (group + (both ? h : 0)) * 4) >> (8 * half);
+            const char* at = base + S::kScales + (h * 32 + r) * 4;
+            sb[h] = *reinterpret_cast<const int*>(at + kBlocksA * 256) >> (8 * half);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f)
+                sa[f][h] = *reinterpret_cast<const int*>(X < 0 ? at + f * 256 : my_scales + (group + (both ? h : 0)) * 4) >> (8 * half);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
-        if (t + kFewStages < trips) fetch(t + kFewStages, stage);
-        acc = mfma32<0>(a[0], b[0], acc, sa[0], sb[0]);
-        acc = mfma32<2>(a[1], b[1], acc, sa[0], sb[0]);
+        if (t + STAGES < trips) fetch(t + STAGES, stage);
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) acc[f] = mfma32<0>(a[f][0], b[0], acc[f], sa[f][0], sb[0]);
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) acc[f] = mfma32<2>(a[f][1], b[1], acc[f], sa[f][0], sb[0]);
         if (both) {
-            acc = mfma32<0>(a[2], b[2], acc, sa[1], sb[1]);
-            acc = mfma32<2>(a[3], b[3], acc, sa[1], sb[1]);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) acc[f] = mfma32<0>(a[f][2], b[2], acc[f], sa[f][1], sb[1]);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) acc[f] = mfma32<2>(a[f][3], b[3], acc[f], sa[f][1], sb[1]);
         }
-        stage ^= 1;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
     __syncthreads();                                               // the rings are done with
     float* sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sums[(wave * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[e];
+    for (int f = 0; f < FRAGS; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[((wave * FRAGS + f) * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[f][e];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < g.m * 32; i += kFewWaves * 64) {
+    for (uint32_t i = threadIdx.x; i < g.m * 32; i += WAVES * 64) {
         const uint32_t row = i / 32, col = i & 31;
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) v += sums[(w * 32 + row) * 33 + col];
+        for (int w = 0; w < WAVES; ++w) v += sums[(w * FRAGS * 32 + row) * 33 + col];
         if (g.add && col0 + col < g.n) v += g.add[row * g.lda + col0 + col];
         store_one<DTYPE>(g, row, col0 + col, v);
     }
@@ -422,14 +471,15 @@ hipError_t launch_tile(MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DTYPE, int X>
+template <int DTYPE, int X, int FRAGS, int WAVES, int STAGES>
 hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 {
+    using S = Few<X, FRAGS, WAVES, STAGES>;
     g.tiles = (g.n + 31) / 32;
     dim3 grid;
-    if (!fold_grid(g.tiles, kFewWaves * 64, 1, grid)) return hipErrorInvalidValue;
-    const uint32_t bytes = (uint32_t)few_bytes(g.m, g.groups);
-    mx_matmul_few_kernel<DTYPE, X><<<grid, kFewWaves * 64, bytes, st>>>(g);
+    if (!fold_grid(g.tiles, WAVES * 64, 1, grid)) return hipErrorInvalidValue;
+    const uint32_t bytes = X < 0 ? (uint32_t)S::kRing : (uint32_t)few_bytes(g.m, g.groups);
+    mx_matmul_few_kernel<DTYPE, X, FRAGS, WAVES, STAGES><<<grid, WAVES * 64, bytes, st>>>(g);
     return hipGetLastError();
 }
 
@@ -450,13 +500,22 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 //   512 x 4096 x 4096   31.5   20.7     25.8    25.0   15.5   11.4   14.5
 //   256 x 4096 x 4096   30.3   19.9     25.0    24.0   14.4    9.0    8.1          64 too: the parts of k run beside each other
 //   128 x 8192 x 8192   53.8   35.0     45.9    42.5   25.7   18.8   13.2
+//   64 x 8192 x 8192                                                  12.8   11.0  4 wavefronts of 64 x 32
+//   64 x 4096 x 4096                                                   8.4    7.1
+//   64 x 32000 x 4096                                          17.1          27.9  1000 tiles, each with all of A to read
+//   32 x 8192 x 8192                                                  12.0    8.9  8 wavefronts of 32 x 32
+//   32 x 4096 x 4096                                                   8.1    4.6
+//   32 x 32000 x 4096                                          16.5          18.7  (4 wavefronts, two workgroups on a unit, 16.0)
+//   1 x 32000 x 4096                                                         16.9  (14.1)
+//   32 x 1000 x 16384                                                 10.2    8.4  k over workgroups against one
+//   32 x 300 x 32768                                                   9.6   13.0
 //   784 x 1000 x 64      6.1    4.4      5.2     5.2    3.7    3.2    4.7          nothing to part
 //   1 x 8192 x 8192     51.7   34.5     43.6    41.5   24.2   17.6   11.3    7.3
 // Enough tiles of 128 for every compute unit: the shape whose rounds take least.  Where the sides leave little over this is 256.
 // Few tiles and a long k: k is split over workgroups too, where at least 40 groups (5 steps of a workgroup, the second launch's
 // price) are saved.  Not split / split, us: 64 x 64 x 8192 9.8 / 7.8, x 32768 28 / 9.5, x 131072 119 / 12, 256 x 256 x 32768 29 / 12,
 // 700 x 700 x 32768 35 / 26; with fewer saved it loses (500 x 500 x 4096 7.3 / 8.6).
-enum Shape { kFew, k256, k256x128, k128x320, k192, k128, k64, k64InParts };
+enum Shape { kFew, kFewOfMany, kFew64, k256, k256x128, k128x320, k192, k128, k64, k64InParts };
 
 // A tile's sides, and the time in ns that 128 elements of k took while 1, 2, .. of them, as many as fit, were at work on every
 // compute unit.
@@ -476,9 +535,18 @@ uint64_t pace(const Pace& p, uint64_t m, uint64_t n)
     return each / fit * p.ns[fit - 1] + (each % fit ? p.ns[each % fit - 1] : 0);
 }
 
+// Over how many workgroups k is split beside the few tiles of 64.
+uint32_t splits_of_64(uint64_t m, uint64_t n, uint64_t groups)
+{
+    const uint64_t most = kUnits / tiles_of(m, n, 64, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
+    return s > 1 && groups - groups / s >= kSplitSaves ? (uint32_t)s : 1;
+}
+
 Shape shape(uint64_t m, uint64_t n, uint64_t groups)
 {
-    if (m <= kFewRowsInForm && few_bytes(m, groups) <= kFewBytes) return kFew;
+    const bool split = splits_of_64(m, n, groups) > 1;
+    if (m <= 32 && (!split || groups <= 128)) return n <= kUnits * 32 ? kFew : kFewOfMany;
+    if (m <= 64 && !split && n <= kUnits * 32) return kFew64;
     if (tiles_of(m, n, 128, 128) < kUnits) return tiles_of(m, n, 64, 64) > kUnits || groups < 4 ? k64 : k64InParts;
     const Pace* best = kPaces;
     for (const Pace& p : kPaces)
@@ -486,19 +554,16 @@ Shape shape(uint64_t m, uint64_t n, uint64_t groups)
     return best->shape;
 }
 
-uint32_t splits(uint64_t m, uint64_t n, uint64_t groups)
-{
-    if (shape(m, n, groups) != k64InParts) return 1;
-    const uint64_t most = kUnits / tiles_of(m, n, 64, 64), wanted = groups / kSplitGroups, s = wanted < most ? wanted : most;
-    return s > 1 && groups - groups / s >= kSplitSaves ? (uint32_t)s : 1;
-}
+uint32_t splits(uint64_t m, uint64_t n, uint64_t groups) { return shape(m, n, groups) == k64InParts ? splits_of_64(m, n, groups) : 1; }
 
 template <int DTYPE>
 hipError_t launch_matmul(MatmulArgs& g, hipStream_t st)
 {
     g.splits = 1;
     switch (shape(g.m, g.n, g.groups)) {
-        case kFew: return launch_few<DTYPE, -1>(g, st);
+        case kFew: return launch_few<DTYPE, -1, 1, 8, 2>(g, st);
+        case kFewOfMany: return launch_few<DTYPE, -1, 1, 4, 2>(g, st);
+        case kFew64: return launch_few<DTYPE, -1, 2, 4, 3>(g, st);
         // 8 wavefronts of 128 x 64, 256 of k a trip (whole lines of 128 bytes): 8192^3 289 us, by 16 wavefronts of 64 x 64 300, and with
         // 128 of k a trip and three buffers 310.  Tiles of which two are to fit have buffers of 128 of k.
         case k256: return launch_tile<DTYPE, 256, 256, 2, 4, 1, 2, 2>(g, st);
@@ -549,7 +614,14 @@ hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, con
     return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
 }
 
-bool tq_mx_linear_in_one(uint64_t m, uint64_t k) { return m <= tq::kFewRows && tq::few_bytes(m, (k + tq::kMxGroup - 1) / tq::kMxGroup) <= tq::kFewBytes; }
+// Rows cast by every workgroup of the product, or once in a launch before it.  Linear layers, in us (one launch / two): 8192 x 8192
+// 1 token 9.4 / 11.0, 4 10.8 / 11.2, 6 12.3 / 11.3, 16 18.9 / 11.5; 4096 x 4096 1 4.7 / 6.0, 8 6.6 / 6.5, 16 9.1 / 6.6; 2048 deep and
+// 8192 wide 16 6.6 / 6.5; 4096 deep and 32000 wide, four rounds of workgroups, 1 14.5 / 16.6, 4 16.5 / 16.9, 8 26.8 / 17.0.
+bool tq_mx_linear_in_one(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint64_t groups = (k + tq::kMxGroup - 1) / tq::kMxGroup, rounds = (n + 32 * tq::kUnits - 1) / (32 * tq::kUnits);
+    return m <= 16 && (m - 1) * groups * rounds <= 256 && tq::few_bytes(m, groups) <= tq::kLds;
+}
 
 hipError_t tq_launch_mx_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const void* sw, uint64_t n,
                                    uint64_t k, void* out, int dtype, uint64_t ldo, hipStream_t st)
@@ -568,8 +640,8 @@ hipError_t tq_launch_mx_linear_few(const void* x, int x_dtype, uint64_t m, uint6
     g.groups = (uint32_t)((k + kMxGroup - 1) / kMxGroup);
     auto as = [&](auto D) {
         constexpr int T = decltype(D)::value;
-        if (x_dtype == TQ_F32) return launch_few<T, TQ_F32>(g, st);
-        return x_dtype == TQ_BF16 ? launch_few<T, TQ_BF16>(g, st) : launch_few<T, TQ_F16>(g, st);
+        if (x_dtype == TQ_F32) return launch_few<T, TQ_F32, 1, kFewWaves, kFewStages>(g, st);
+        return x_dtype == TQ_BF16 ? launch_few<T, TQ_BF16, 1, kFewWaves, kFewStages>(g, st) : launch_few<T, TQ_F16, 1, kFewWaves, kFewStages>(g, st);
     };
     if (dtype == TQ_F32) return as(std::integral_constant<int, TQ_F32>{});
     return dtype == TQ_BF16 ? as(std::integral_constant<int, TQ_BF16>{}) : as(std::integral_constant<int, TQ_F16>{});

@@ -71,9 +71,10 @@ def test_product_over_a_long_axis(m, n, k, out):
     assert e.value.code == B.EINVAL
 
 
-@pytest.mark.parametrize("m,k,in_one", [(1, 177_280, True), (1, 177_281, False), (16, 11_000, True), (32, 5_000, True), (32, 6_000, False),
+@pytest.mark.parametrize("m,k,in_one", [(1, 177_280, True), (1, 177_281, False), (2, 32_768, True), (2, 32_769, False), (16, 2_176, True),
+                                        (16, 2_177, False), (16, 11_000, False), (17, 100, False), (32, 5_000, False), (32, 6_000, False),
                                         (33, 100, False)])
-def test_linear_on_both_sides_of_what_lds_holds(m, k, in_one):
+def test_linear_on_both_sides_of_what_is_cast_in_the_product(m, k, in_one):
     n = 70
     w, vw = random_form(n, k, 9, 118, 122)
     nbytes = B.mx_linear_workspace_bytes(m, n, k)
@@ -204,3 +205,41 @@ def test_product_in_tiles_of_every_shape(m, n, k, out, offset):
     bound = (k + 1) * 2.0 ** -23 * size + 1.001 * LC.HALF_ULP[out] * ref.abs() + (2.0 ** -25 if out == "f16" else 0.0)
     assert ((o.double() - ref).abs() <= bound).all()
     assert (wide[:, :offset] == 7).all() and (wide[:, offset + n:] == 7).all()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(17, 33, 129), (32, 257, 1000), (3, 40, 16384), (31, 8200, 260), (5, 8300, 130), (1, 16390, 64), (33, 70, 129),
+                                   (40, 100, 2000), (64, 33, 1), (63, 8190, 385), (64, 8200, 300), (20, 40, 30000)])
+def test_product_of_few_rows(m, n, k, out):
+    (a, va), (b, vb) = random_form(m, k, 21, 118, 122), random_form(n, k, 22, 118, 122)
+    va, vb = on_device(va), on_device(vb)
+    ref, size = va @ vb.t().contiguous(), va.abs() @ vb.abs().t().contiguous()
+    add = torch.randn(m, n + 3, generator=torch.Generator(device="cuda").manual_seed(23), device="cuda")[:, 1:n + 1]
+    ws = scratch(B.mx_matmul_workspace_bytes(m, n, k))
+    for extra in (None, add):
+        o = torch.full((m + 2, n + 1), 7.0, dtype=LC.TYPES[out], device="cuda")
+        B.tq_mx_matmul(a, b, o[1:m + 1, :n], ws, add=extra)
+        want = ref if extra is None else ref + extra.double()
+        bound = (k + 1) * 2.0 ** -23 * (size if extra is None else size + extra.double().abs()) + 1.001 * LC.HALF_ULP[out] * want.abs() \
+            + (2.0 ** -25 if out == "f16" else 0.0)
+        assert ((o[1:m + 1, :n].double() - want).abs() <= bound).all()
+        assert (o[:, n] == 7).all() and (o[0] == 7).all() and (o[m + 1] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(1, 50, 8192), (2, 33, 4096), (5, 130, 8192), (6, 130, 8192), (16, 64, 2048), (16, 70, 2176), (9, 8200, 384),
+                                   (16, 8200, 2048), (17, 31, 1024), (16, 40, 1990), (33, 65, 640)])
+def test_linear_of_few_tokens_is_the_product_of_the_cast(m, n, k, dtype):
+    """Cast inside the product or before it: the same codes, so only the order of the sums is open."""
+    w, vw = random_form(n, k, 31, 118, 122)
+    wide = torch.randn(m, k + 5, generator=torch.Generator(device="cuda").manual_seed(32), device="cuda").to(LC.TYPES[dtype])
+    for x in (wide[:, :k].contiguous(), wide[:, 3:k + 3]):
+        out = torch.full((m, n + 1), 7.0, device="cuda")
+        B.tq_mx_linear(x, w, out[:, :n], scratch(B.mx_linear_workspace_bytes(m, n, k)))
+        form = B.alloc_mx(m, k)
+        B.tq_mx_quantize(x, form)
+        vx = on_device(LC.mx_values(form.codes.cpu().numpy(), form.scales.cpu().numpy(), k))
+        vw_ = on_device(vw)
+        ref, size = vx @ vw_.t().contiguous(), vx.abs() @ vw_.abs().t().contiguous()
+        assert ((out[:, :n].double() - ref).abs() <= (k + 1) * 2.0 ** -23 * size).all()
+        assert (out[:, n] == 7).all()
