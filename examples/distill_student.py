@@ -19,7 +19,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2402_01798_amd import binding as tq                                        # noqa: E402
 
 WORKERS, TOKENS, WIDTH, HIDDEN, VOCAB, TOP, BITS = 4, 512, 256, 512, 1000, 16, 4
-TAU, RATE, MOMENTUM, SEED = 2.0, 0.2, 0.9, 7
+TAU, RATE, MOMENTUM, SEED = 2.0, 0.1, 0.9, 7
 
 
 class Matrix:
