@@ -161,6 +161,32 @@ struct Softmax {
 // The compiler would keep the values that it has unpacked for the next pass over them, in twice the registers.
 __device__ __forceinline__ void keep_packed(u32x4& w) { asm volatile("" : "+v"(w)); }
 
+__host__ __device__ constexpr uint32_t whole_fours(uint32_t n) { return (n + 3) & ~3u; }
+
+// Whether another entry has entry i's id, whether one before it does, and the sum of t over those behind it, in order.  Four entries
+// at a time and no branch between them: one by one, a row of 512 entries with ids that occur twice took 150 us, so 77.
+struct Alike {
+    bool any = false, before = false;
+    float sum = 0.0f;
+};
+__device__ __forceinline__ Alike alike(const int* id, const float* t, uint32_t top, uint32_t i)
+{
+    const int mine = id[i];
+    Alike r;
+#pragma unroll 4
+    for (uint32_t j = 0; j < top; j += 4) {
+        const u32x4 ids = *reinterpret_cast<const u32x4*>(id + j), ts = *reinterpret_cast<const u32x4*>(t + j);
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const bool same = (int)ids[u] == mine && j + u < top && j + u != i;
+            r.any |= same;
+            r.before |= same && j + u < i;
+            r.sum += same ? __uint_as_float(ts[u]) : 0.0f;
+        }
+    }
+    return r;
+}
+
 // One workgroup a row.  VECTORS > 0: the row stays in the registers, VECTORS x 16 bytes a thread, so memory is read once; 0: it is
 // read again for the gradient.  WHOLE: dz lies to its 16-byte lines as z does.
 template <int DTYPE, int MODE, int THREADS, int VECTORS, bool WHOLE>
@@ -172,10 +198,10 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
     constexpr int WAVES = THREADS / 64;
     constexpr uint32_t IN = R::kIn;
     __shared__ float parts[3][WAVES][2];
-    extern __shared__ char entries[];                              // the teacher's: id, logit and then probability, z
+    extern __shared__ __attribute__((aligned(16))) char entries[]; // the teacher's: id, logit and then probability, z
     int* id = reinterpret_cast<int*>(entries);
-    float* t = reinterpret_cast<float*>(id + a.top);
-    float* at_id = t + a.top;
+    float* t = reinterpret_cast<float*>(id + whole_fours(a.top));
+    float* at_id = t + whole_fours(a.top);
     __shared__ uint32_t seen[MODE == kForward ? 1 : kSeenBits / 32];
     const uint32_t block = linear_block(), tid = threadIdx.x, row = MODE == kBackward ? block / a.pieces : block;
     if (row >= a.rows) return;
@@ -219,7 +245,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
         __syncthreads();
         for (uint32_t i = tid; i < a.top; i += THREADS)
             if (id[i] >= 0 && (atomicOr(&seen[(id[i] & (kSeenBits - 1)) / 32], 1u << (id[i] & 31)) >> (id[i] & 31) & 1u))
-                for (uint32_t j = 0; j < a.top; ++j) twice |= j != i && id[j] == id[i];
+                twice |= alike(id, t, a.top, i).any;
     }
 
     float top = z_loose, log_total = 0.0f;                         // the row's largest logit, ln sum exp((z - top) / tau)
@@ -325,13 +351,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs a)
             if (id[i] >= 0 && lies.within(id[i], k_first, k_end)) {
                 float p = t[i];
                 if (count != 0.0f) {                               // an id's first entry takes the probabilities of all
-                    bool first = true;
-                    for (uint32_t j = 0; j < a.top; ++j)
-                        if (j != i && id[j] == id[i]) {
-                            first &= j > i;
-                            p += t[j];
-                        }
-                    if (!first) continue;
+                    const Alike others = alike(id, t, a.top, i);
+                    if (others.before) continue;
+                    p += others.sum;
                 }
                 dz[id[i]] = E::store(scale * power(at_id[i]) - g * p);
             }
@@ -343,7 +365,7 @@ hipError_t launch(const DistillArgs& a, hipStream_t st)
 {
     dim3 grid;
     if (!fold_grid((uint64_t)a.rows * a.pieces, THREADS, 1, grid)) return hipErrorInvalidValue;
-    const size_t entries = 12 * (size_t)a.top;
+    const size_t entries = 12 * (size_t)whole_fours(a.top);
     if constexpr (MODE != kForward) {
         const uint64_t size = DTYPE == TQ_F32 ? 4 : 2;
         if (((reinterpret_cast<uintptr_t>(a.dz) - reinterpret_cast<uintptr_t>(a.z)) | (a.lddz - a.ldz) * size) & 15u) {

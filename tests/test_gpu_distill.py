@@ -179,3 +179,13 @@ def test_repeats_bit_for_bit():
         B.tq_distill(z, ids, t, grad, loss, dz, 2.0)
         out.append((loss, dz))
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+@pytest.mark.parametrize("top", [2, 3, 5, 37, 258, 1023])
+def test_ids_that_occur_twice_among_any_number(top):
+    z, ids, t, grad = make(7, 2048, top, "f32", 9)
+    ids[:, top - 1] = ids[:, 0]                             # the first and the last
+    ids[1] = 2047                                           # all of them
+    ids[2, ::2] = int(ids[2, 0])
+    ids[3, 1:] = -1                                         # those that are left out are not alike
+    check(z, ids, t, grad, 2.0, "f32")
