@@ -62,8 +62,8 @@ int tq_mx_dequantize(const void* codes_dev, const void* scales_dev, uint64_t row
  * layer's three products want: y = x W^T, dx = dy (W^T)^T, dW = dy^T (x^T)^T, the transposes from tq_mx_quantize.
  * Products are exact, sums are binary32, one rounding to out's type at the end.  The same call on the same device gives
  * the same bits every time.
- *   add_dev        NULL, or [m][lda] floats that are added before the rounding; may be out_dev (gradients that are
- *                  accumulated over batches), with the same row length then
+ *   add_dev        NULL, or [m][lda] floats, each added once, to the finished sum in binary32, before the rounding to out's
+ *                  type; may be out_dev (gradients that are accumulated over batches), with the same row length then
  *   out_dev        [m][ldo] of TQ_F32, TQ_BF16 or TQ_F16; ldo >= n elements from row to row
  *   workspace_dev  at least tq_mx_matmul_workspace_bytes(m, n, k) bytes, 16-byte aligned (NULL if that is 0): partial
  *                  sums where k is split; contents undefined afterwards; calls that share it have to be ordered

@@ -82,6 +82,13 @@ struct Tile {
     static constexpr int kRing = STAGES * kStage;
     static constexpr int kSums = KS > 1 ? BM * (BN + 1) * 4 : 0;   // a part's outputs, a row longer against bank conflicts
     static constexpr int kBytes = KS * (kRing > kSums ? kRing : kSums);
+    static constexpr int kOnUnit = kThreads > 512 ? 1 : (int)(kLds / kBytes);  // workgroups on a compute unit
+    static constexpr int kOnSimd = (kOnUnit * kThreads + 255) / 256;           // wavefronts on a SIMD, which share 512 registers
+    static constexpr int kFrags = kFragsM * kFragsN;
+    // registers that sums (16 a fragment), operands (8 a row and column of them) and some 38 others leave, and the fragments whose
+    // addends they hold
+    static constexpr int kRoom = (512 / kOnSimd < 256 ? 512 / kOnSimd : 256) - 16 * kFrags - 8 * (kFragsM + kFragsN) - 38;
+    static constexpr int kEarly = kRoom < 16 ? 0 : kRoom / 16 < kFrags ? kRoom / 16 : kFrags, kAhead = kEarly ? kEarly : 1;
     static_assert(BM % 64 == 0 && BN % 64 == 0 && kBytes <= kLds, "requests of scales are of 64 rows");
 };
 
@@ -95,10 +102,9 @@ __device__ __forceinline__ void wait_for_stages(uint32_t newer)
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER * N) : "memory");
 }
 
-// Two workgroups of 4 wavefronts at least on a compute unit: given all its registers the compiler keeps sums in those that only the
-// matrix instructions reach, and moves the addend there before anything else is requested.
+// Registers for as many wavefronts on a SIMD as LDS has room for workgroups on the compute unit.
 template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
-__global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void mx_matmul_tile_kernel(MatmulArgs g)
+__global__ __launch_bounds__(WM * WN * KS * 64, (Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>::kOnSimd)) void mx_matmul_tile_kernel(MatmulArgs g)
 {
     using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
     extern __shared__ char lds[];
@@ -162,30 +168,39 @@ __global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void 
     // whole 16-byte stores of 16-bit elements (bf16 2056 x 1000 x 1999 9.4 -> 8.7 us); else of one column 4 rows of every 8, 32 lanes
     // with 128 bytes of fp32 in a row (fp32 with an addend, the same size, 13.2 -> 10.0 us).
     constexpr bool kAlongRow = KS == 1 && DTYPE != TQ_F32;
-    if (g.add && part == 0 && split == 0) {                        // requested first, so that it is there when the sums begin
-        const bool whole = col0 + BN <= g.n;                       // no test between two requests
+    // The addend comes after the sums: they would be rounded to its bits at every step, and gradients that are accumulated over batches
+    // are far larger than what one batch adds.  Fragment f's 16, as they are stored.  The first kEarly fragments' are requested before
+    // the sums begin, one more when one is used; without registers for that each when it is wanted, while other workgroups work.
+    // In the sums from the start / after them, us: 2056 x 1000 x 1999 fp32 10.1 / 10.1, 4096 x 4096 x 512 26.2 / 26.4, 8192 x 8192 x 8192
+    // 370 / 366, as bf16 352 / 363, 1037 x 8192 x 4096 bf16 45 / 37.
+    auto addends = [&](int f, uint32_t me, float (&v)[2][8]) {
+        const uint32_t row = row0 + (wm * S::kFragsM + f / S::kFragsN) * 32, col = col0 + (wn * S::kFragsN + f % S::kFragsN) * 32;
+        if constexpr (kAlongRow) {
+            const float* from_row = g.add + min(row + (me & 31), g.m - 1) * g.lda;
 #pragma unroll
-        for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::kFragsN; ++j) {
-                const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
-                if (kAlongRow && whole) {
-                    const float* from_row = g.add + min(row + r, g.m - 1) * g.lda + col + half * 4;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float v[4];
-                        __builtin_memcpy(v, from_row + q * 8, 16);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][q * 4 + e] = v[e];
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t at = (e / 4) * 8 + half * 4 + e % 4;
-                        acc[i][j][e] = g.add[min(row + (kAlongRow ? r : at), g.m - 1) * g.lda + min(col + (kAlongRow ? at : r), g.n - 1)];
-                    }
-                }
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t at = col + q * 16 + (me >> 5) * 8;
+                load8<TQ_F32>(from_row + at, (int)min((int64_t)g.n - (int64_t)at, (int64_t)8), v[q]);
             }
+        } else {
+            const float* from_col = g.add + min(col + (me & 31), g.n - 1);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e / 8][e % 8] = from_col[min(row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, g.m - 1) * g.lda];
+        }
+    };
+    constexpr int kEach = KS > 1 ? BM * BN / S::kThreads : 1;      // outputs of a thread where the parts are joined
+    float extra[S::kAhead][2][8] = {}, extra_of[kEach] = {};
+    if constexpr (KS == 1) {
+        if (g.add && S::kEarly) {
+#pragma unroll
+            for (int f = 0; f < S::kAhead; ++f) addends(f, lane, extra[f]);
+        }
+    } else if (g.add && g.splits == 1) {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const uint32_t at = threadIdx.x + u * S::kThreads;
+            extra_of[u] = g.add[min(row0 + at / BN, g.m - 1) * g.lda + min(col0 + at % BN, g.n - 1)];
+        }
     }
 #pragma unroll
     for (uint32_t t = 0; t < STAGES - 1; ++t)
@@ -241,43 +256,65 @@ __global__ __launch_bounds__(WM * WN * KS * 64, WM * WN * KS == 4 ? 2 : 1) void 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sums[at + (i * 32 + (e / 4) * 8 + e % 4) * (BN + 1) + j * 32] = acc[i][j][e];
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < BM * BN; i += S::kThreads) {
-            const uint32_t row = i / BN, col = i % BN;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const uint32_t i = threadIdx.x + u * S::kThreads, row = i / BN, col = i % BN;
             float v = 0.0f;
 #pragma unroll
             for (int q = 0; q < KS; ++q) v += sums[(q * BM + row) * (BN + 1) + col];
+            if (g.add) v += extra_of[u];
             if (g.splits == 1) store_one<DTYPE>(g, row0 + row, col0 + col, v);
             else if (row0 + row < g.m && col0 + col < g.n) g.partial[((uint64_t)split * g.m + row0 + row) * g.n + col0 + col] = v;
         }
         return;
     }
-    uint32_t me = threadIdx.x & 63;
-    asm volatile("" : "+v"(me));                                   // places in the output are found here, not kept through the loop
+    auto store = [&](auto ADD) {
+        uint32_t me = threadIdx.x & 63;
+        asm volatile("" : "+v"(me));                               // places in the output are found here, not kept through the loop
 #pragma unroll
-    for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::kFragsN; ++j) {
+        for (int f = 0; f < S::kFrags; ++f) {
+            const int i = f / S::kFragsN, j = f % S::kFragsN;
             const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
-            if constexpr (kAlongRow) {                             // 4 columns changed for 4 with the other half make 8 in a row
+            if constexpr (decltype(ADD)::value && !S::kEarly) addends(f, me, extra[0]);
+            float v[2][8];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float v[8];
+            for (int q = 0; q < 2; ++q)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < (kAlongRow ? 4 : 8); ++e) {
+                    if constexpr (kAlongRow) {                     // 4 columns changed for 4 with the other half make 8 in a row
                         const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 8 + e]),
                                                                         __float_as_uint(acc[i][j][q * 8 + 4 + e]), false, false);
-                        v[e] = __uint_as_float(w[0]);
-                        v[4 + e] = __uint_as_float(w[1]);
+                        v[q][e] = __uint_as_float(w[0]);
+                        v[q][4 + e] = __uint_as_float(w[1]);
+                    } else {
+                        v[q][e] = acc[i][j][q * 8 + e];
                     }
+                }
+            if constexpr (decltype(ADD)::value) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    v[e / 8][e % 8] += extra[f % S::kAhead][e / 8][e % 8];
+                    asm volatile("" : "+v"(v[e / 8][e % 8]));      // here: beside its store it would wait for the stores before it
+                }
+                if (S::kEarly && f + S::kAhead < S::kFrags) addends(f + S::kAhead, me, extra[f % S::kAhead]);
+                asm volatile("" : "+v"(me));                       // nor from one fragment to the next, where addends wait as well
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (kAlongRow) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
                     const uint32_t to_row = row + (me & 31), to_col = col + q * 16 + (me >> 5) * 8;
                     if (to_row < g.m && to_col < g.n)
-                        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v);
+                        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v[q]);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), acc[i][j][e]);
+                for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), v[e / 8][e % 8]);
             }
         }
+    };
+    if (g.add) store(std::true_type{});
+    else store(std::false_type{});
 }
 
 // Few rows of A, FRAGS x 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds
@@ -456,7 +493,9 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MatmulArgs g)
     float v = g.partial[at];
 #pragma unroll 8
     for (uint32_t s = 1; s < g.splits; ++s) v += g.partial[s * size + at];
-    store_one<DTYPE>(g, (uint32_t)(at / g.n), (uint32_t)(at % g.n), v);
+    const uint32_t row = (uint32_t)(at / g.n), col = (uint32_t)(at % g.n);
+    if (g.add) v += g.add[row * g.lda + col];
+    store_one<DTYPE>(g, row, col, v);
 }
 
 template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>

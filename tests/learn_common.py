@@ -104,3 +104,17 @@ def distill(z, ids, t, tau, grad=None):
                 np.add.at(teacher, place, p)
                 dz[i] = np.nan if np.isnan(p).any() else tau * grad[i] * (q - teacher)
     return loss, stats, dz, all_q
+
+
+def small_form(rows, cols, seed):
+    """(codes, scales, values) of a random matrix whose products are exact in 32 bits in any order: magnitudes up to 2 and scales of 1
+    and 2, so that a product of two elements is a multiple of 1/4 and at most 16, and 2^18 of them stay within 2^24 quarters."""
+    assert cols <= 2 ** 18
+    rng = np.random.default_rng(seed)
+    groups = -(-cols // 128)
+    nibbles = rng.integers(0, 5, (rows, groups * 128)) + 8 * rng.integers(0, 2, (rows, groups * 128))
+    nibbles[:, cols:] = 0
+    scales = rng.integers(127, 129, (groups, rows, 4)).astype(np.uint8)
+    scales[np.broadcast_to((np.arange(groups * 4).reshape(groups, 1, 4) * 32 >= cols), scales.shape)] = 0
+    codes = (nibbles[:, 0::2] | nibbles[:, 1::2] << 4).astype(np.uint8)
+    return codes, scales, mx_values(codes, scales, cols)
