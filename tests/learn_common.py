@@ -118,3 +118,16 @@ def small_form(rows, cols, seed):
     scales[np.broadcast_to((np.arange(groups * 4).reshape(groups, 1, 4) * 32 >= cols), scales.shape)] = 0
     codes = (nibbles[:, 0::2] | nibbles[:, 1::2] << 4).astype(np.uint8)
     return codes, scales, mx_values(codes, scales, cols)
+
+
+# Products over a long axis of matrices made by small_form, and linear layers of tokens made by small_tokens.
+LONG_PRODUCTS = [(64, 64, 8192), (70, 130, 8100), (17, 33, 20_001), (300, 500, 16_384), (1, 40, 200_000), (129, 65, 65_665)]
+LONG_LINEARS = [(1, 70, 177_280), (1, 70, 177_281), (2, 70, 32_768), (2, 70, 32_769), (5, 70, 8_192), (16, 70, 2_176), (16, 70, 2_177),
+                (16, 70, 11_000), (32, 70, 5_000), (33, 70, 20_000)]
+
+
+def small_tokens(rows, cols, seed):
+    """Multiples of 1/2 up to 2, which 4-bit form holds whatever the largest of their block is; the last column is not 0."""
+    x = np.random.default_rng(seed).integers(-4, 5, (rows, cols)) / 2.0
+    x[:, -1] = 1.5
+    return x

@@ -37,3 +37,31 @@ def test_the_addend_is_added_once(m, n, k, out):
         place = add.contiguous()
         B.tq_mx_matmul(a, b, place, ws, add=place)
         assert torch.equal(place, want)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", LC.LONG_PRODUCTS)
+def test_product_over_a_long_axis(m, n, k, out):
+    """k over workgroups and a second launch that joins them, whatever the workspace held: no part is left out or comes twice."""
+    (a, va), (b, vb) = small(m, k, 1), small(n, k, 2)
+    product = (va @ vb.t().contiguous()).float()
+    nbytes = B.mx_matmul_workspace_bytes(m, n, k)
+    assert nbytes > 0
+    add = torch.randn(m, n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    for extra in (None, add):
+        want = (product if extra is None else product + extra).to(LC.TYPES[out])
+        for fill in (0x00, 0xFF):                           # 0xFF: NaN
+            ws = torch.full((nbytes,), fill, dtype=torch.uint8, device="cuda")
+            got = B.tq_mx_matmul(a, b, torch.full((m, n + 2), 5.0, dtype=LC.TYPES[out], device="cuda")[:, 1:n + 1], ws, extra)
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", LC.LONG_LINEARS)
+def test_linear_over_a_long_axis(m, n, k, dtype):
+    """On both sides of what is cast in the product, up to all that LDS holds."""
+    x = torch.from_numpy(LC.small_tokens(m, k, 1)).to(LC.TYPES[dtype]).cuda()
+    w, vw = small(n, k, 2)
+    want = (x.double() @ vw.t().contiguous()).float()
+    got = B.tq_mx_linear(x, w, torch.empty(m, n, device="cuda"), scratch(B.mx_linear_workspace_bytes(m, n, k)))
+    assert torch.equal(got, want)
