@@ -131,3 +131,60 @@ def small_tokens(rows, cols, seed):
     x = np.random.default_rng(seed).integers(-4, 5, (rows, cols)) / 2.0
     x[:, -1] = 1.5
     return x
+
+
+def draws_of_all(rows, cols, seed, worker, step, first_row=0, first_col=0):
+    """draws(), all elements at a time, of a part of a matrix."""
+    assert first_col % 8 == 0
+    u = np.uint64
+    mask = u(0xFFFFFFFF)
+    c0, c1 = np.meshgrid(np.arange(-(-cols // 8), dtype=np.uint64) + u(first_col // 8), np.arange(rows, dtype=np.uint64) + u(first_row))
+    c2, c3 = np.full_like(c0, worker), np.full_like(c0, step)
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF
+    for _ in range(10):
+        p0, p1 = c0 * u(0xD2511F53), c2 * u(0xCD9E8D57)
+        c0, c1, c2, c3 = p1 >> u(32) ^ c1 ^ u(k0), p1 & mask, p0 >> u(32) ^ c3 ^ u(k1), p0 & mask
+        k0, k1 = k0 + 0x9E3779B9 & 0xFFFFFFFF, k1 + 0xBB67AE85 & 0xFFFFFFFF
+    low, high = u(0xFFFF), u(16)
+    words = np.stack([v for c in (c0, c1, c2, c3) for v in (c & low, c >> high)], axis=2)
+    return words.reshape(rows, -1)[:, :cols].astype(np.int64)
+
+
+def mx_form_of_all(x, r=None):
+    """mx_form(), all blocks at a time."""
+    rows, cols = x.shape
+    groups = -(-cols // 128)
+    fill = lambda v: np.pad(v, ((0, 0), (0, groups * 128 - cols))).reshape(rows, groups * 4, 32)
+    v, there = fill(x), np.arange(groups * 4) * 32 < cols
+    a = np.abs(v)
+    whole = np.isfinite(a).all(axis=2)
+    largest = np.where(whole, a.max(axis=2), 0.0)
+    mantissa, e = np.frexp(largest)
+    byte = np.where(largest > 0, np.maximum(e - 3 + ((mantissa > 0.75) if r is not None else 0) + 127, 0), 0)
+    t = np.where(whole[:, :, None], a, 0.0) * np.exp2(127.0 - byte)[:, :, None]
+    low = np.searchsorted(GRID, np.minimum(t, 6.0), side="right") - 1
+    below, above = GRID[low], GRID[np.minimum(low + 1, 7)]
+    share = np.where(low < 7, (np.minimum(t, 6.0) - below) / np.where(low < 7, above - below, 1.0), 0.0)
+    if r is None:
+        up = (share > 0.5) | ((share == 0.5) & (low % 2 == 1))
+    else:
+        up = np.floor(share * 65536).astype(np.int64) + fill(r) >= 65536
+    code = np.where(whole[:, :, None], low + (up & (low < 7)) + 8 * np.signbit(v), 0).astype(np.uint8).reshape(rows, -1)
+    code[:, cols:] = 0
+    scales = np.where(there, np.where(whole, byte, 255), 0).astype(np.uint8).reshape(rows, groups, 4).transpose(1, 0, 2)
+    return code[:, 0::2] | code[:, 1::2] << 4, np.ascontiguousarray(scales)
+
+
+def hard_matrix(rows, cols, dtype, seed):
+    """Heavy-tailed values with both zeros, ties of the grid, subnormal numbers, the largest finite ones, infinities and NaN."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * np.exp(1.5 * rng.standard_normal((rows, cols))) * 0.03
+    pick = lambda share: rng.random((rows, cols)) < share
+    x[pick(0.05)] = 0.0
+    x[pick(0.02)] = -0.0
+    x[::3] = np.where(pick(0.3)[::3], rng.integers(-28, 29, x[::3].shape) / 4.0, x[::3])
+    x[1::5] *= 2.0 ** (-12 if dtype == "f16" else -128)
+    x[2::7, ::2] = torch.finfo(TYPES[dtype]).max
+    x[pick(0.002)] = np.nan
+    x[pick(0.002)] = -np.inf
+    return torch.from_numpy(x).to(TYPES[dtype])

@@ -34,3 +34,16 @@ def test_small_tokens_are_exact_in_4_bits():
     x[1, :32] = 0.5
     codes, scales = LC.mx_form(x)
     assert (LC.mx_values(codes, scales, 500) == x).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (7, 31), (5, 128), (9, 300), (40, 136), (21, 1000)])
+def test_all_blocks_at_a_time_is_block_by_block(rows, cols):
+    key = 2 ** 40 + 7, 3, 2 ** 31 + 5
+    x = LC.hard_matrix(rows, cols, "f32", rows).double().numpy()
+    r = LC.draws(rows, cols, *key)
+    assert (LC.draws_of_all(rows, cols, *key) == r).all()
+    if rows > 4 and cols > 40:
+        assert (LC.draws_of_all(rows - 3, cols - 16, *key, first_row=3, first_col=16) == r[3:, 16:]).all()
+    for d in (None, r):
+        for one, all_of_them in zip(LC.mx_form(x, d), LC.mx_form_of_all(x, d)):
+            assert one.shape == all_of_them.shape and (one == all_of_them).all()
