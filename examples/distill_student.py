@@ -23,13 +23,15 @@ TAU, RATE, MOMENTUM, SEED = 2.0, 0.1, 0.9, 7
 
 
 class Matrix:
-    """A matrix of one shape, in both 4-bit forms."""
+    """A matrix of one shape, in both 4-bit forms.  What is rounded stochastically has a seed of its own: casts and payloads of one
+    (seed, worker, step) would draw the same numbers."""
 
-    def __init__(self, rows, cols):
+    def __init__(self, rows, cols, seed=0):
         self.form, self.form_t = tq.alloc_mx(rows, cols), tq.alloc_mx(cols, rows)
+        self.seed = seed
 
     def take(self, x, rounding=tq.MX_NEAREST, worker=0, step=0):
-        tq.tq_mx_quantize(x, self.form, self.form_t, rounding, SEED, worker, step)
+        tq.tq_mx_quantize(x, self.form, self.form_t, rounding, self.seed, worker, step)
         return self
 
 
@@ -46,7 +48,7 @@ class Student:
         self.w2.normal_(0, HIDDEN ** -0.5, generator=g)
         self.m1, self.m2 = Matrix(HIDDEN, WIDTH), Matrix(VOCAB, HIDDEN)
         self.mx, self.mh = Matrix(TOKENS, WIDTH), Matrix(TOKENS, HIDDEN)
-        self.mdz, self.mdh = Matrix(TOKENS, VOCAB), Matrix(TOKENS, HIDDEN)
+        self.mdz, self.mdh = Matrix(TOKENS, VOCAB, SEED + 1), Matrix(TOKENS, HIDDEN, SEED + 2)
         shapes = ((TOKENS, HIDDEN, WIDTH), (TOKENS, VOCAB, HIDDEN), (TOKENS, HIDDEN, VOCAB), (VOCAB, HIDDEN, TOKENS), (HIDDEN, WIDTH, TOKENS))
         self.ws = torch.empty(max(tq.mx_matmul_workspace_bytes(*s) for s in shapes) or 1, dtype=torch.uint8, device="cuda")
         self.h = torch.empty(TOKENS, HIDDEN, dtype=torch.bfloat16, device="cuda")
@@ -73,11 +75,11 @@ class Student:
         h = self.mh.take(self.h)
         tq.tq_mx_matmul(h.form, self.m2.form, self.z, self.ws)
         tq.tq_distill(self.z, ids, t, self.grad, self.loss, self.z, TAU)                # dz in place of z
-        dz = self.mdz.take(self.z, tq.MX_STOCHASTIC, i, 2 * step)
+        dz = self.mdz.take(self.z, tq.MX_STOCHASTIC, i, step)
         tq.tq_mx_matmul(dz.form_t, h.form_t, dw2, self.ws)
         tq.tq_mx_matmul(dz.form, self.m2.form_t, self.dh, self.ws)
         self.dh.masked_fill_(self.h <= 0, 0)
-        dh = self.mdh.take(self.dh, tq.MX_STOCHASTIC, i, 2 * step + 1)
+        dh = self.mdh.take(self.dh, tq.MX_STOCHASTIC, i, step)
         tq.tq_mx_matmul(dh.form_t, x.form_t, dw1, self.ws)
         return self.loss.mean()
 

@@ -41,7 +41,10 @@ uint64_t tq_mx_scale_bytes(uint64_t rows, uint64_t cols);
  *              floor(65536 t) + r >= 65536 with 16 random bits r: the mean over the draws is v up to 2^-16 of the step.
  *              Scales are at least 2^-127.  A block that holds a NaN or an infinity gets scale 255 and codes 0.
  *   seed, worker, step   element (i, j) draws the 16 bits at place j % 8 of Philox4x32-10 with the counter
- *              (j / 8, i, worker, step) and the key `seed`, the same for both forms; not used by TQ_MX_NEAREST
+ *              (j / 8, i, worker, step) and the key `seed`, the same for both forms; not used by TQ_MX_NEAREST.  Two matrices
+ *              cast with one (seed, worker, step) draw the same numbers, and so do a matrix's first row and the payload that
+ *              tq_compress makes with them: roundings that are to be independent, as the mean of what is made of several of
+ *              them wants it, take different ones, a seed for each matrix of a step say
  *   codes_dev, scales_dev       the form of x [rows, cols], blocks along a row; both NULL if not wanted
  *   codes_t_dev, scales_t_dev   the form of x^T [cols, rows], blocks along a column of x; both NULL if not wanted
  * All four 16-byte aligned, written in full, padding included.  rows, cols = 1 .. 2^31 - 1, rows * ld <= 2^40.

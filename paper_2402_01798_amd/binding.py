@@ -611,7 +611,8 @@ def _scratch(workspace):
 
 
 def tq_mx_quantize(x, form, form_t=None, rounding=MX_NEAREST, seed=0, worker=0, step=0):
-    """``form`` takes x [rows, cols], ``form_t`` its transpose; either may be None."""
+    """``form`` takes x [rows, cols], ``form_t`` its transpose; either may be None.  Matrices and payloads of one (seed, worker, step) draw
+    the same numbers: give each matrix a seed of its own."""
     if _native_learn("tq_mx_quantize", x, *(_NO_FORM if form is None else form.all()),
                      *(_NO_FORM if form_t is None else form_t.all()), rounding, seed, worker, step):
         return form, form_t
