@@ -9,7 +9,10 @@
  *
  *   z_dev     [rows][ldz] of TQ_F32, TQ_BF16 or TQ_F16, aligned to an element; ldz >= vocab
  *   ids_dev   [rows][top] of int32 (ids_bytes = 4) or int64 (8).  An entry is absent if its id is not in [0, vocab) or its
- *             logit is -inf.  An id may occur twice: the probabilities add up.
+ *             logit is -inf.  An id may occur twice: in the gradient its probabilities add up.  The loss is the sum over the
+ *             entries as it stands above, ln p_i of each entry alone: below the divergence of the added probabilities by
+ *             tau^2 sum_i p_i ln(P_i / p_i), P_i the sum of what shares entry i's id, so that it can be negative.  That does not
+ *             depend on z: the gradient is the loss's.
  *   t_dev     [rows][top] floats
  *   loss_dev, grad_dev   [rows] floats
  *   stats_dev   [rows][2] floats: the row's largest logit M and ln sum_j exp((z_j - M) / tau).  Apart, because their sum
