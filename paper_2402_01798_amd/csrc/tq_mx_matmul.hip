@@ -541,7 +541,10 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 //   128 x 8192 x 8192   53.8   35.0     45.9    42.5   25.7   18.8   13.2
 //   64 x 8192 x 8192                                                  12.8   11.0  4 wavefronts of 64 x 32
 //   64 x 4096 x 4096                                                   8.4    7.1
-//   64 x 32000 x 4096                                          17.1          27.9  1000 tiles, each with all of A to read
+//   64 x 32000 x 4096                                          18.0   16.7   27.6  1000 tiles, each with all of A to read
+//   33 x 33000 x 4096                                          26.0   17.6   29.0  rows that are not there take half of a tile of 128
+//   64 x 128256 x 4096                                         62.3   56.1  103
+//   64 x 131001 x 1024                                         24.5   21.8   54
 //   32 x 8192 x 8192                                                  12.0    8.9  8 wavefronts of 32 x 32
 //   32 x 4096 x 4096                                                   8.1    4.6
 //   32 x 32000 x 4096                                          16.5          18.7  (4 wavefronts, two workgroups on a unit, 16.0)
@@ -586,7 +589,7 @@ Shape shape(uint64_t m, uint64_t n, uint64_t groups)
     const bool split = splits_of_64(m, n, groups) > 1;
     if (m <= 32 && (!split || groups <= 128)) return n <= kUnits * 32 ? kFew : kFewOfMany;
     if (m <= 64 && !split && n <= kUnits * 32) return kFew64;
-    if (tiles_of(m, n, 128, 128) < kUnits) return tiles_of(m, n, 64, 64) > kUnits || groups < 4 ? k64 : k64InParts;
+    if (m <= 64 || tiles_of(m, n, 128, 128) < kUnits) return tiles_of(m, n, 64, 64) > kUnits || groups < 4 ? k64 : k64InParts;
     const Pace* best = kPaces;
     for (const Pace& p : kPaces)
         if (pace(p, m, n) < pace(*best, m, n)) best = &p;

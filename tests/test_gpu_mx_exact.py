@@ -39,6 +39,19 @@ def test_the_addend_is_added_once(m, n, k, out):
         assert torch.equal(place, want)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,n,k", [(33, 32641, 300), (64, 32640, 513), (64, 32801, 1100), (50, 128256, 130)])
+def test_product_of_few_rows_and_a_large_vocabulary(m, n, k, out):
+    (a, va), (b, vb) = small(m, k, 1), small(n, k, 2)
+    product = (va @ vb.t().contiguous()).float()
+    add = torch.randn(m, n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    for extra in (None, add):
+        wide = torch.full((m, n + 3), 5.0, dtype=LC.TYPES[out], device="cuda")
+        B.tq_mx_matmul(a, b, wide[:, 1:n + 1], scratch(B.mx_matmul_workspace_bytes(m, n, k)), extra)
+        assert torch.equal(wide[:, 1:n + 1], (product if extra is None else product + extra).to(LC.TYPES[out]))
+        assert (wide[:, 0] == 5).all() and (wide[:, n + 1:] == 5).all()
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,k", LC.LONG_PRODUCTS)
 def test_product_over_a_long_axis(m, n, k, out):
