@@ -103,7 +103,7 @@ __device__ __forceinline__ void wait_for_stages(uint32_t newer)
 }
 
 // Registers for as many wavefronts on a SIMD as LDS has room for workgroups on the compute unit.
-template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES>
+template <int DTYPE, int BM, int BN, int WM, int WN, int KS, int GROUPS, int STAGES, bool ADD>
 __global__ __launch_bounds__(WM * WN * KS * 64, (Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>::kOnSimd)) void mx_matmul_tile_kernel(MatmulArgs g)
 {
     using S = Tile<BM, BN, WM, WN, KS, GROUPS, STAGES>;
@@ -171,8 +171,9 @@ __global__ __launch_bounds__(WM * WN * KS * 64, (Tile<BM, BN, WM, WN, KS, GROUPS
     // The addend comes after the sums: they would be rounded to its bits at every step, and gradients that are accumulated over batches
     // are far larger than what one batch adds.  Fragment f's 16, as they are stored.  The first kEarly fragments' are requested before
     // the sums begin, one more when one is used; without registers for that each when it is wanted, while other workgroups work.
-    // In the sums from the start / after them, us: 2056 x 1000 x 1999 fp32 10.1 / 10.1, 4096 x 4096 x 512 26.2 / 26.4, 8192 x 8192 x 8192
-    // 370 / 366, as bf16 352 / 363, 1037 x 8192 x 4096 bf16 45 / 37.
+    // In the sums from the start / after them, us: 2056 x 1000 x 1999 fp32 10.1 / 10.1, 4096 x 4096 x 512 26.6 / 25.8, 8192 x 8192 x 8192
+    // 364 / 357, as bf16 348 / 361, 1037 x 8192 x 4096 bf16 45 / 36.  A kernel for products with an addend and one for those without:
+    // the registers that wait for it cost the others 1 % at 8192 x 8192 x 8192.
     auto addends = [&](int f, uint32_t me, float (&v)[2][8]) {
         const uint32_t row = row0 + (wm * S::kFragsM + f / S::kFragsN) * 32, col = col0 + (wn * S::kFragsN + f % S::kFragsN) * 32;
         if constexpr (kAlongRow) {
@@ -190,16 +191,16 @@ __global__ __launch_bounds__(WM * WN * KS * 64, (Tile<BM, BN, WM, WN, KS, GROUPS
     };
     constexpr int kEach = KS > 1 ? BM * BN / S::kThreads : 1;      // outputs of a thread where the parts are joined
     float extra[S::kAhead][2][8] = {}, extra_of[kEach] = {};
-    if constexpr (KS == 1) {
-        if (g.add && S::kEarly) {
+    if constexpr (ADD && KS == 1 && S::kEarly) {
 #pragma unroll
-            for (int f = 0; f < S::kAhead; ++f) addends(f, lane, extra[f]);
-        }
-    } else if (g.add && g.splits == 1) {
+        for (int f = 0; f < S::kAhead; ++f) addends(f, lane, extra[f]);
+    } else if constexpr (ADD && KS > 1) {
+        if (g.splits == 1) {
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            const uint32_t at = threadIdx.x + u * S::kThreads;
-            extra_of[u] = g.add[min(row0 + at / BN, g.m - 1) * g.lda + min(col0 + at % BN, g.n - 1)];
+            for (int u = 0; u < kEach; ++u) {
+                const uint32_t at = threadIdx.x + u * S::kThreads;
+                extra_of[u] = g.add[min(row0 + at / BN, g.m - 1) * g.lda + min(col0 + at % BN, g.n - 1)];
+            }
         }
     }
 #pragma unroll
@@ -262,59 +263,55 @@ __global__ __launch_bounds__(WM * WN * KS * 64, (Tile<BM, BN, WM, WN, KS, GROUPS
             float v = 0.0f;
 #pragma unroll
             for (int q = 0; q < KS; ++q) v += sums[(q * BM + row) * (BN + 1) + col];
-            if (g.add) v += extra_of[u];
+            if constexpr (ADD) v += extra_of[u];
             if (g.splits == 1) store_one<DTYPE>(g, row0 + row, col0 + col, v);
             else if (row0 + row < g.m && col0 + col < g.n) g.partial[((uint64_t)split * g.m + row0 + row) * g.n + col0 + col] = v;
         }
         return;
     }
-    auto store = [&](auto ADD) {
-        uint32_t me = threadIdx.x & 63;
-        asm volatile("" : "+v"(me));                               // places in the output are found here, not kept through the loop
+    uint32_t me = threadIdx.x & 63;
+    asm volatile("" : "+v"(me));                                   // places in the output are found here, not kept through the loop
 #pragma unroll
-        for (int f = 0; f < S::kFrags; ++f) {
-            const int i = f / S::kFragsN, j = f % S::kFragsN;
-            const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
-            if constexpr (decltype(ADD)::value && !S::kEarly) addends(f, me, extra[0]);
-            float v[2][8];
+    for (int f = 0; f < S::kFrags; ++f) {
+        const int i = f / S::kFragsN, j = f % S::kFragsN;
+        const uint32_t row = row0 + (wm * S::kFragsM + i) * 32, col = col0 + (wn * S::kFragsN + j) * 32;
+        if constexpr (ADD && !S::kEarly) addends(f, me, extra[0]);
+        float v[2][8];
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int e = 0; e < (kAlongRow ? 4 : 8); ++e) {
-                    if constexpr (kAlongRow) {                     // 4 columns changed for 4 with the other half make 8 in a row
-                        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 8 + e]),
-                                                                        __float_as_uint(acc[i][j][q * 8 + 4 + e]), false, false);
-                        v[q][e] = __uint_as_float(w[0]);
-                        v[q][4 + e] = __uint_as_float(w[1]);
-                    } else {
-                        v[q][e] = acc[i][j][q * 8 + e];
-                    }
+            for (int e = 0; e < (kAlongRow ? 4 : 8); ++e) {
+                if constexpr (kAlongRow) {                         // 4 columns changed for 4 with the other half make 8 in a row
+                    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][q * 8 + e]),
+                                                                    __float_as_uint(acc[i][j][q * 8 + 4 + e]), false, false);
+                    v[q][e] = __uint_as_float(w[0]);
+                    v[q][4 + e] = __uint_as_float(w[1]);
+                } else {
+                    v[q][e] = acc[i][j][q * 8 + e];
                 }
-            if constexpr (decltype(ADD)::value) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    v[e / 8][e % 8] += extra[f % S::kAhead][e / 8][e % 8];
-                    asm volatile("" : "+v"(v[e / 8][e % 8]));      // here: beside its store it would wait for the stores before it
-                }
-                if (S::kEarly && f + S::kAhead < S::kFrags) addends(f + S::kAhead, me, extra[f % S::kAhead]);
-                asm volatile("" : "+v"(me));                       // nor from one fragment to the next, where addends wait as well
-                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (kAlongRow) {
+        if constexpr (ADD) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const uint32_t to_row = row + (me & 31), to_col = col + q * 16 + (me >> 5) * 8;
-                    if (to_row < g.m && to_col < g.n)
-                        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v[q]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), v[e / 8][e % 8]);
+            for (int e = 0; e < 16; ++e) {
+                v[e / 8][e % 8] += extra[f % S::kAhead][e / 8][e % 8];
+                asm volatile("" : "+v"(v[e / 8][e % 8]));          // here: beside its store it would wait for the stores before it
             }
+            if (S::kEarly && f + S::kAhead < S::kFrags) addends(f + S::kAhead, me, extra[f % S::kAhead]);
+            asm volatile("" : "+v"(me));                           // nor from one fragment to the next, where addends wait as well
+            __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    if (g.add) store(std::true_type{});
-    else store(std::false_type{});
+        if constexpr (kAlongRow) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t to_row = row + (me & 31), to_col = col + q * 16 + (me >> 5) * 8;
+                if (to_row < g.m && to_col < g.n)
+                    store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + to_row * g.ldo + to_col, (int)min(g.n - to_col, 8u), v[q]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) store_one<DTYPE>(g, row + (e / 4) * 8 + (me >> 5) * 4 + e % 4, col + (me & 31), v[e / 8][e % 8]);
+        }
+    }
 }
 
 // Few rows of A, FRAGS x 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds
@@ -506,7 +503,8 @@ hipError_t launch_tile(MatmulArgs& g, hipStream_t st)
     g.tiles = (uint64_t)g.tiles_x * ((g.m + BM - 1) / BM) * g.splits;
     dim3 grid;
     if (!fold_grid((g.tiles + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
-    mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES><<<grid, S::kThreads, S::kBytes, st>>>(g);
+    if (g.add) mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES, true><<<grid, S::kThreads, S::kBytes, st>>>(g);
+    else mx_matmul_tile_kernel<DTYPE, BM, BN, WM, WN, KS, GROUPS, STAGES, false><<<grid, S::kThreads, S::kBytes, st>>>(g);
     return hipGetLastError();
 }
 
