@@ -67,7 +67,7 @@ int tq_mx_dequantize(const void* codes_dev, const void* scales_dev, uint64_t row
  * the same bits every time.
  *   add_dev        NULL, or [m][lda] floats, each added once, to the finished sum in binary32, before the rounding to out's
  *                  type; may be out_dev (gradients that are accumulated over batches), with the same row length then
- *   out_dev        [m][ldo] of TQ_F32, TQ_BF16 or TQ_F16; ldo >= n elements from row to row
+ *   out_dev        [m][ldo] of TQ_F32, TQ_BF16 or TQ_F16 (infinite beyond its range); ldo >= n elements from row to row
  *   workspace_dev  at least tq_mx_matmul_workspace_bytes(m, n, k) bytes, 16-byte aligned (NULL if that is 0): partial
  *                  sums where k is split; contents undefined afterwards; calls that share it have to be ordered
  * m, n, k = 1 .. 2^31 - 1, m * k, n * k, m * ldo and m * lda <= 2^40.

@@ -181,8 +181,8 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest)
 // Stochastic rounding.  A magnitude t (in units of the scale, at most 6) times 2^-126 has, as an fp32 number, the grid's own
 // structure: below 1 it is subnormal and a step of 0.5 is 2^22 units in the last place, above it has one bit of the mantissa above
 // those 22.  So its bits, 16 random bits added where the fraction begins, are the code << 22 and what is dropped.  The product
-// has to be cut off, not rounded, where it is subnormal: round_toward_zero.  5 instructions an element and form, 11 as
-// comparisons and shifts of a fixed-point number.
+// has to be cut off, not rounded, where it is subnormal: round_toward_zero.  4 instructions an element and form and one for an
+// element's draw, 11 as comparisons and shifts of a fixed-point number.
 __device__ __forceinline__ uint32_t round_toward_zero()
 {
     // bits 0 and 1 of the wavefront's mode: fp32 arithmetic.  Gives 0: what is loaded from an address that it is added to comes after.

@@ -521,13 +521,16 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 }
 
 // Which kernel.  Times in us of bf16 products, in turn, replayed from a graph; `64/4` are tiles of 64 with k in 4 parts, `few` is
-// the kernel for few rows:
+// the kernel for few rows; the last seven rows are fp32:
 //   m x n x k            256  256x128  128x320   192    128     64   64/4    few
 //   8192 x 8192 x 8192   283    325      360     372    390    459    645          large tiles move least through the caches
 //   4096 x 4096 x 4096  47.9   54.0     62.9    62.4   62.3   72.4    113
 //   5000 x 5000 x 3000  63.1   67.2     71.2    70.1   73.7   80.5    143
 //   2000 x 6000 x 4096  38.9   41.3     54.6    51.1   42.3   49.5   80.7          the others leave a last round with few tiles
 //   1037 x 8192 x 4096  38.3   40.2     34.1    52.4   39.6   39.3   63.0
+//   600 x 14336 x 4096  39.7   41.4     34.2    54.2   39.5
+//   1800 x 5120 x 4096  38.2   40.6     33.8    52.4   39.2
+//   3500 x 2816 x 4096  37.2   40.4     34.0    51.5   39.4
 //   3000 x 3000 x 4096  37.2   39.0     34.2    32.0   39.1   39.5   62.2
 //   1500 x 4000 x 8192  58.6   44.3     51.3    48.5   47.9   52.0   68.4
 //   2048 x 2048 x 2048  20.2   14.2     16.5    16.1   11.7   11.4   20.0          256 leaves three quarters of the device without a tile
@@ -551,7 +554,16 @@ hipError_t launch_few(MatmulArgs& g, hipStream_t st)
 //   32 x 300 x 32768                                                   9.6   13.0
 //   784 x 1000 x 64      6.1    4.4      5.2     5.2    3.7    3.2    4.7          nothing to part
 //   1 x 8192 x 8192     51.7   34.5     43.6    41.5   24.2   17.6   11.3    7.3
-// Enough tiles of 128 for every compute unit: the shape whose rounds take least.  Where the sides leave little over this is 256.
+//   4096 x 4096 x 128   14.8   13.8                    13.3   16.6                 the stores, and requests that nothing overlaps
+//   4096 x 4096 x 512   18.0   17.5                    16.9   20.4
+//   4096 x 4096 x 1024  22.1   21.5                    21.9   26.3
+//   8192 x 4096 x 256   27.6   25.8                    24.3   28.8
+//   8192 x 8192 x 128   57.0   46.4                    44.4   55.5
+//   8192 x 8192 x 512   70.3   71.7                    60.6   76.8
+//   64 x 131001 x 1024                                 27.4   24.4   56
+// Enough tiles of 128 for every compute unit: the shape whose rounds take least.  Where the sides leave little over this is 256.  The
+// rounds are compared by their steps alone.  What a round costs beside them is left out, so up to 512 of k the rule takes tiles of
+// 256 where those of 128 are 6 to 22 % faster (two or three of them share a compute unit); from 1024 on that is within 3 %.
 // Few tiles and a long k: k is split over workgroups too, where at least 40 groups (5 steps of a workgroup, the second launch's
 // price) are saved.  Not split / split, us: 64 x 64 x 8192 9.8 / 7.8, x 32768 28 / 9.5, x 131072 119 / 12, 256 x 256 x 32768 29 / 12,
 // 700 x 700 x 32768 35 / 26; with fewer saved it loses (500 x 500 x 4096 7.3 / 8.6).
@@ -654,9 +666,15 @@ hipError_t tq_launch_mx_matmul(const void* a, const void* sa, const void* b, con
     return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
 }
 
-// Rows cast by every workgroup of the product, or once in a launch before it.  Linear layers, in us (one launch / two): 8192 x 8192
-// 1 token 9.4 / 11.0, 4 10.8 / 11.2, 6 12.3 / 11.3, 16 18.9 / 11.5; 4096 x 4096 1 4.7 / 6.0, 8 6.6 / 6.5, 16 9.1 / 6.6; 2048 deep and
-// 8192 wide 16 6.6 / 6.5; 4096 deep and 32000 wide, four rounds of workgroups, 1 14.5 / 16.6, 4 16.5 / 16.9, 8 26.8 / 17.0.
+// Rows cast by every workgroup of the product, or once in a launch before it.  Linear layers of n x k, in us (one launch / two), * where
+// the rule takes one launch:
+//                   1            2            3            4            5            8            16 tokens
+//   4096 x 4096    *4.6 / 6.0   *5.0 / 6.1   *5.5 / 6.2   *5.4 / 6.2   *5.9 / 6.3   *6.6 / 6.3    9.0 / 6.5
+//   8192 x 2048    *4.5 / 6.0   *4.5 / 6.2   *4.9 / 6.2   *4.9 / 6.3   *5.3 / 6.4   *5.3 / 6.4   *6.5 / 6.5
+//   8192 x 8192    *8.7 / 10.4  *9.1 / 10.8  *9.8 / 10.5 *10.4 / 10.9 *11.1 / 10.6  13.0 / 11.0  18.0 / 11.2
+//   4096 x 14336   *8.8 / 9.5   *9.9 / 9.5  *10.8 / 9.7   11.8 / 9.6   12.6 / 9.7   15.7 / 9.8   (beyond LDS)
+//   32000 x 4096  *14.4 / 16.3 *16.0 / 16.1 *17.3 / 16.3  15.9 / 16.4  17.5 / 16.2  26.2 / 16.3  35.8 / 16.9   four rounds of workgroups
+// At its edge the two are within 6 % of each other, with 4096 x 14336 and 32000 x 4096 11 and 6 % apart.
 bool tq_mx_linear_in_one(uint64_t m, uint64_t n, uint64_t k)
 {
     const uint64_t groups = (k + tq::kMxGroup - 1) / tq::kMxGroup, rounds = (n + 32 * tq::kUnits - 1) / (32 * tq::kUnits);
