@@ -14,7 +14,7 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 try:
     from . import _tq_marshal
-    if getattr(_tq_marshal, "interface", 0) != 3:
+    if getattr(_tq_marshal, "interface", 0) != 4:
         raise ImportError("built from other sources than this file's")
 except ImportError as e:                # the loops below do the same, slower
     _tq_marshal = None
@@ -26,10 +26,13 @@ except ImportError as e:                # the loops below do the same, slower
 LIB_PATH = os.environ.get("TQ_LIBRARY_PATH") or os.path.join(HERE, "libtq.so")
 
 OK, EINVAL, EALIGN, EUNSUPPORTED, EHIP = 0, 1, 2, 3, 4
-F32, BF16, F16 = 0, 1, 2                # F16: the calls of tq_mx.h and tq_distill.h only
+F32, BF16, F16 = 0, 1, 2                # F16: not the calls of tq.h
 GRID_UNIFORM, GRID_NONUNIFORM, GRID_BISCALED = 0, 1, 2
 MX_NEAREST, MX_STOCHASTIC = 0, 1
 DISTILL_MAX_TOP = 1024
+I8_MAX_K = 131071
+ORTH_HALF, ORTH_SPLIT = 0, 1
+ORTH_MAX_SIDE, ORTH_MAX_COUNT, ORTH_MAX_STEPS = 32768, 64, 16
 NBINS = 898
 MAX_WORKERS = 64
 STATS_BYTES = 3632
@@ -113,6 +116,27 @@ def lib():
         for f in (L.tq_mx_quantize, L.tq_mx_dequantize, L.tq_mx_matmul, L.tq_mx_linear, L.tq_distill_forward,
                   L.tq_distill_backward, L.tq_distill):
             f.restype = i32
+        L.tq_layernorm_workspace_bytes.argtypes = L.tq_i8_code_bytes.argtypes = [u64, u64]
+        L.tq_i8_matmul_workspace_bytes.argtypes = L.tq_i8_linear_workspace_bytes.argtypes = [u64, u64, u64]
+        L.tq_orthogonalize_workspace_bytes.argtypes = [u64, u64, i32, i32]
+        for f in (L.tq_layernorm_workspace_bytes, L.tq_i8_code_bytes, L.tq_i8_matmul_workspace_bytes,
+                  L.tq_i8_linear_workspace_bytes, L.tq_orthogonalize_workspace_bytes):
+            f.restype = u64
+        L.tq_layernorm_forward.argtypes = [vp, i32, u64, u64, u64, vp, vp, i32, f32, vp, u64, vp, vp]
+        L.tq_layernorm_backward.argtypes = [vp, i32, u64, u64, u64, vp, u64, vp, i32, vp, vp, u64, vp, vp, i32, vp, u64, vp]
+        L.tq_i8_quantize.argtypes = [vp, i32, u64, u64, u64, vp, vp, vp]
+        L.tq_i8_dequantize.argtypes = [vp, vp, u64, u64, vp, i32, u64, vp]
+        L.tq_i8_matmul.argtypes = [vp, vp, vp, vp, u64, u64, u64, vp, vp, i32, u64, vp, u64, vp]
+        L.tq_i8_linear.argtypes = [vp, i32, u64, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp, u64, vp]
+        L.tq_orthogonalize.argtypes = [vp, i32, u64, u64, i32, vp, i32, f32, vp, i32, vp, u64, vp]
+        L.tq_orthogonalize_multi.argtypes = [vp, i32, i32, u64, u64, i32, vp, i32, f32, vp, i32, vp, u64, vp]
+        update = [f32, f32, i32, f32, f32, i32, vp, i32, f32, vp, vp, vp, vp, vp, u64, vp]
+        L.tq_orthogonal_update.argtypes = [vp, i32, u64, u64] + update
+        L.tq_orthogonal_update_multi.argtypes = [vp, i32, i32, u64, u64] + update
+        for f in (L.tq_layernorm_forward, L.tq_layernorm_backward, L.tq_i8_quantize, L.tq_i8_dequantize, L.tq_i8_matmul,
+                  L.tq_i8_linear, L.tq_orthogonalize, L.tq_orthogonalize_multi, L.tq_orthogonal_update,
+                  L.tq_orthogonal_update_multi):
+            f.restype = i32
         for name in (*_NATIVE, *_NATIVE_LEARN):
             f = getattr(L, name)
             f.address = C.cast(f, C.c_void_p).value
@@ -130,10 +154,12 @@ _NATIVE = {"tq_stats": "stats", "tq_stats_multi": "stats_multi", "tq_params": "p
            "tq_decompress_aggregate_segments": "aggregate_segments"}
 
 
-# The same for the calls of tq_mx.h and tq_distill.h.
+# The same for the calls of tq_mx.h, tq_distill.h, tq_norm.h and tq_i8.h.
 _NATIVE_LEARN = {"tq_mx_quantize": "mx_quantize", "tq_mx_dequantize": "mx_dequantize", "tq_mx_matmul": "mx_matmul",
                  "tq_mx_linear": "mx_linear", "tq_distill_forward": "distill_forward", "tq_distill_backward": "distill_backward",
-                 "tq_distill": "distill"}
+                 "tq_distill": "distill", "tq_layernorm_forward": "layernorm_forward",
+                 "tq_layernorm_backward": "layernorm_backward", "tq_i8_quantize": "i8_quantize",
+                 "tq_i8_dequantize": "i8_dequantize", "tq_i8_matmul": "i8_matmul", "tq_i8_linear": "i8_linear"}
 _native_calls = {}
 
 
@@ -716,6 +742,257 @@ def tq_distill(z, ids, t, grad, loss, dz, temperature=1.0):
     args, rows = _distill_args(z, ids, t, temperature, grad=grad, loss=loss)
     _check(lib().tq_distill(*args, *rows, *_gradient(z, dz), _stream()), "tq_distill")
     return loss, dz
+
+
+# Layer norm (tq_norm.h), 8-bit integer matrices (tq_i8.h) and orthogonalised updates (tq_orth.h).  All tensors of a call have to be
+# on the current device.
+
+def _here(t, what):
+    """The address of a contiguous tensor on the current device."""
+    p = _dev(t, what)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % what)
+    return p
+
+
+def _matrix_here(t, what):
+    m = _matrix(t, what)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is not on the current device" % what)
+    return m
+
+
+def _vector(t, n, what, dtypes=_TYPES):
+    """(address, type code) of a vector of n elements; (None, None) for None."""
+    if t is None:
+        return None, None
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, got %s" % (what, " or ".join(str(d)[6:] for d in dtypes), t.dtype))
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (what, n))
+    return _here(t, what), _TYPES[t.dtype]
+
+
+_FLOATS = {torch.float32: F32}
+
+
+def _scratch_here(workspace):
+    return (None, 0) if workspace is None or workspace.numel() == 0 else (_here(workspace, "workspace"), workspace.nbytes)
+
+
+def _same_shape(x, t, what):
+    if t.dtype != x.dtype or t.shape != x.shape:
+        raise ValueError("%s must have x's type and shape" % what)
+
+
+def layernorm_workspace_bytes(rows, cols):
+    return int(lib().tq_layernorm_workspace_bytes(rows, cols))
+
+
+def tq_layernorm_forward(x, weight, bias, y, stats=None, eps=1e-5):
+    """y = (x - mean) / sqrt(var + eps) * weight + bias for each row; ``weight`` and ``bias`` may be None.  ``stats`` [rows, 2]: what
+    tq_layernorm_backward takes.  ``y`` may be ``x``."""
+    if _native_learn("tq_layernorm_forward", x, weight, bias, y, stats, eps):
+        return y
+    px, code, rows, cols, ldx = _matrix_here(x, "x")
+    py, _, _, _, ldy = _matrix_here(y, "y")
+    _same_shape(x, y, "y")
+    pw, wtype = _vector(weight, cols, "weight")
+    pb, btype = _vector(bias, cols, "bias")
+    if None not in (wtype, btype) and wtype != btype:
+        raise TypeError("weight and bias must have one type")
+    ps, _ = _vector(stats, 2 * rows, "stats", _FLOATS)
+    _check(lib().tq_layernorm_forward(px, code, rows, cols, ldx, pw, pb, wtype or btype or F32, eps, py, ldy, ps, _stream()),
+           "tq_layernorm_forward")
+    return y
+
+
+def tq_layernorm_backward(x, dy, weight, stats, dx, dweight=None, dbias=None, workspace=None, accumulate=False):
+    """``dx`` may be None, ``dy`` or ``x``; ``dweight`` and ``dbias`` float32, added to what they hold if ``accumulate``."""
+    if _native_learn("tq_layernorm_backward", x, dy, weight, stats, dx, dweight, dbias, workspace, accumulate):
+        return dx, dweight, dbias
+    px, code, rows, cols, ldx = _matrix_here(x, "x")
+    pdy, _, _, _, lddy = _matrix_here(dy, "dy")
+    _same_shape(x, dy, "dy")
+    pdx, lddx = None, 0
+    if dx is not None:
+        pdx, _, _, _, lddx = _matrix_here(dx, "dx")
+        _same_shape(x, dx, "dx")
+    pw, wtype = _vector(weight, cols, "weight")
+    ps, _ = _vector(stats, 2 * rows, "stats", _FLOATS)
+    pdw, _ = _vector(dweight, cols, "dweight", _FLOATS)
+    pdb, _ = _vector(dbias, cols, "dbias", _FLOATS)
+    _check(lib().tq_layernorm_backward(px, code, rows, cols, ldx, pdy, lddy, pw, wtype or F32, ps, pdx, lddx, pdw, pdb,
+                                       int(bool(accumulate)), *_scratch_here(workspace), _stream()), "tq_layernorm_backward")
+    return dx, dweight, dbias
+
+
+class I8Matrix:
+    """A matrix [rows, cols] of 8-bit integers: ``codes`` int8 [rows, 128 G], G groups of 128 in a row, ``scales`` float32 [rows]
+    (see tq_i8.h)."""
+
+    __slots__ = ("codes", "scales", "rows", "cols")
+
+    def __init__(self, codes, scales, rows, cols):
+        if rows < 1 or cols < 1:
+            raise ValueError("a matrix in 8-bit form has elements")
+        if codes.dtype != torch.int8 or scales.dtype != torch.float32:
+            raise TypeError("codes must be int8 and scales float32")
+        if tuple(codes.shape) != (rows, -(-cols // 128) * 128) or tuple(scales.shape) != (rows,):
+            raise ValueError("codes and scales do not match a [%d, %d] matrix" % (rows, cols))
+        _dev(codes, "codes")
+        _dev(scales, "scales")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+
+    def args(self):
+        return _here(self.codes, "codes"), _here(self.scales, "scales")
+
+    def all(self):
+        return self.codes, self.scales, self.rows, self.cols
+
+
+def alloc_i8(rows, cols, device="cuda"):
+    return I8Matrix(torch.empty((rows, -(-cols // 128) * 128), dtype=torch.int8, device=device),
+                    torch.empty((rows,), dtype=torch.float32, device=device), rows, cols)
+
+
+def i8_matmul_workspace_bytes(m, n, k):
+    return int(lib().tq_i8_matmul_workspace_bytes(m, n, k))
+
+
+def i8_linear_workspace_bytes(m, n, k):
+    return int(lib().tq_i8_linear_workspace_bytes(m, n, k))
+
+
+def tq_i8_quantize(x, form):
+    """``form`` takes x [rows, cols], with a scale for each row."""
+    if _native_learn("tq_i8_quantize", x, *form.all()):
+        return form
+    px, code, rows, cols, ld = _matrix_here(x, "x")
+    if form.rows != rows or form.cols != cols:
+        raise ValueError("form must be [%d, %d]" % (rows, cols))
+    _check(lib().tq_i8_quantize(px, code, rows, cols, ld, *form.args(), _stream()), "tq_i8_quantize")
+    return form
+
+
+def tq_i8_dequantize(form, out):
+    if _native_learn("tq_i8_dequantize", *form.all(), out):
+        return out
+    po, code, rows, cols, ld = _matrix_here(out, "out")
+    if (rows, cols) != (form.rows, form.cols):
+        raise ValueError("out must be [%d, %d]" % (form.rows, form.cols))
+    _check(lib().tq_i8_dequantize(*form.args(), rows, cols, po, code, ld, _stream()), "tq_i8_dequantize")
+    return out
+
+
+def tq_i8_matmul(a, b, out, workspace=None, bias=None):
+    """out [m, n] = a [m, k] b [n, k]^T (+ bias [n], float32)."""
+    if _native_learn("tq_i8_matmul", *a.all(), *b.all(), out, workspace, bias):
+        return out
+    po, code, m, n, ld = _matrix_here(out, "out")
+    if a.cols != b.cols or a.rows != m or b.rows != n:
+        raise ValueError("[%d, %d] times [%d, %d]^T does not fit out [%d, %d]" % (a.rows, a.cols, b.rows, b.cols, m, n))
+    pb, _ = _vector(bias, n, "bias", _FLOATS)
+    _check(lib().tq_i8_matmul(*a.args(), *b.args(), m, n, a.cols, pb, po, code, ld, *_scratch_here(workspace), _stream()),
+           "tq_i8_matmul")
+    return out
+
+
+def tq_i8_linear(x, w, out, workspace=None, bias=None):
+    """out [m, n] = Q(x [m, k]) w [n, k]^T (+ bias [n], float32), Q the rounding of tq_i8_quantize."""
+    if _native_learn("tq_i8_linear", x, *w.all(), out, workspace, bias):
+        return out
+    px, code, m, k, ldx = _matrix_here(x, "x")
+    po, ocode, om, n, ldo = _matrix_here(out, "out")
+    if w.cols != k or w.rows != n or om != m:
+        raise ValueError("[%d, %d] times [%d, %d]^T does not fit out [%d, %d]" % (m, k, w.rows, w.cols, om, n))
+    pb, _ = _vector(bias, n, "bias", _FLOATS)
+    _check(lib().tq_i8_linear(px, code, m, ldx, *w.args(), n, k, pb, po, ocode, ldo, *_scratch_here(workspace), _stream()),
+           "tq_i8_linear")
+    return out
+
+
+def orthogonalize_workspace_bytes(rows, cols, count=1, precision=ORTH_SPLIT):
+    return int(lib().tq_orthogonalize_workspace_bytes(rows, cols, count, precision))
+
+
+def _whole(t, what, shape=None, dtypes=_TYPES):
+    """The address of a contiguous matrix on the current device."""
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, got %s" % (what, " or ".join(str(d)[6:] for d in dtypes), t.dtype))
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError("%s must be %s" % (what, "a matrix" if shape is None else "[%d, %d]" % tuple(shape)))
+    return _here(t, what)
+
+
+def _matrices(ts, what, first, dtypes):
+    """Host array of the addresses of as many matrices as there are in ``first``, all alike."""
+    if len(ts) != len(first):
+        raise ValueError("%d matrices for %d of %s" % (len(first), len(ts), what))
+    return (C.c_void_p * len(ts))(*[_whole(t, what, first[0].shape, dtypes) for t in ts])
+
+
+def _orth_head(gs):
+    if not gs:
+        raise ValueError("no matrices")
+    ps = _matrices(gs, "g", gs, (gs[0].dtype,) if gs[0].dtype in _TYPES else _TYPES)
+    rows, cols = gs[0].shape
+    return ps, len(gs), _TYPES[gs[0].dtype], rows, cols
+
+
+def _steps(steps, coefficients):
+    """(number of steps, host array of their coefficients or None)"""
+    if coefficients is None:
+        return steps, None
+    flat = [float(v) for step in coefficients for v in step]
+    if len(flat) != 3 * steps or any(len(step) != 3 for step in coefficients):
+        raise ValueError("coefficients must be %d times (a, b, c)" % steps)
+    return steps, (C.c_float * len(flat))(*flat)
+
+
+def _precision(precision, dtype):
+    """Operands of 11 bits are enough for a result of 8 or 11, for one of 24 they are not."""
+    return (ORTH_SPLIT if dtype == torch.float32 else ORTH_HALF) if precision is None else precision
+
+
+def tq_orthogonalize(g, out, workspace, steps=5, precision=None, eps=1e-7, coefficients=None):
+    """``out`` = the result of ``steps`` Newton-Schulz steps on g [rows, cols] (see tq_orth.h); may be ``g``.  ``coefficients``: (a, b, c) of
+    each step.  ``precision``: ORTH_HALF or ORTH_SPLIT; None: ORTH_SPLIT for a float32 ``out``, ORTH_HALF for others."""
+    tq_orthogonalize_multi([g], [out], workspace, steps, precision, eps, coefficients)
+    return out
+
+
+def tq_orthogonalize_multi(gs, outs, workspace, steps=5, precision=None, eps=1e-7, coefficients=None):
+    """tq_orthogonalize for up to 64 matrices of one shape and type."""
+    head = _orth_head(gs)
+    po = _matrices(outs, "out", gs, (outs[0].dtype,) if outs and outs[0].dtype in _TYPES else _TYPES)
+    n, f = _steps(steps, coefficients)
+    _check(lib().tq_orthogonalize_multi(*head, n, f, _precision(precision, outs[0].dtype), eps, po, _TYPES[outs[0].dtype],
+                                        *_scratch_here(workspace), _stream()), "tq_orthogonalize_multi")
+    return outs
+
+
+def tq_orthogonal_update(g, velocity, theta, workspace, eta, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
+                         precision=None, eps=1e-7, coefficients=None, velocity_out=None, theta_out=None):
+    """Momentum, its orthogonal factor and the new parameters (see tq_orth.h); in place unless ``velocity_out`` or ``theta_out`` is given."""
+    tq_orthogonal_update_multi([g], [velocity], [theta], workspace, eta, momentum, nesterov, weight_decay, scale, steps, precision, eps,
+                               coefficients, None if velocity_out is None else [velocity_out], None if theta_out is None else [theta_out])
+    return theta if theta_out is None else theta_out
+
+
+def tq_orthogonal_update_multi(gs, velocities, thetas, workspace, eta, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
+                               precision=None, eps=1e-7, coefficients=None, velocities_out=None, thetas_out=None):
+    """tq_orthogonal_update for up to 64 matrices of one shape and type."""
+    head = _orth_head(gs)
+    velocities_out = velocities if velocities_out is None else velocities_out
+    thetas_out = thetas if thetas_out is None else thetas_out
+    pv, pvo, pt, pto = (_matrices(ts, what, gs, _FLOATS) for ts, what in
+                        ((velocities, "velocity"), (velocities_out, "velocity_out"), (thetas, "theta"), (thetas_out, "theta_out")))
+    n, f = _steps(steps, coefficients)
+    _check(lib().tq_orthogonal_update_multi(*head, eta, momentum, int(bool(nesterov)), weight_decay, scale, n, f,
+                                            _precision(precision, torch.float32), eps, pv, pvo, pt, pto, *_scratch_here(workspace),
+                                            _stream()), "tq_orthogonal_update_multi")
+    return thetas_out
 
 
 def stats_to_numpy(stats):

@@ -18,9 +18,11 @@ LIB = os.path.join(HERE, "libtq.so")
 FOLD_TEST_LIB = os.path.join(HERE, "libtq_foldtest.so")
 
 MARSHAL = os.path.join(HERE, "_tq_marshal.so")
+MARSHAL_HEADERS = ("tq.h", "tq_mx.h", "tq_distill.h", "tq_norm.h", "tq_i8.h", "tq_orth.h")
 
 LEARN_SOURCES = ["tq_learn_api.hip", "tq_mx_cast.hip", "tq_mx_matmul.hip", "tq_distill.hip"]
-SOURCES = ["tq_api.hip", "tq_stats.hip", "tq_params.hip", "tq_compress.hip", "tq_decode.hip"] + LEARN_SOURCES
+LAYER_SOURCES = ["tq_layer_api.hip", "tq_norm.hip", "tq_i8_cast.hip", "tq_i8_matmul.hip", "tq_orth.hip"]
+SOURCES = ["tq_api.hip", "tq_stats.hip", "tq_params.hip", "tq_compress.hip", "tq_decode.hip"] + LEARN_SOURCES + LAYER_SOURCES
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -42,11 +44,15 @@ def build(force: bool = False, extra_flags=(), verbose: bool = False, lib: str =
                os.path.join(CSRC, "tq_layout.h"), __file__]
     learn_headers = [os.path.join(ROOT, "include", "tq_mx.h"), os.path.join(ROOT, "include", "tq_distill.h"),
                      os.path.join(CSRC, "tq_mx_device.h")]
+    layer_headers = learn_headers[:1] + learn_headers[2:] + \
+        [os.path.join(ROOT, "include", h) for h in ("tq_norm.h", "tq_i8.h", "tq_orth.h")] + \
+        [os.path.join(CSRC, h) for h in ("tq_reduce.h", "tq_i8_device.h", "tq_tiles.h")]
 
     def compile_one(src):
         s = os.path.join(CSRC, src)
         o = os.path.join(obj_dir, src.replace(".hip", ".o"))
-        if force or _stale(o, [s] + headers + (learn_headers if src in LEARN_SOURCES else [])):
+        more = learn_headers if src in LEARN_SOURCES else layer_headers if src in LAYER_SOURCES else []
+        if force or _stale(o, [s] + headers + more):
             cmd = [HIPCC, *FLAGS, *extra_flags, "-c", s, "-o", o]
             if verbose:
                 print(" ".join(cmd))
@@ -76,7 +82,7 @@ def build_marshal(force: bool = False, verbose: bool = False) -> str:
     from torch.utils import cpp_extension
 
     src = os.path.join(CSRC, "tq_marshal.cpp")
-    if force or _stale(MARSHAL, [src, *(os.path.join(ROOT, "include", h) for h in ("tq.h", "tq_mx.h", "tq_distill.h")), __file__]):
+    if force or _stale(MARSHAL, [src, *(os.path.join(ROOT, "include", h) for h in MARSHAL_HEADERS), __file__]):
         lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
         tmp = MARSHAL + ".tmp.%d" % os.getpid()
         cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wno-attributes",

@@ -9,13 +9,17 @@
 // entry point -- because for small tensors the binding's Python code and ctypes took longer than the launch.
 #include <cstdint>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "tq.h"
 #include "tq_distill.h"
+#include "tq_i8.h"
 #include "tq_mx.h"
+#include "tq_norm.h"
+#include "tq_orth.h"
 
 namespace {
 
@@ -666,6 +670,154 @@ PyObject* call_distill(Args in)
     return finish(in, f, z.p, z.dtype, z.rows, z.cols, z.ld, e.ids, e.id_bytes, e.t, e.top, e.temperature, grad, loss, dz.p, dz.ld);
 }
 
+// ---- the calls of tq_norm.h, tq_i8.h and tq_orth.h, whose tensors have to be on the current device
+
+bool here(const Args& in, Py_ssize_t i)
+{
+    return THPVariable_Unpack(in.a[i]).get_device() == c10::hip::current_device();
+}
+
+// A matrix of the three floating-point types on the current device.
+struct DenseHere : Dense {
+    DenseHere(Args& in, Py_ssize_t i) : Dense(in, i)
+    {
+        if (in.ok && !here(in, i)) in.ok = false;
+    }
+};
+
+// A vector of `n` elements of one of the three types, or None.
+struct Vector {
+    const void* p = nullptr;
+    int dtype = -1;
+
+    Vector(Args& in, Py_ssize_t i, uint64_t n)
+    {
+        if (!in.ok || in.a[i] == Py_None) return;
+        const at::Tensor* t = in.tensor(i, (long long)n, (long long)n);
+        if (!t) return;
+        const at::ScalarType type = t->scalar_type();
+        dtype = type == at::kFloat ? TQ_F32 : type == at::kBFloat16 ? TQ_BF16 : type == at::kHalf ? TQ_F16 : -1;
+        if (dtype < 0 || !here(in, i)) in.ok = false;
+        p = t->data_ptr();
+    }
+};
+
+// `n` floats, or None.
+float* floats_or_none(Args& in, Py_ssize_t i, uint64_t n)
+{
+    const Vector v(in, i, n);
+    if (v.p && v.dtype != TQ_F32) in.ok = false;
+    return (float*)v.p;
+}
+
+struct ScratchHere : Scratch {
+    ScratchHere(Args& in, Py_ssize_t i) : Scratch(in, i)
+    {
+        if (in.ok && p && !here(in, i)) in.ok = false;
+    }
+};
+
+// A matrix in 8-bit form: codes, scales, rows, columns, as the binding's I8Matrix holds them.
+struct Form8 {
+    void* codes = nullptr;
+    float* scales = nullptr;
+    uint64_t rows = 0, cols = 0;
+
+    Form8(Args& in, Py_ssize_t i)
+    {
+        if (!in.ok) return;
+        rows = in.u64(i + 2, INT32_MAX);
+        cols = in.u64(i + 3, INT32_MAX);
+        const long long n = (long long)(rows * ((cols + 127) / 128 * 128));
+        codes = in.address(i, n, n);
+        scales = (float*)in.floats(i + 1, (long long)rows, (long long)rows);
+        if (in.ok && (THPVariable_Unpack(in.a[i]).scalar_type() != at::kChar || !here(in, i) || !here(in, i + 1))) in.ok = false;
+    }
+};
+
+bool alike(const Dense& a, const Dense& b, bool type) { return a.rows == b.rows && a.cols == b.cols && (!type || a.dtype == b.dtype); }
+
+// x, weight, bias, y, stats, eps
+PyObject* call_layernorm_forward(Args in)
+{
+    const auto f = in.entry<decltype(&tq_layernorm_forward)>();
+    const DenseHere x(in, 1), y(in, 4);
+    const Vector weight(in, 2, x.cols), bias(in, 3, x.cols);
+    float* stats = floats_or_none(in, 5, 2 * x.rows);
+    const float eps = in.f32(6);
+    if (!alike(x, y, true) || (weight.p && bias.p && weight.dtype != bias.dtype)) in.ok = false;
+    const int wtype = weight.p ? weight.dtype : bias.p ? bias.dtype : TQ_F32;
+    return finish(in, f, x.p, x.dtype, x.rows, x.cols, x.ld, weight.p, bias.p, wtype, eps, y.p, y.ld, stats);
+}
+
+// x, dy, weight, stats, dx, dweight, dbias, workspace, accumulate
+PyObject* call_layernorm_backward(Args in)
+{
+    const auto f = in.entry<decltype(&tq_layernorm_backward)>();
+    const DenseHere x(in, 1), dy(in, 2);
+    const Vector weight(in, 3, x.cols);
+    const float* stats = floats_or_none(in, 4, 2 * x.rows);
+    void* dx = nullptr;
+    uint64_t lddx = 0;
+    if (in.ok && in.a[5] != Py_None) {
+        const DenseHere d(in, 5);
+        if (!alike(x, d, true)) in.ok = false;
+        dx = d.p;
+        lddx = d.ld;
+    }
+    float *dweight = floats_or_none(in, 6, x.cols), *dbias = floats_or_none(in, 7, x.cols);
+    const ScratchHere ws(in, 8);
+    const int accumulate = in.flag(9);
+    if (!alike(x, dy, true)) in.ok = false;
+    return finish(in, f, x.p, x.dtype, x.rows, x.cols, x.ld, dy.p, dy.ld, weight.p, weight.p ? weight.dtype : TQ_F32, stats, dx, lddx,
+                  dweight, dbias, accumulate, ws.p, ws.bytes);
+}
+
+// x, form (4)
+PyObject* call_i8_quantize(Args in)
+{
+    const auto f = in.entry<decltype(&tq_i8_quantize)>();
+    const DenseHere x(in, 1);
+    const Form8 form(in, 2);
+    if (form.rows != x.rows || form.cols != x.cols) in.ok = false;
+    return finish(in, f, x.p, x.dtype, x.rows, x.cols, x.ld, form.codes, form.scales);
+}
+
+// form (4), out
+PyObject* call_i8_dequantize(Args in)
+{
+    const auto f = in.entry<decltype(&tq_i8_dequantize)>();
+    const Form8 form(in, 1);
+    const DenseHere out(in, 5);
+    if (out.rows != form.rows || out.cols != form.cols) in.ok = false;
+    return finish(in, f, form.codes, form.scales, form.rows, form.cols, out.p, out.dtype, out.ld);
+}
+
+// a (4), b (4), out, workspace, bias
+PyObject* call_i8_matmul(Args in)
+{
+    const auto f = in.entry<decltype(&tq_i8_matmul)>();
+    const Form8 a(in, 1), b(in, 5);
+    const DenseHere out(in, 9);
+    const ScratchHere ws(in, 10);
+    const float* bias = floats_or_none(in, 11, out.cols);
+    if (a.cols != b.cols || a.rows != out.rows || b.rows != out.cols) in.ok = false;
+    return finish(in, f, a.codes, a.scales, b.codes, b.scales, out.rows, out.cols, a.cols, bias, out.p, out.dtype, out.ld, ws.p, ws.bytes);
+}
+
+// x, w (4), out, workspace, bias
+PyObject* call_i8_linear(Args in)
+{
+    const auto f = in.entry<decltype(&tq_i8_linear)>();
+    const DenseHere x(in, 1);
+    const Form8 w(in, 2);
+    const DenseHere out(in, 6);
+    const ScratchHere ws(in, 7);
+    const float* bias = floats_or_none(in, 8, out.cols);
+    if (w.cols != x.cols || w.rows != out.cols || out.rows != x.rows) in.ok = false;
+    return finish(in, f, x.p, x.dtype, x.rows, x.ld, w.codes, w.scales, w.rows, w.cols, bias, out.p, out.dtype, out.ld, ws.p, ws.bytes);
+}
+
 template <PyObject* (*CALL)(Args), int ARGS>
 PyObject* take(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
@@ -706,6 +858,12 @@ PyMethodDef methods[] = {
     method<call_distill_forward, 7>("distill_forward"),
     method<call_distill_backward, 8>("distill_backward"),
     method<call_distill, 8>("distill"),
+    method<call_layernorm_forward, 7>("layernorm_forward"),
+    method<call_layernorm_backward, 10>("layernorm_backward"),
+    method<call_i8_quantize, 6>("i8_quantize"),
+    method<call_i8_dequantize, 6>("i8_dequantize"),
+    method<call_i8_matmul, 12>("i8_matmul"),
+    method<call_i8_linear, 9>("i8_linear"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tq_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -716,6 +874,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tq_marshal", nullptr, -1, methods
 PyMODINIT_FUNC PyInit__tq_marshal()
 {
     PyObject* m = PyModule_Create(&module);
-    if (m && PyModule_AddIntConstant(m, "interface", 3) != 0) Py_CLEAR(m);
+    if (m && PyModule_AddIntConstant(m, "interface", 4) != 0) Py_CLEAR(m);
     return m;
 }

@@ -1,0 +1,528 @@
+// Layer norm (tq_norm.h): forward and backward pass, the gradients of weight and bias.
+#include <type_traits>
+
+#include "tq_reduce.h"
+
+namespace tq {
+namespace {
+
+struct NormArgs {
+    const void *x, *dy, *weight, *bias;
+    const float* stats_in;
+    void* out;                                 // y, or dx; dx may be NULL
+    float* stats;
+    float* partial;                            // [parts][2][cols]: sums of dy h and of dy
+    float *dweight, *dbias;
+    uint64_t ldx, lddy, ldo;
+    uint32_t rows, cols, parts;
+    float eps;
+    int accumulate;
+};
+
+// How many of the 8 elements at 8 `oct` a row has.
+__device__ __forceinline__ int left_of(uint32_t cols, uint32_t oct)
+{
+    const int64_t n = (int64_t)cols - (int64_t)oct * 8;
+    return n >= 8 ? 8 : n > 0 ? (int)n : 0;
+}
+
+// A row's mean m, its rest c (m + c is nearer to the mean than m) and 1 / deviation, from passes over its elements:
+// each(f) calls f(value) for all of this thread's.  Where a square or a sum leaves binary32's range, once more in units of 2^80.
+struct RowStats {
+    float unit;                                // x in units of 1 / unit
+    float m, c, r;                             // of x * unit; (x * unit - m - c) * r = h
+    float mean, rstd;                          // of x
+};
+
+template <int WAVES, typename Each>
+__device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, float (*part)[WAVES][2], Each each)
+{
+    const float n = (float)cols;
+    RowStats s;
+    s.unit = 1.0f;
+    float sum = 0.0f, none = 0.0f;
+    each([&](float x) { sum += x; });
+    row_total<WAVES>(sum, none, part[0]);
+    s.m = sum / n;
+    float d1 = 0.0f, d2 = 0.0f;
+    each([&](float x) {
+        const float d = x - s.m;
+        d1 += d;
+        d2 = fmaf(d, d, d2);
+    });
+    row_total<WAVES>(d1, d2, part[1]);
+    s.c = d1 / n;
+    const float var = fmaxf(fmaf(-s.c, s.c, d2 / n), 0.0f);
+    s.r = 1.0f / sqrtf(var + eps);
+    s.mean = s.m + s.c;
+    s.rstd = s.r;
+    if (!(d2 < __builtin_inff())) {            // the whole row's: all its threads take this turn
+        s.unit = 0x1p-80f;
+        sum = none = 0.0f;
+        each([&](float x) { sum += x * s.unit; });
+        if constexpr (WAVES > 1) __syncthreads();                  // a wavefront with a row of its own goes on alone
+        row_total<WAVES>(sum, none, part[0]);
+        s.m = sum / n;
+        d1 = d2 = 0.0f;
+        each([&](float x) {
+            const float d = x * s.unit - s.m;
+            d1 += d;
+            d2 = fmaf(d, d, d2);
+        });
+        row_total<WAVES>(d1, d2, part[1]);
+        s.c = d1 / n;
+        const double v = (double)fmaf(-s.c, s.c, d2 / n), r = 1.0 / sqrt((v > 0.0 || v != v ? v : 0.0) * 0x1p160 + (double)eps);
+        s.r = (float)(r * 0x1p80);
+        s.mean = (s.m + s.c) * 0x1p80f;
+        s.rstd = (float)r;
+    }
+    return s;
+}
+
+// A row by WAVES wavefronts that hold it in registers, 8 V elements each lane; short rows several to a workgroup.
+template <int DTYPE, int WTYPE, int WAVES, int V>
+__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_forward_kernel(NormArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    using W = typename Element<WTYPE>::type;
+    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
+    __shared__ float part[kRows][2][WAVES][2];
+    const uint32_t sub = threadIdx.x / kThreads, tid = threadIdx.x % kThreads;
+    const uint64_t row = (uint64_t)linear_block() * kRows + sub;
+    static_assert(WAVES == 1 || kRows == 1, "barriers are for whole workgroups");
+    if (row >= a.rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    Eight<DTYPE> w[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t oct = tid + i * kThreads;
+        const int n = left_of(a.cols, oct);
+        if (n == 8) w[i].load(x + (uint64_t)oct * 8);
+        else if (n) w[i].load(x + (uint64_t)oct * 8, n);
+        else w[i].clear();
+    }
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int n = left_of(a.cols, tid + i * kThreads);
+            float v[8];
+            w[i].unpack(v);
+            if (n == 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f(v[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) f(v[j]);
+            }
+        }
+    };
+    const RowStats s = row_stats<WAVES>(a.cols, a.eps, part[sub], each);
+    if (a.stats && tid == 0) {
+        a.stats[2 * row] = s.mean;
+        a.stats[2 * row + 1] = s.rstd;
+    }
+    T* y = static_cast<T*>(a.out) + row * a.ldo;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t oct = tid + i * kThreads;
+        const int n = left_of(a.cols, oct);
+        if (n == 0) continue;
+        float v[8], weight[8], bias[8];
+        w[i].unpack(v);
+        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+        if (a.bias) load8<WTYPE>(static_cast<const W*>(a.bias) + (uint64_t)oct * 8, n, bias);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float h = ((v[j] * s.unit - s.m) - s.c) * s.r;
+            v[j] = a.weight ? h * weight[j] : h;
+            if (a.bias) v[j] += bias[j];
+        }
+        store8<DTYPE>(y + (uint64_t)oct * 8, n, v);
+    }
+}
+
+constexpr int kLongWaves = 16;
+
+// Rows that do not fit the registers, by a workgroup each, read anew for every pass.
+template <int DTYPE, int WTYPE>
+__global__ __launch_bounds__(kLongWaves * 64) void norm_forward_long_kernel(NormArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    using W = typename Element<WTYPE>::type;
+    __shared__ float part[2][kLongWaves][2];
+    const uint64_t row = linear_block();
+    if (row >= a.rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    const uint32_t octs = (uint32_t)(((uint64_t)a.cols + 7) / 8);
+    auto each = [&](auto f) {
+        for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
+            const int n = left_of(a.cols, oct);
+            float v[8];
+            load8<DTYPE>(x + (uint64_t)oct * 8, n, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) f(v[j]);
+        }
+    };
+    const RowStats s = row_stats<kLongWaves>(a.cols, a.eps, part, each);
+    if (a.stats && threadIdx.x == 0) {
+        a.stats[2 * row] = s.mean;
+        a.stats[2 * row + 1] = s.rstd;
+    }
+    T* y = static_cast<T*>(a.out) + row * a.ldo;
+    for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
+        const int n = left_of(a.cols, oct);
+        float v[8], weight[8], bias[8];
+        load8<DTYPE>(x + (uint64_t)oct * 8, n, v);
+        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+        if (a.bias) load8<WTYPE>(static_cast<const W*>(a.bias) + (uint64_t)oct * 8, n, bias);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float h = ((v[j] * s.unit - s.m) - s.c) * s.r;
+            v[j] = a.weight ? h * weight[j] : h;
+            if (a.bias) v[j] += bias[j];
+        }
+        store8<DTYPE>(y + (uint64_t)oct * 8, n, v);
+    }
+}
+
+// h of an element: the difference in quarters, which two numbers of the largest magnitude do not take out of range.
+__device__ __forceinline__ float deviation(float x, float quarter_mean, float four_rstd)
+{
+    return fmaf(x, 0.25f, -quarter_mean) * four_rstd;
+}
+
+// dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
+// other; their sums over rows are joined at the end.
+template <int DTYPE, int WTYPE, int WAVES, int V>
+__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    using W = typename Element<WTYPE>::type;
+    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
+    __shared__ float part[2][WAVES][2];
+    __shared__ float sums[kRows > 1 ? kThreads * V * 8 : 1];
+    static_assert(WAVES == 1 || kRows == 1, "barriers are for whole workgroups");
+    const uint32_t sub = threadIdx.x / kThreads, tid = threadIdx.x % kThreads, block = linear_block();
+    if (block >= a.parts) return;
+    const float n_inv = 1.0f / (float)a.cols;
+    float dw[V][8] = {}, db[V][8] = {};
+    uint32_t turn = 0;
+    for (uint64_t row = (uint64_t)block * kRows + sub; row < a.rows; row += (uint64_t)a.parts * kRows) {
+        const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+        const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
+        Eight<DTYPE> wx[V], wdy[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t oct = tid + i * kThreads;
+            const int n = left_of(a.cols, oct);
+            if (n == 8) {
+                wx[i].load(x + (uint64_t)oct * 8);
+                wdy[i].load(dy + (uint64_t)oct * 8);
+            } else if (n) {
+                wx[i].load(x + (uint64_t)oct * 8, n);
+                wdy[i].load(dy + (uint64_t)oct * 8, n);
+            } else {
+                wx[i].clear();
+                wdy[i].clear();
+            }
+        }
+        const float quarter = 0.25f * a.stats_in[2 * row], r = a.stats_in[2 * row + 1], four = 4.0f * r;
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t oct = tid + i * kThreads;
+            const int n = left_of(a.cols, oct);
+            float v[8], g[8], weight[8];
+            wx[i].unpack(v);
+            wdy[i].unpack(g);
+            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float h = deviation(v[j], quarter, four);
+                dw[i][j] = fmaf(g[j], h, dw[i][j]);
+                db[i][j] += g[j];
+                if (j < n) {
+                    const float gw = a.weight ? g[j] * weight[j] : g[j];
+                    s1 += gw;
+                    s2 = fmaf(gw, h, s2);
+                }
+            }
+        }
+        if (!a.out) continue;
+        row_total<WAVES>(s1, s2, part[turn]);
+        turn ^= 1;
+        s1 *= n_inv;
+        s2 *= n_inv;
+        T* dx = static_cast<T*>(a.out) + row * a.ldo;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const uint32_t oct = tid + i * kThreads;
+            const int n = left_of(a.cols, oct);
+            if (n == 0) continue;
+            float v[8], g[8], weight[8];
+            wx[i].unpack(v);
+            wdy[i].unpack(g);
+            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float h = deviation(v[j], quarter, four);
+                const float gw = a.weight ? g[j] * weight[j] : g[j];
+                v[j] = r * ((gw - s1) - h * s2);
+            }
+            store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
+        }
+    }
+    if (!a.partial) return;
+    float* to = a.partial + (uint64_t)block * 2 * a.cols;
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (kRows > 1) {                                 // the workgroup's rows, in their order
+            for (uint32_t k = 1; k < kRows; ++k) {
+                __syncthreads();
+                if (sub == k) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sums[(i * 8 + j) * kThreads + tid] = which ? db[i][j] : dw[i][j];
+                }
+                __syncthreads();
+                if (sub == 0) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) (which ? db[i][j] : dw[i][j]) += sums[(i * 8 + j) * kThreads + tid];
+                }
+            }
+        }
+        if (sub == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t oct = tid + i * kThreads;
+                const int n = left_of(a.cols, oct);
+                if (n) store8<TQ_F32>(to + (uint64_t)which * a.cols + (uint64_t)oct * 8, n, which ? db[i] : dw[i]);
+            }
+        }
+    }
+}
+
+// dx of a row that does not fit the registers.
+template <int DTYPE, int WTYPE>
+__global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(NormArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    using W = typename Element<WTYPE>::type;
+    __shared__ float part[kLongWaves][2];
+    const uint64_t row = linear_block();
+    if (row >= a.rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
+    T* dx = static_cast<T*>(a.out) + row * a.ldo;
+    const float quarter = 0.25f * a.stats_in[2 * row], r = a.stats_in[2 * row + 1], four = 4.0f * r;
+    const uint32_t octs = (uint32_t)(((uint64_t)a.cols + 7) / 8);
+    float s1 = 0.0f, s2 = 0.0f;
+    auto each = [&](auto f) {
+        for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
+            const int n = left_of(a.cols, oct);
+            float v[8], g[8], weight[8];
+            load8<DTYPE>(x + (uint64_t)oct * 8, n, v);
+            load8<DTYPE>(dy + (uint64_t)oct * 8, n, g);
+            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = deviation(v[j], quarter, four);
+                if (a.weight) g[j] *= weight[j];
+            }
+            f(oct, n, v, g);
+        }
+    };
+    each([&](uint32_t, int n, const float (&h)[8], const float (&g)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) {
+                s1 += g[j];
+                s2 = fmaf(g[j], h[j], s2);
+            }
+    });
+    row_total<kLongWaves>(s1, s2, part);
+    s1 /= (float)a.cols;
+    s2 /= (float)a.cols;
+    each([&](uint32_t oct, int n, const float (&h)[8], const float (&g)[8]) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = r * ((g[j] - s1) - h[j] * s2);
+        store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
+    });
+}
+
+// Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, uint32_t across)
+{
+    using T = typename Element<DTYPE>::type;
+    const uint32_t block = linear_block(), by = block / across, oct = (block - by * across) * 256 + threadIdx.x;
+    if (by >= a.parts) return;
+    const int n = left_of(a.cols, oct);
+    if (n == 0) return;
+    float dw[8] = {}, db[8] = {};
+    for (uint64_t row = by; row < a.rows; row += a.parts) {
+        float v[8], g[8];
+        load8<DTYPE>(static_cast<const T*>(a.x) + row * a.ldx + (uint64_t)oct * 8, n, v);
+        load8<DTYPE>(static_cast<const T*>(a.dy) + row * a.lddy + (uint64_t)oct * 8, n, g);
+        const float quarter = 0.25f * a.stats_in[2 * row], four = 4.0f * a.stats_in[2 * row + 1];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            dw[j] = fmaf(g[j], deviation(v[j], quarter, four), dw[j]);
+            db[j] += g[j];
+        }
+    }
+    float* to = a.partial + (uint64_t)by * 2 * a.cols + (uint64_t)oct * 8;
+    store8<TQ_F32>(to, n, dw);
+    store8<TQ_F32>(to + a.cols, n, db);
+}
+
+// The parts' sums, joined in a fixed order: 32 columns of dweight and dbias by 32 threads each.
+__global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
+{
+    __shared__ float sums[32][33];
+    const uint32_t lane = threadIdx.x & 31, strip = threadIdx.x >> 5;
+    const uint64_t at = (uint64_t)linear_block() * 32 + lane, all = 2 * (uint64_t)a.cols;
+    if ((uint64_t)linear_block() * 32 >= all) return;
+    float v = 0.0f;
+    if (at < all)
+        for (uint32_t p = strip; p < a.parts; p += 32) v += a.partial[p * all + at];
+    sums[strip][lane] = v;
+    __syncthreads();
+    if (strip || at >= all) return;
+    for (int s = 1; s < 32; ++s) v += sums[s][lane];
+    float* to = at < a.cols ? a.dweight : a.dbias;
+    if (!to) return;
+    to += at < a.cols ? at : at - a.cols;
+    *to = a.accumulate ? *to + v : v;
+}
+
+// The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.
+template <typename F>
+hipError_t by_shape(uint32_t cols, F f)
+{
+    auto as = [&](auto w, auto v) { return f(w, v); };
+#define TQ_NORM_SHAPE(WAVES, V) return as(std::integral_constant<int, WAVES>{}, std::integral_constant<int, V>{})
+    if (cols <= 512) TQ_NORM_SHAPE(1, 1);
+    if (cols <= 1024) TQ_NORM_SHAPE(1, 2);
+    if (cols <= 2048) TQ_NORM_SHAPE(4, 1);
+    if (cols <= 4096) TQ_NORM_SHAPE(4, 2);
+    if (cols <= 8192) TQ_NORM_SHAPE(8, 2);
+    TQ_NORM_SHAPE(16, 2);
+#undef TQ_NORM_SHAPE
+}
+
+constexpr uint32_t kMostInRegisters = 16384;
+
+template <typename F>
+hipError_t by_type(int dtype, F f)
+{
+    if (dtype == TQ_F32) return f(std::integral_constant<int, TQ_F32>{});
+    return dtype == TQ_BF16 ? f(std::integral_constant<int, TQ_BF16>{}) : f(std::integral_constant<int, TQ_F16>{});
+}
+
+uint32_t rows_at_once(uint32_t cols) { return cols <= 1024 ? 4 : 1; }
+
+// Workgroups that share the rows of a backward pass, and with it the partial sums.
+uint32_t parts_of(uint64_t rows, uint64_t cols)
+{
+    if (cols > kMostInRegisters) return (uint32_t)(rows < 64 ? rows : 64);
+    const uint64_t most = cols <= 4096 ? 1024 : cols <= 8192 ? 512 : 256, r = rows_at_once((uint32_t)cols), wanted = (rows + r - 1) / r;
+    return (uint32_t)(wanted < most ? wanted : most);
+}
+
+}  // namespace
+}  // namespace tq
+
+hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ldx, const void* weight,
+                                       const void* bias, int wtype, float eps, void* y, uint64_t ldy, float* stats, hipStream_t st)
+{
+    using namespace tq;
+    NormArgs a = {};
+    a.x = x;
+    a.ldx = ldx;
+    a.weight = weight;
+    a.bias = bias;
+    a.out = y;
+    a.ldo = ldy;
+    a.stats = stats;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.eps = eps;
+    return by_type(dtype, [&](auto D) {
+        return by_type(wtype, [&](auto W) -> hipError_t {
+            constexpr int kD = decltype(D)::value, kW = decltype(W)::value;
+            dim3 grid;
+            if (cols > kMostInRegisters) {
+                if (!fold_grid(rows, kLongWaves * 64, 1, grid)) return hipErrorInvalidValue;
+                norm_forward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
+                return hipGetLastError();
+            }
+            return by_shape(a.cols, [&](auto N, auto V) -> hipError_t {
+                constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
+                const uint32_t each = kThreads / (kN * 64);
+                if (!fold_grid((rows + each - 1) / each, kThreads, 1, grid)) return hipErrorInvalidValue;
+                norm_forward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
+                return hipGetLastError();
+            });
+        });
+    });
+}
+
+uint64_t tq_layernorm_workspace_bytes_impl(uint64_t rows, uint64_t cols) { return (uint64_t)tq::parts_of(rows, cols) * 2 * cols * sizeof(float); }
+
+hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ldx, const void* dy, uint64_t lddy,
+                                        const void* weight, int wtype, const float* stats, void* dx, uint64_t lddx, float* dweight,
+                                        float* dbias, int accumulate, void* workspace, hipStream_t st)
+{
+    using namespace tq;
+    NormArgs a = {};
+    a.x = x;
+    a.ldx = ldx;
+    a.dy = dy;
+    a.lddy = lddy;
+    a.weight = weight;
+    a.stats_in = stats;
+    a.out = dx;
+    a.ldo = lddx;
+    a.dweight = dweight;
+    a.dbias = dbias;
+    a.accumulate = accumulate;
+    a.partial = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.parts = parts_of(rows, cols);
+    dim3 grid;
+    const hipError_t e = by_type(dtype, [&](auto D) {
+        return by_type(wtype, [&](auto W) -> hipError_t {
+            constexpr int kD = decltype(D)::value, kW = decltype(W)::value;
+            if (cols > kMostInRegisters) {
+                if (a.partial) {                                   // first: dx may take the place of what it reads
+                    const uint32_t across = (uint32_t)(((cols + 7) / 8 + 255) / 256);
+                    if (!fold_grid((uint64_t)across * a.parts, 256, 1, grid)) return hipErrorInvalidValue;
+                    norm_columns_kernel<kD><<<grid, 256, 0, st>>>(a, across);
+                    const hipError_t e = hipGetLastError();
+                    if (e != hipSuccess) return e;
+                }
+                if (!a.out) return hipSuccess;
+                if (!fold_grid(rows, kLongWaves * 64, 1, grid)) return hipErrorInvalidValue;
+                norm_backward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
+                return hipGetLastError();
+            }
+            return by_shape(a.cols, [&](auto N, auto V) -> hipError_t {
+                constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
+                if (!fold_grid(a.parts, kThreads, 1, grid)) return hipErrorInvalidValue;
+                norm_backward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
+                return hipGetLastError();
+            });
+        });
+    });
+    if (e != hipSuccess || !a.partial) return e;
+    if (!fold_grid((2 * cols + 31) / 32, 1024, 1, grid)) return hipErrorInvalidValue;
+    norm_join_kernel<<<grid, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}

@@ -1,0 +1,157 @@
+"""Matrices of 8-bit integers: codes, scales and products bit for bit against a plain statement (layer_common)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2402_01798_amd import binding as B
+from layer_common import TYPES, i8_form, i8_product, strided
+
+pytestmark = pytest.mark.gpu
+
+
+def cast(x):
+    form = B.alloc_i8(*x.shape)
+    form.codes.fill_(99)
+    B.tq_i8_quantize(x, form)
+    return form
+
+
+def check_cast(x, view=None):
+    form = cast(x.cuda() if view is None else view)
+    codes, scales = i8_form(x.float().numpy())
+    assert np.array_equal(form.scales.cpu().numpy(), scales, equal_nan=True)
+    assert np.array_equal(form.codes.cpu().numpy(), codes)
+    return form
+
+
+SHAPES = [(1, 1), (3, 1), (2, 7), (5, 127), (4, 128), (9, 129), (3, 512), (5, 513), (2, 2048), (3, 2049), (2, 8193), (1, 32768), (2, 40001)]
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows, cols", SHAPES)
+def test_cast(rows, cols, dtype):
+    g = torch.Generator().manual_seed(rows + cols)
+    x = (torch.randn(rows, cols, generator=g) * torch.exp(torch.randn(rows, 1, generator=g))).to(TYPES[dtype])
+    form = check_cast(x)
+    for out in TYPES:
+        values = torch.empty(rows, cols, dtype=TYPES[out], device="cuda")
+        B.tq_i8_dequantize(form, values)
+        want = (form.codes[:, :cols].float() * form.scales.view(-1, 1)).to(TYPES[out])
+        assert torch.equal(values, want)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("cols", [3, 130, 3001, 33000])
+def test_cast_of_rows_apart(cols, dtype):
+    x = torch.randn(5, cols, generator=torch.Generator().manual_seed(cols)).to(TYPES[dtype])
+    view = strided(x, 3, 1)
+    check_cast(x, view)
+    out = strided(torch.zeros(5, cols), 5, 3)
+    form = cast(view)
+    B.tq_i8_dequantize(form, out)
+    assert torch.equal(out, form.codes[:, :cols].float() * form.scales.view(-1, 1))
+    assert torch.as_strided(out, (4, 5), out.stride(), out.storage_offset() + cols).isnan().all()
+
+
+def test_ties_and_their_neighbours():
+    """Elements exactly between two codes (127 x / A = k + 1/2) and the binary32 numbers beside them."""
+    for a in (127.0, 254.0, 1.0, 3.0, 127 * 2.0 ** -100, 127 * 2.0 ** -140, 127 * 2.0 ** 100, 0.7, 2.0 ** -149 * 127):
+        a = np.float32(a)
+        middle = ((np.arange(127) + 0.5) * np.float64(a) / 127).astype(np.float32)
+        row = np.concatenate([[a], middle, np.nextafter(middle, np.float32(np.inf)), np.nextafter(middle, np.float32(0)), -middle])
+        check_cast(torch.from_numpy(np.minimum(np.maximum(row, -a), a).astype(np.float32)).view(1, -1))
+
+
+def test_special_rows():
+    x = torch.randn(8, 300, generator=torch.Generator().manual_seed(3))
+    x[1] = 0
+    x[2, 7] = float("nan")
+    x[3, 299] = float("inf")
+    x[4] = -0.0
+    x[5] *= 1e-42
+    x[6] *= 1e38
+    x[7] = 2.0 ** -149
+    form = check_cast(x)
+    assert form.scales[1] == 0 and form.scales[4] == 0 and form.scales[2].isnan() and form.scales[3].isnan()
+    y = torch.empty(8, 5, device="cuda")
+    w = cast(torch.ones(5, 300, device="cuda"))
+    B.tq_i8_matmul(form, w, y, scratch(B.i8_matmul_workspace_bytes(8, 5, 300)))
+    # row 6 holds numbers up to 3e38: its sums may be infinite, as the definition's are
+    want = i8_product(*(t.cpu().numpy() for t in (form.codes, form.scales, w.codes, w.scales)), None, "f32")
+    assert np.array_equal(y.cpu().numpy(), want.numpy(), equal_nan=True)
+    assert y[2].isnan().all() and y[3].isnan().all() and (y[1] == 0).all() and y[[0, 1, 4, 5, 7]].isfinite().all()
+
+
+def scratch(nbytes):
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+def random_form(rows, cols, seed, low=-127):
+    g = np.random.default_rng(seed)
+    codes = np.zeros((rows, -(-cols // 128) * 128), dtype=np.int8)
+    codes[:, :cols] = g.integers(low, 128, (rows, cols))
+    scales = np.exp(g.normal(size=rows) - 4).astype(np.float32)
+    return codes, scales
+
+
+def device_form(codes, scales, cols):
+    return B.I8Matrix(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), codes.shape[0], cols)
+
+
+MNK = [(1, 1, 1), (1, 17, 5), (3, 40, 129), (1, 300, 4096), (2, 65, 1000), (7, 100, 128), (16, 96, 513), (17, 33, 700), (31, 1000, 260),
+       (32, 64, 4097), (33, 200, 300), (64, 64, 64), (65, 70, 2000), (100, 129, 255), (128, 128, 128), (129, 257, 385), (200, 1000, 1200),
+       (300, 500, 64), (520, 260, 1), (1030, 300, 200), (700, 700, 700), (1, 9000, 300), (24, 8200, 130), (40, 8200, 130), (257, 4100, 130),
+       (2100, 2050, 140)]
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("m, n, k", MNK)
+def test_product(m, n, k, dtype):
+    a, sa = random_form(m, k, m + k)
+    b, sb = random_form(n, k, n + 2 * k)
+    bias = np.random.default_rng(n).normal(size=n).astype(np.float32)
+    fa, fb, ws = device_form(a, sa, k), device_form(b, sb, k), scratch(B.i8_matmul_workspace_bytes(m, n, k))
+    for add in (None, bias):
+        out = strided(torch.zeros(m, n, dtype=TYPES[dtype]), 3, 1)
+        B.tq_i8_matmul(fa, fb, out, ws, None if add is None else torch.from_numpy(add).cuda())
+        assert torch.equal(out.cpu(), i8_product(a, sa, b, sb, add, dtype))
+        if m > 1:
+            assert torch.as_strided(out, (m - 1, 3), out.stride(), out.storage_offset() + n).isnan().all()
+
+
+@pytest.mark.parametrize("m, n", [(1, 40), (20, 64), (60, 64), (130, 64), (300, 200)])
+@pytest.mark.parametrize("k", [131071, 20000])
+def test_long_sums_at_the_ends_of_the_range(m, n, k):
+    """Every product 128 * 128 or its opposite: the largest sums that 32 bits have to hold."""
+    a = np.zeros((m, -(-k // 128) * 128), dtype=np.int8)
+    b = np.zeros((n, a.shape[1]), dtype=np.int8)
+    a[:, :k] = -128
+    b[:, :k] = -128
+    b[1::2, :k] = 127
+    ones = np.ones(m, np.float32), np.ones(n, np.float32)
+    out = torch.empty(m, n, device="cuda")
+    B.tq_i8_matmul(device_form(a, ones[0], k), device_form(b, ones[1], k), out, scratch(B.i8_matmul_workspace_bytes(m, n, k)))
+    assert torch.equal(out.cpu(), i8_product(a, ones[0], b, ones[1], None, "f32"))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("m, n, k", [(1, 33, 100), (1, 8200, 1000), (2, 70, 4096), (4, 300, 5000), (8, 64, 129), (16, 256, 300), (17, 256, 300), (1, 100, 40000),
+                                     (16, 40, 9000), (33, 100, 1030), (300, 260, 515), (1, 1, 1)])
+def test_linear_is_cast_and_product(m, n, k, dtype):
+    g = torch.Generator().manual_seed(m + n + k)
+    x = torch.randn(m, k, generator=g).to(TYPES[dtype])
+    if m > 2:
+        x[1] = 0
+        x[2, k // 2] = float("nan")
+    w, sw = random_form(n, k, k)
+    fw = device_form(w, sw, k)
+    bias = torch.randn(n, generator=g)
+    view = strided(x, 1, 1)
+    form = cast(view)
+    for b in (None, bias.cuda()):
+        got, want = torch.empty(m, n, dtype=TYPES[dtype], device="cuda"), torch.empty(m, n, dtype=TYPES[dtype], device="cuda")
+        B.tq_i8_linear(view, fw, got, scratch(B.i8_linear_workspace_bytes(m, n, k)), bias=b)
+        B.tq_i8_matmul(form, fw, want, scratch(B.i8_matmul_workspace_bytes(m, n, k)), bias=b)
+        assert torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0))
+    codes, scales = i8_form(x.float().numpy())
+    assert torch.equal(want.cpu().nan_to_num(7.0), i8_product(codes, scales, w, sw, bias.numpy(), dtype).nan_to_num(7.0))
