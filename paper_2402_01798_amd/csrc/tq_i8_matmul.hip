@@ -57,7 +57,7 @@ hipError_t launch_tiles(I8MatmulArgs& g, hipStream_t st)
 template <int DTYPE>
 hipError_t launch_matmul(I8MatmulArgs& g, hipStream_t st)
 {
-    return launch_tiles<DTYPE, TileShape<kInt8, 128, 128, 2, 2, 2>>(g, st);
+    return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 2, 64, 5>>(g, st);
 }
 
 }  // namespace

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(OrthPointers p, OrthArgs
 template <int KIND>
 __device__ __forceinline__ uint64_t in_row(uint32_t col)
 {
-    return KIND == kHalf ? (uint64_t)col * 2 : (uint64_t)(col / 32) * 128 + col % 32 * 2;
+    return KIND == kHalf ? (uint64_t)col * 2 : (uint64_t)(col / 16) * 64 + col % 16 * 2;
 }
 
 __device__ __forceinline__ float low_part(float v, _Float16 high) { return v - (float)high; }
@@ -94,7 +94,7 @@ __device__ __forceinline__ void put8(char* row, uint32_t col, const float (&v)[8
     }
     char* to = row + in_row<KIND>(col);
     *reinterpret_cast<tile_f16x8*>(to) = high;
-    if constexpr (KIND == kHalfPair) *reinterpret_cast<tile_f16x8*>(to + 64) = low;
+    if constexpr (KIND == kHalfPair) *reinterpret_cast<tile_f16x8*>(to + 32) = low;
 }
 
 template <int KIND>
@@ -103,7 +103,7 @@ __device__ __forceinline__ void put1(char* row, uint32_t col, float v)
     char* to = row + in_row<KIND>(col);
     const _Float16 high = (_Float16)v;
     *reinterpret_cast<_Float16*>(to) = high;
-    if constexpr (KIND == kHalfPair) *reinterpret_cast<_Float16*>(to + 64) = (_Float16)low_part(v, high);
+    if constexpr (KIND == kHalfPair) *reinterpret_cast<_Float16*>(to + 32) = (_Float16)low_part(v, high);
 }
 
 template <int KIND>
@@ -112,7 +112,7 @@ __device__ __forceinline__ void get8(const char* row, uint32_t col, float (&v)[8
     const char* from = row + in_row<KIND>(col);
     const tile_f16x8 high = *reinterpret_cast<const tile_f16x8*>(from);
     if constexpr (KIND == kHalfPair) {
-        const tile_f16x8 low = *reinterpret_cast<const tile_f16x8*>(from + 64);
+        const tile_f16x8 low = *reinterpret_cast<const tile_f16x8*>(from + 32);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = (float)high[e] + (float)low[e];
     } else {
@@ -349,7 +349,7 @@ hipError_t launch_begin(const OrthCall& q, const OrthPointers& p, OrthArgs& o, h
 template <int KIND>
 hipError_t launch_orth(const OrthCall& q, hipStream_t st)
 {
-    using Square = TileShape<KIND, 128, 128, 2, 2, 2>;
+    using Square = std::conditional_t<KIND == kHalf, TileShape<KIND, 256, 256, 2, 2, 64, 5>, TileShape<KIND, 128, 128, 2, 2, 128, 2>>;
     const Layout l = layout(q.rows, q.cols, KIND);
     const bool flip = q.rows > q.cols;
     const uint32_t r = (uint32_t)(flip ? q.cols : q.rows), c = (uint32_t)(flip ? q.rows : q.cols);

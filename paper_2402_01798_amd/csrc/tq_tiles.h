@@ -2,13 +2,16 @@
 // numbers, or pairs of those.  The sums of a tile stay in registers; what becomes of them is the calling kernel's.
 #pragma once
 
+#include <type_traits>
+
 #include "tq_mx_device.h"
 
 namespace tq {
 
 constexpr uint64_t kComputeUnits = 256, kLdsBytes = 160 << 10;
 
-// What a group of 128 bytes holds.  kHalfPair: 32 elements as the sum of two binary16 numbers, the 32 larger ones first.
+// What a group of 128 bytes holds.  kHalfPair: elements as the sum of two binary16 numbers, 16 larger ones and the 16 smaller ones that go with
+// them, twice.
 enum { kInt8, kHalf, kHalfPair };
 
 constexpr __host__ __device__ uint32_t in_group(int kind) { return kind == kInt8 ? 128u : kind == kHalf ? 64u : 32u; }
@@ -17,7 +20,6 @@ typedef int tile_i32x4 __attribute__((ext_vector_type(4)));
 typedef int tile_i32x16 __attribute__((ext_vector_type(16)));
 typedef float tile_f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 tile_f16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(1))) const void tile_global_bytes;
 typedef __attribute__((address_space(3))) void tile_lds_bytes;
 
 // 32 x 32 outputs += 16 bytes of k of 64 lanes: lane l holds row l % 32, half l / 32 of 32 bytes, of both operands.
@@ -38,116 +40,161 @@ struct TileProduct<kInt8> {
     }
 };
 
-// BM x BN outputs by WM x WN wavefronts, a group of k at a time through a ring of STAGES buffers in LDS: BM rows of A, then BN of B.
-template <int KIND_, int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// BM x BN outputs by WM x WN wavefronts, a slice of ROW bytes of k at a time through a ring of STAGES buffers in LDS: BM rows of A, then BN
+// of B.
+template <int KIND_, int BM_, int BN_, int WM_, int WN_, int ROW_, int STAGES_>
 struct TileShape {
-    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, ROW = ROW_, STAGES = STAGES_;
     using Product = TileProduct<KIND>;
     using Sums = typename Product::Sums;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int kFragsM = BM / WM / 32, kFragsN = BN / WN / 32;
-    static constexpr int kStage = (BM + BN) * 128, kBytes = STAGES * kStage;
-    static constexpr int kLoads = (BM + BN) / 8 / kWaves;          // requests of a wavefront for a buffer, 8 rows each
-    static constexpr int kOnUnit = kThreads > 512 ? 1 : (int)(kLdsBytes / kBytes) * kThreads > 2048 ? 2048 / kThreads : (int)(kLdsBytes / kBytes);
-    static constexpr int kOnSimd = (kOnUnit * kThreads + 255) / 256 > 4 ? 4 : (kOnUnit * kThreads + 255) / 256;
-    static_assert((BM + BN) / 8 % kWaves == 0 && kWaves % 2 == 0 && kBytes <= (int)kLdsBytes, "requests in equal numbers");
+    static constexpr int kStage = (BM + BN) * ROW, kBytes = STAGES * kStage;
+    static constexpr int kPieces = ROW / 16, kRows = 64 / kPieces; // rows that a request of a wavefront covers
+    static constexpr int kLoadsA = BM / kRows / kWaves, kLoads = (BM + BN) / kRows / kWaves;   // requests of a wavefront for a buffer
+    static constexpr int kOnUnit = (int)kLdsBytes / kBytes;        // workgroups on a compute unit
+    static constexpr int kOnSimd = kOnUnit * kWaves / 4 < 1 ? 1 : kOnUnit * kWaves / 4 > 4 ? 4 : kOnUnit * kWaves / 4;      // wavefronts
+    static constexpr bool kPair = KIND == kHalfPair;
+    static constexpr int kStep = kPair ? 64 : 32, kSteps = ROW / kStep;        // bytes of a row that are multiplied at a time
+    static constexpr int kReads = (kFragsM + kFragsN) * (kPair ? 2 : 1), kProducts = kFragsM * kFragsN * (kPair ? 3 : 1);     // of a step
+    static_assert((ROW == 64 || ROW == 128) && kSteps % 2 == 0, "operands are read into two sets of registers in turn");
+    static_assert(BM / kRows % kWaves == 0 && BN / kRows % kWaves == 0 && kRows * kWaves % 16 == 0 && kBytes <= (int)kLdsBytes && STAGES >= 2,
+                  "requests in equal numbers");
 };
-
-// Waits until the requests of all but the newest `newer` buffers (at most N) are there.
-template <int PER, int N>
-__device__ __forceinline__ void wait_for_buffers(uint32_t newer)
-{
-    if constexpr (N > 0) {
-        if (newer < N) return wait_for_buffers<PER, N - 1>(newer);
-    }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PER * N) : "memory");
-}
 
 struct TileOperands {
-    const uint8_t *a, *b;          // rows of groups * 128 bytes
+    const uint8_t *a, *b;          // rows of groups * 128 bytes, 256 of them within 2^32 bytes
     uint32_t m, n, groups;
-    uint32_t first, trips;         // the groups of k that are summed
+    uint32_t first, count;         // the groups of k that are summed
 };
 
-// A row's 8 pieces of 16 bytes lie in a buffer in another order from row to row: piece p of row r in place p ^ tile_turn(r), so that
+// A row's pieces of 16 bytes lie in a buffer in another order from row to row: piece p of row r in place p ^ tile_turn(r), so that
 // 16 rows' pieces of the same k, which are read together, lie in 64 different banks.
-__device__ __forceinline__ uint32_t tile_turn(uint32_t row) { return row >> 1 & 7; }
+template <int ROW>
+__device__ __forceinline__ uint32_t tile_turn(uint32_t row) { return ROW == 128 ? row >> 1 & 7 : row >> 2 & 3; }
+
+// A step's operands in a wavefront's registers; of pairs, their second numbers too.
+template <class S>
+struct TileFragments {
+    tile_i32x4 a[S::kPair ? 2 : 1][S::kFragsM], b[S::kPair ? 2 : 1][S::kFragsN];
+
+    // The R-th of kReads requests, first those of the first products.
+    template <int R>
+    __device__ __forceinline__ void read(const char* rows_a, const char* rows_b, uint32_t at)
+    {
+        constexpr int low = R / (S::kFragsM + S::kFragsN), r = R % (S::kFragsM + S::kFragsN);
+        if constexpr (low) at ^= 32;
+        if constexpr (r == 0) b[low][0] = *reinterpret_cast<const tile_i32x4*>(rows_b + at);
+        else if constexpr (r <= S::kFragsM) a[low][r - 1] = *reinterpret_cast<const tile_i32x4*>(rows_a + (r - 1) * 32 * S::ROW + at);
+        else b[low][r - S::kFragsM] = *reinterpret_cast<const tile_i32x4*>(rows_b + (r - S::kFragsM) * 32 * S::ROW + at);
+    }
+    // The P-th of kProducts.  Of pairs (a + a')(b + b') but for a' b', which is 2^-22 of it.
+    template <int P>
+    __device__ __forceinline__ void product(typename S::Sums (&acc)[S::kFragsM][S::kFragsN]) const
+    {
+        constexpr int which = P / (S::kFragsM * S::kFragsN), i = P % S::kFragsM, j = P / S::kFragsM % S::kFragsN;
+        acc[i][j] = S::Product::step(b[which == 2][j], a[which == 1][i], acc[i][j]);
+    }
+};
+
+template <int N, typename F>
+__device__ __forceinline__ void repeat(F f)
+{
+    if constexpr (N > 0) {
+        repeat<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
 
 // Sums of the tile at (row0, col0).  Rows past the end repeat the last: their sums mean nothing.  A lane holds of 32 x 32 outputs
 // one row's: element e is column (e / 4) * 8 + (lane / 32) * 4 + e % 4 of row lane % 32.
+// A step's operands are read while the step before it is multiplied, one request behind a product; the first ones of the next slice in the
+// second half of a slice's last step, behind the barrier after which every wavefront is done with this slice's buffer.
 template <class S>
 __device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, uint32_t col0, char* lds,
                                           typename S::Sums (&acc)[S::kFragsM][S::kFragsN])
 {
-    using P = typename S::Product;
+#ifdef __HIP_DEVICE_COMPILE__                                      // the host's pass does not know the type of a buffer
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 31, half = lane >> 5, wm = wave / S::WN, wn = wave % S::WN;
-    const uint8_t* from[S::kLoads];
-    const uint32_t piece = (lane % 8) ^ tile_turn(wave * 8 + lane / 8);        // the same in each of a wavefront's requests
+    row0 = __builtin_amdgcn_readfirstlane(row0);                   // the same in all lanes, which divisions hide from the compiler
+    col0 = __builtin_amdgcn_readfirstlane(col0);
+    const uint64_t stride = (uint64_t)g.groups * 128;
+    const uint32_t trips = g.count * (128 / S::ROW);
+    uint32_t from[S::kLoads];
+    const uint32_t piece = (lane % S::kPieces) ^ tile_turn<S::ROW>(wave * S::kRows + lane / S::kPieces);       // in each of a wavefront's requests
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
-        const uint32_t c = i * S::kWaves + wave;                   // A's rows first
-        const bool is_a = c < S::BM / 8;
-        const uint32_t row = (is_a ? c : c - S::BM / 8) * 8 + lane / 8;
-        from[i] = (is_a ? g.a : g.b) + ((uint64_t)(is_a ? min(row0 + row, g.m - 1) : min(col0 + row, g.n - 1)) * g.groups + g.first) * 128 + piece * 16;
+        const bool is_a = i < S::kLoadsA;                          // A's rows first
+        const uint32_t row = (i * S::kWaves + wave) * S::kRows - (is_a ? 0 : S::BM) + lane / S::kPieces;
+        from[i] = min(row, (is_a ? g.m - row0 : g.n - col0) - 1) * (uint32_t)stride + piece * 16;
     }
-    auto fetch = [&](uint32_t t, uint32_t stage) {
-#pragma unroll
-        for (int i = 0; i < S::kLoads; ++i)
-            __builtin_amdgcn_global_load_lds((tile_global_bytes*)(from[i] + (uint64_t)t * 128),
-                                             (tile_lds_bytes*)(lds + stage * S::kStage + (i * S::kWaves + wave) * 1024), 16, 0, 0);
+    // The slices behind the last are requested with a length of 0 in place of the operands': nothing is read, and every trip is alike.
+    auto fetch_one = [&](auto I, uint32_t t, uint32_t stage) {
+        constexpr int i = decltype(I)::value;
+        // buffer addressing: a lane's place in the tile is a 32-bit number, and what all lanes share a scalar
+        const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(i < S::kLoadsA ? g.a + row0 * stride : g.b + col0 * stride), 0,
+                                                          __builtin_amdgcn_readfirstlane(t < trips ? -1 : 0), 0x20000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(of, (tile_lds_bytes*)(lds + stage * S::kStage + (i * S::kWaves + wave) * 1024), 16, from[i],
+                                                 g.first * 128 + t * S::ROW, 0, 0);
     };
+#pragma unroll
+    for (uint32_t t = 0; t < S::STAGES; ++t) repeat<S::kLoads>([&](auto I) { fetch_one(I, t, t); });
 #pragma unroll
     for (int i = 0; i < S::kFragsM; ++i)
 #pragma unroll
         for (int j = 0; j < S::kFragsN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    const uint32_t ra = wm * S::kFragsM * 32 + r, rb = S::BM + wn * S::kFragsN * 32 + r;
-#pragma unroll
-    for (uint32_t t = 0; t < S::STAGES - 1; ++t)
-        if (t < g.trips) fetch(t, t);
-    uint32_t stage = 0, free_stage = S::STAGES - 1;
-    for (uint32_t t = 0; t < g.trips; ++t) {
-        // this trip's requests are there, and every wavefront is done with the buffer that is filled next
-        wait_for_buffers<S::kLoads, S::STAGES - 2>(g.trips - 1 - t);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + S::STAGES - 1 < g.trips) fetch(t + S::STAGES - 1, free_stage);
+    const uint32_t rows_a = (wm * S::kFragsM * 32 + r) * S::ROW, rows_b = (S::BM + wn * S::kFragsN * 32 + r) * S::ROW;
+    const uint32_t first_piece = (half ^ tile_turn<S::ROW>(lane)) * 16;        // of step 0
+    auto read = [&](TileFragments<S>& f, auto R, const char* base, int s) {
+        f.template read<decltype(R)::value>(base + rows_a, base + rows_b, first_piece ^ (S::kStep * s));
+    };
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::kLoads * (S::STAGES - 1)) : "memory");
+    TileFragments<S> now[2];
+    repeat<S::kReads>([&](auto R) { read(now[0], R, lds, 0); });
+    constexpr int kHalfway = S::kProducts / 2, kLeft = S::kProducts - kHalfway;
+    constexpr int kReadsEach = (2 * S::kReads + kLeft - 1) / kLeft, kLoadsEach = (S::kLoads + kLeft - 1) / kLeft;
+    uint32_t stage = 0;
+    for (uint32_t t = 0; t < trips; ++t) {
         const char* base = lds + stage * S::kStage;
-        auto read = [&](uint32_t row, int s) {
-            return *reinterpret_cast<const tile_i32x4*>(base + row * 128 + ((2 * s + half) ^ tile_turn(lane)) * 16);
-        };
-        constexpr int kSteps = S::KIND == kHalfPair ? 2 : 4;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            tile_i32x4 a[S::kFragsM], b[S::kFragsN];
-#pragma unroll
-            for (int i = 0; i < S::kFragsM; ++i) a[i] = read(ra + i * 32, s);
-#pragma unroll
-            for (int j = 0; j < S::kFragsN; ++j) b[j] = read(rb + j * 32, s);
-            if constexpr (S::KIND == kHalfPair) {                  // (a + a')(b + b') but for a' b', which is 2^-22 of it
-                tile_i32x4 low[S::kFragsN > S::kFragsM ? S::kFragsN : S::kFragsM];
-#pragma unroll
-                for (int j = 0; j < S::kFragsN; ++j) low[j] = read(rb + j * 32, s + 2);
-#pragma unroll
-                for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-                    for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = P::step(low[j], a[i], acc[i][j]);
-#pragma unroll
-                for (int i = 0; i < S::kFragsM; ++i) low[i] = read(ra + i * 32, s + 2);
-#pragma unroll
-                for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-                    for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = P::step(b[j], low[i], acc[i][j]);
-            }
-#pragma unroll
-            for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::kFragsN; ++j) acc[i][j] = P::step(b[j], a[i], acc[i][j]);
-        }
-        free_stage = stage;
-        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        repeat<S::kSteps - 1>([&](auto I) {
+            constexpr int s = decltype(I)::value;
+            repeat<S::kProducts>([&](auto P) {
+                now[s & 1].template product<decltype(P)::value>(acc);
+                constexpr int each = (S::kReads + S::kProducts - 1) / S::kProducts;
+                repeat<each>([&](auto R) {
+                    constexpr int at = decltype(P)::value * each + decltype(R)::value;
+                    if constexpr (at < S::kReads) read(now[~s & 1], std::integral_constant<int, at>{}, base, s + 1);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        TileFragments<S>& last = now[(S::kSteps - 1) & 1];
+        const uint32_t next = stage + 1 == S::STAGES ? 0 : stage + 1;
+        repeat<kHalfway>([&](auto P) { last.template product<decltype(P)::value>(acc); });
+        __builtin_amdgcn_sched_barrier(0);
+        // the next slice is there, and every wavefront has read this one
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(S::kLoads * (S::STAGES - 2)) : "memory");
+        const char* after = lds + next * S::kStage;
+        repeat<kLeft>([&](auto Q) {
+            constexpr int q = decltype(Q)::value;
+            last.template product<kHalfway + q>(acc);
+            repeat<kReadsEach>([&](auto R) {
+                constexpr int at = q * kReadsEach + decltype(R)::value;
+                if constexpr (at < S::kReads) read(now[0], std::integral_constant<int, at>{}, after, 0);
+            });
+            repeat<kLoadsEach>([&](auto I) {
+                constexpr int at = q * kLoadsEach + decltype(I)::value;
+                if constexpr (at < S::kLoads) fetch_one(std::integral_constant<int, at>{}, t + S::STAGES, stage);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        stage = next;
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // nothing is on its way to LDS any more
+#endif
 }
 
 // f(row, column of the first, 8 sums side by side) for all of this lane's sums of the tile.
