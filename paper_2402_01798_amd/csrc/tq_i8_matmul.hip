@@ -1,4 +1,4 @@
-// Products of matrices of 8-bit integers (tq_i8.h): out = A B^T (+ bias).
+// Products of matrices of 8-bit integers (tq_i8.h): out = A B^T (+ bias), and linear layers whose tokens are cast inside.
 #include <type_traits>
 
 #include "tq_i8_device.h"
@@ -8,37 +8,224 @@ namespace tq {
 namespace {
 
 struct I8MatmulArgs {
+    const void* x;                 // tokens that are not in 8-bit form yet, in place of a and sa
     const uint8_t *a, *b;
     const float *sa, *sb, *bias;
     void* out;
-    uint64_t ldo;
-    uint32_t m, n, groups;
+    uint64_t ldx, ldo;
+    uint32_t m, n, k, groups;
     uint32_t tiles_x, tiles_y, tiles;
+    uint32_t splits;               // of k, over workgroups
+    int* partial;                  // [splits][m][n]
 };
+
+// Of 8 sums of a row from column `col` on.
+template <int DTYPE>
+__device__ __forceinline__ void store_scaled(const I8MatmulArgs& g, uint32_t row, uint32_t col, const int (&sums)[8])
+{
+    const int n = (int)min(g.n - col, 8u);
+    const float sa = g.sa[row];
+    float sb[8], bias[8], v[8];
+    load8<TQ_F32>(g.sb + col, n, sb);
+    if (g.bias) load8<TQ_F32>(g.bias + col, n, bias);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = (float)sums[e] * sa * sb[e];
+        if (g.bias) v[e] += bias[e];
+    }
+    store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + row * g.ldo + col, n, v);
+}
 
 template <int DTYPE, class S>
 __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void i8_tile_kernel(I8MatmulArgs g)
 {
     extern __shared__ char lds[];
     uint32_t tile, ty, tx;
-    if (!tile_number(linear_block(), g.tiles, tile)) return;
-    tile_place(tile, g.tiles_y, g.tiles_x, ty, tx);
+    if (!tile_number(linear_block(), g.tiles * g.splits, tile)) return;
+    const uint32_t split = tile / g.tiles, each = (g.groups + g.splits - 1) / g.splits, first = min(split * each, g.groups);
+    tile_place(tile - split * g.tiles, g.tiles_y, g.tiles_x, ty, tx);
     typename S::Sums acc[S::kFragsM][S::kFragsN];
-    tile_sums<S>(TileOperands{g.a, g.b, g.m, g.n, g.groups, 0, g.groups}, ty * S::BM, tx * S::BN, lds, acc);
+    tile_sums<S>(TileOperands{g.a, g.b, g.m, g.n, g.groups, first, min(each, g.groups - first)}, ty * S::BM, tx * S::BN, lds, acc);
     tile_chunks<S>(acc, ty * S::BM, tx * S::BN, [&](uint32_t row, uint32_t col, const int (&sums)[8]) {
         if (row >= g.m || col >= g.n) return;
-        const int n = (int)min(g.n - col, 8u);
-        const float sa = g.sa[row];
-        float sb[8], bias[8], v[8];
-        load8<TQ_F32>(g.sb + col, n, sb);
-        if (g.bias) load8<TQ_F32>(g.bias + col, n, bias);
+        if (g.splits == 1) return store_scaled<DTYPE>(g, row, col, sums);
+        float bits[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = (float)sums[e] * sa * sb[e];
-            if (g.bias) v[e] += bias[e];
-        }
-        store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + row * g.ldo + col, n, v);
+        for (int e = 0; e < 8; ++e) bits[e] = __int_as_float(sums[e]);
+        store8<TQ_F32>(reinterpret_cast<float*>(g.partial) + ((uint64_t)split * g.m + row) * g.n + col, (int)min(g.n - col, 8u), bits);
     });
+}
+
+// The splits' sums, joined: whole numbers, so in any order.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void i8_join_kernel(I8MatmulArgs g)
+{
+    const uint32_t chunks = (g.n + 7) / 8;
+    const uint64_t at = (uint64_t)linear_block() * 256 + threadIdx.x, row = at / chunks;
+    if (row >= g.m) return;
+    const uint32_t col = (uint32_t)(at - row * chunks) * 8;
+    const int n = (int)min(g.n - col, 8u);
+    int sums[8] = {};
+    for (uint32_t s = 0; s < g.splits; ++s) {
+        float bits[8];
+        load8<TQ_F32>(reinterpret_cast<const float*>(g.partial) + (s * (uint64_t)g.m + row) * g.n + col, n, bits);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[e] += __float_as_int(bits[e]);
+    }
+    store_scaled<DTYPE>(g, (uint32_t)row, col, sums);
+}
+
+// Few rows of A, FRAGS x 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds it.
+// B comes through a ring of STAGES buffers for each wavefront, 128 bytes of k at a time.  A, by HOW: in the same ring (kStream); whole into
+// LDS, where it is small (kKept); or cast there by every workgroup, from type HOW (0 ..).
+enum { kStream = -2, kKept = -1 };
+
+template <int HOW, int FRAGS, int WAVES, int STAGES>
+struct Few {
+    static constexpr int kBlocksA = HOW == kStream ? FRAGS : 0;    // blocks of 32 rows in a buffer, A's before B's
+    static constexpr int kStage = (kBlocksA + 1) * 4096, kLoads = (kBlocksA + 1) * 4;
+    static constexpr int kRing = WAVES * STAGES * kStage, kSums = WAVES * FRAGS * 32 * 33 * 4;
+    static_assert(kRing <= (int)kLdsBytes && (HOW == kStream || FRAGS == 1), "rows that are kept are few");
+};
+
+__host__ __device__ constexpr uint64_t kept_row(uint64_t groups) { return groups * 128 + 16; }    // 16 more: rows in different banks
+
+template <class S>
+constexpr uint64_t few_bytes(uint64_t kept) { return S::kRing + kept > (uint64_t)S::kSums ? S::kRing + kept : S::kSums; }
+
+template <int DTYPE, int HOW, int FRAGS, int WAVES, int STAGES>
+__global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
+{
+#ifdef __HIP_DEVICE_COMPILE__                                      // the host's pass does not know the type of a buffer
+    using S = Few<HOW, FRAGS, WAVES, STAGES>;
+    using P = TileProduct<kInt8>;
+    extern __shared__ char lds[];
+    const uint32_t tx = linear_block();
+    if (tx >= g.tiles) return;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
+    const uint32_t col0 = tx * 32, per = (g.groups + WAVES - 1) / WAVES, first = min(wave * per, g.groups), trips = min(per, g.groups - first);
+    const uint64_t stride = (uint64_t)g.groups * 128;
+    char* ring = lds + wave * (STAGES * S::kStage);
+    char* kept = lds + S::kRing;
+    float* kept_scales = reinterpret_cast<float*>(kept + g.m * kept_row(g.groups));
+    // Rows past the end repeat the last.  A request covers 8 rows; pieces of 16 bytes lie as in tiles.
+    uint32_t from[S::kLoads];
+#pragma unroll
+    for (int i = 0; i < S::kLoads; ++i) {
+        const bool is_a = i < 4 * S::kBlocksA;
+        const uint32_t row = (is_a ? i : i - 4 * S::kBlocksA) * 8 + lane / 8;
+        from[i] = min(row, (is_a ? g.m : g.n - col0) - 1) * (uint32_t)stride + ((lane & 7) ^ tile_turn<128>(i * 8 + lane / 8)) * 16;
+    }
+    auto fetch = [&](uint32_t t, uint32_t stage) {
+        const int some = __builtin_amdgcn_readfirstlane(t < trips ? -1 : 0);        // of length 0 behind the last
+        const auto of_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.b) + col0 * stride, 0, some, 0x20000);
+        const auto of_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.a), 0, some, 0x20000);
+#pragma unroll
+        for (int i = 0; i < S::kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 * S::kBlocksA ? of_a : of_b, (tile_lds_bytes*)(ring + stage * S::kStage + i * 1024), 16,
+                                                     from[i], (first + t) * 128, 0, 0);
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < STAGES; ++t) fetch(t, t);
+
+    if constexpr (HOW == kKept) {
+        for (uint32_t row = wave; row < g.m; row += WAVES)
+            for (uint32_t i = lane; i < g.groups * 8; i += 64)
+                *reinterpret_cast<u32x4*>(kept + row * kept_row(g.groups) + i * 16) = *reinterpret_cast<const u32x4*>(g.a + row * stride + i * 16);
+        __syncthreads();
+    } else if constexpr (HOW >= 0) {                               // a wavefront casts a row, 16 requests of a lane on their way together
+        using T = typename Element<HOW>::type;
+        constexpr int kAhead = HOW == TQ_F32 ? 8 : 16;
+        const uint32_t octs = g.groups * 16;
+        for (uint32_t row = wave; row < g.m; row += WAVES) {
+            const T* x = static_cast<const T*>(g.x) + row * g.ldx;
+            auto load = [&](Eight<HOW>& e, uint32_t oct) {
+                const int64_t n = (int64_t)g.k - (int64_t)oct * 8;
+                if (n >= 8) e.load(x + (uint64_t)oct * 8);
+                else if (n > 0) e.load(x + (uint64_t)oct * 8, (int)n);
+                else e.clear();
+            };
+            Eight<HOW> w[kAhead];
+            uint32_t largest = 0;
+            for (uint32_t o = 0; o < octs; o += kAhead * 64) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) load(w[i], o + i * 64 + lane);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) largest = max(largest, w[i].largest());
+            }
+            const I8Row s(wave_largest(largest));
+            if (lane == 0) kept_scales[row] = s.scale;
+            for (uint32_t o = 0; o < octs; o += kAhead * 64) {
+                if (octs > kAhead * 64) {                          // a longer row is read again
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) load(w[i], o + i * 64 + lane);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    float v[8];
+                    w[i].unpack(v);
+                    if (o + i * 64 + lane < octs) *reinterpret_cast<u32x2*>(kept + row * kept_row(g.groups) + (o + i * 64 + lane) * 8) = s.codes(v);
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    const char* mine = kept + min(r, g.m - 1) * kept_row(g.groups) + half * 16;
+    P::Sums acc[FRAGS];
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[f][e] = 0;
+    uint32_t stage = 0;
+    for (uint32_t t = 0; t < trips; ++t) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(S::kLoads * (STAGES - 1)) : "memory");
+        const char* base = ring + stage * S::kStage;
+        tile_i32x4 a[FRAGS][4], b[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint32_t at = r * 128 + ((2 * s + half) ^ tile_turn<128>(r)) * 16;
+            b[s] = *reinterpret_cast<const tile_i32x4*>(base + S::kBlocksA * 4096 + at);
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f)
+                a[f][s] = *reinterpret_cast<const tile_i32x4*>(HOW == kStream ? base + f * 4096 + at : mine + (first + t) * 128 + s * 32);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
+        fetch(t + STAGES, stage);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) acc[f] = P::step(a[f][s], b[s], acc[f]);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    float scales[4 * FRAGS];                                       // of the rows that this thread joins below
+    constexpr int kEach = FRAGS * 32 * 32 / (WAVES * 64);
+    static_assert(kEach <= 4 * FRAGS, "outputs of a thread");
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const uint32_t row = min((threadIdx.x + u * WAVES * 64) / 32, g.m - 1);
+        scales[u] = HOW >= 0 ? kept_scales[row] : g.sa[row];
+    }
+    __syncthreads();                                               // the rings and what is kept behind them are done with
+    int* sums = reinterpret_cast<int*>(lds);
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[((wave * FRAGS + f) * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[f][e];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const uint32_t i = threadIdx.x + u * WAVES * 64, row = i / 32, col = i & 31;
+        if (row >= g.m || col0 + col >= g.n) continue;
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += sums[(w * FRAGS * 32 + row) * 33 + col];
+        float v = (float)sum * scales[u] * g.sb[col0 + col];
+        if (g.bias) v += g.bias[col0 + col];
+        static_cast<typename Element<DTYPE>::type*>(g.out)[row * g.ldo + col0 + col] = Element<DTYPE>::store(v);
+    }
+#endif
 }
 
 template <int DTYPE, class S>
@@ -46,7 +233,7 @@ hipError_t launch_tiles(I8MatmulArgs& g, hipStream_t st)
 {
     const uint64_t x = ((uint64_t)g.n + S::BN - 1) / S::BN, y = ((uint64_t)g.m + S::BM - 1) / S::BM;
     dim3 grid;
-    if (x * y > 0xFFFFFFF0ull || !fold_grid((x * y + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
+    if (x * y * g.splits > 0xFFFFFFF0ull || !fold_grid((x * y * g.splits + 7) / 8 * 8, S::kThreads, 1, grid)) return hipErrorInvalidValue;
     g.tiles_x = (uint32_t)x;
     g.tiles_y = (uint32_t)y;
     g.tiles = (uint32_t)(x * y);
@@ -54,16 +241,88 @@ hipError_t launch_tiles(I8MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int DTYPE, int HOW, int FRAGS, int WAVES, int STAGES>
+hipError_t launch_few(I8MatmulArgs& g, hipStream_t st)
+{
+    using S = Few<HOW, FRAGS, WAVES, STAGES>;
+    g.tiles = (g.n + 31) / 32;
+    dim3 grid;
+    if (!fold_grid(g.tiles, WAVES * 64, 1, grid)) return hipErrorInvalidValue;
+    const uint64_t kept = HOW == kStream ? 0 : g.m * kept_row(g.groups) + g.m * 4;
+    i8_few_kernel<DTYPE, HOW, FRAGS, WAVES, STAGES><<<grid, WAVES * 64, few_bytes<S>(kept), st>>>(g);
+    return hipGetLastError();
+}
+
+constexpr uint64_t kKeptBytes = 30 << 10;      // of A in LDS, beside rings of 64 or 128 KiB
+
+enum Shape { kFewShape, k256, k192, k256x128, k128x256, k128, k64 };
+
+// A tile's sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute unit, and what
+// a round of them costs beside that.
+struct Pace {
+    Shape shape;
+    uint64_t bm, bn;
+    uint32_t ns[3], round;
+};
+constexpr Pace kPaces[] = {{k256, 256, 256, {1553, 0, 0}, 12000},   {k192, 192, 192, {943, 0, 0}, 9000},      {k256x128, 256, 128, {853, 0, 0}, 9000},
+                           {k128x256, 128, 256, {870, 0, 0}, 9000}, {k128, 128, 128, {580, 925, 0}, 8000}, {k64, 64, 64, {262, 375, 560}, 3500}};
+
+uint64_t pace(const Pace& p, uint64_t m, uint64_t n, uint64_t groups)
+{
+    const uint64_t tiles = (m + p.bm - 1) / p.bm * ((n + p.bn - 1) / p.bn), each = (tiles + kComputeUnits - 1) / kComputeUnits;
+    const uint64_t fit = p.ns[2] ? 3 : p.ns[1] ? 2 : 1, rest = each % fit;
+    return each / fit * (p.ns[fit - 1] * groups + p.round) + (rest ? p.ns[rest - 1] * groups + p.round : 0);
+}
+
+Shape shape_of(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (m <= 32) return kFewShape;
+    const Pace* best = kPaces;
+    for (const Pace& p : kPaces)
+        if (pace(p, m, n, groups) < pace(*best, m, n, groups)) best = &p;
+    return best->shape;
+}
+
+// Over how many workgroups k is split where few tiles of 64 leave compute units idle.
+uint32_t splits_of(uint64_t m, uint64_t n, uint64_t groups)
+{
+    if (shape_of(m, n, groups) != k64) return 1;
+    const uint64_t tiles = (m + 63) / 64 * ((n + 63) / 64), most = 2 * kComputeUnits / tiles, wanted = groups / 8, s = wanted < most ? wanted : most;
+    return s > 1 && (groups - groups / s) * kPaces[5].ns[0] >= 6000 ? (uint32_t)s : 1;
+}
+
 template <int DTYPE>
 hipError_t launch_matmul(I8MatmulArgs& g, hipStream_t st)
 {
-    return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 2, 64, 5>>(g, st);
+    g.splits = splits_of(g.m, g.n, g.groups);
+    switch (shape_of(g.m, g.n, g.groups)) {
+        case kFewShape:
+            if (g.m * kept_row(g.groups) <= kKeptBytes)
+                return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kKept, 1, 8, 4>(g, st) : launch_few<DTYPE, kKept, 1, 4, 3>(g, st);
+            return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kStream, 1, 8, 2>(g, st) : launch_few<DTYPE, kStream, 1, 4, 2>(g, st);
+        case k256: return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 4, 128, 2>>(g, st);
+        case k192: return launch_tiles<DTYPE, TileShape<kInt8, 192, 192, 2, 6, 128, 3>>(g, st);
+        case k256x128: return launch_tiles<DTYPE, TileShape<kInt8, 256, 128, 4, 2, 128, 3>>(g, st);
+        case k128x256: return launch_tiles<DTYPE, TileShape<kInt8, 128, 256, 2, 4, 128, 3>>(g, st);
+        case k128: return launch_tiles<DTYPE, TileShape<kInt8, 128, 128, 2, 4, 128, 2>>(g, st);
+        case k64: break;
+    }
+    const hipError_t e = launch_tiles<DTYPE, TileShape<kInt8, 64, 64, 2, 2, 128, 3>>(g, st);
+    if (e != hipSuccess || g.splits == 1) return e;
+    dim3 grid;
+    if (!fold_grid(((uint64_t)g.m * ((g.n + 7) / 8) + 255) / 256, 256, 1, grid)) return hipErrorInvalidValue;
+    i8_join_kernel<DTYPE><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
 }  // namespace
 }  // namespace tq
 
-uint64_t tq_i8_matmul_workspace_bytes_impl(uint64_t, uint64_t, uint64_t) { return 0; }
+uint64_t tq_i8_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint32_t s = tq::splits_of(m, n, (k + 127) / 128);
+    return s == 1 ? 0 : s * m * n * sizeof(int);
+}
 
 hipError_t tq_launch_i8_matmul(const void* a, const float* sa, const void* b, const float* sb, uint64_t m, uint64_t n, uint64_t k,
                                const float* bias, void* out, int dtype, uint64_t ldo, void* workspace, hipStream_t st)
@@ -79,7 +338,42 @@ hipError_t tq_launch_i8_matmul(const void* a, const float* sa, const void* b, co
     g.ldo = ldo;
     g.m = (uint32_t)m;
     g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
     g.groups = (uint32_t)((k + 127) / 128);
+    g.partial = static_cast<int*>(workspace);
     if (dtype == TQ_F32) return launch_matmul<TQ_F32>(g, st);
     return dtype == TQ_BF16 ? launch_matmul<TQ_BF16>(g, st) : launch_matmul<TQ_F16>(g, st);
+}
+
+bool tq_i8_linear_in_one(uint64_t m, uint64_t n, uint64_t k)
+{
+    return m <= 8 && m * tq::kept_row((k + 127) / 128) <= tq::kKeptBytes;
+}
+
+hipError_t tq_launch_i8_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const float* sw, uint64_t n, uint64_t k,
+                                   const float* bias, void* out, int dtype, uint64_t ldo, hipStream_t st)
+{
+    using namespace tq;
+    I8MatmulArgs g = {};
+    g.x = x;
+    g.ldx = ldx;
+    g.b = static_cast<const uint8_t*>(w);
+    g.sb = sw;
+    g.bias = bias;
+    g.out = out;
+    g.ldo = ldo;
+    g.m = (uint32_t)m;
+    g.n = (uint32_t)n;
+    g.k = (uint32_t)k;
+    g.groups = (uint32_t)((k + 127) / 128);
+    auto as = [&](auto D, auto X) {
+        constexpr int T = decltype(D)::value, F = decltype(X)::value;
+        return g.n <= 32 * kComputeUnits ? launch_few<T, F, 1, 8, 4>(g, st) : launch_few<T, F, 1, 4, 3>(g, st);
+    };
+    auto from = [&](auto D) {
+        if (x_dtype == TQ_F32) return as(D, std::integral_constant<int, TQ_F32>{});
+        return x_dtype == TQ_BF16 ? as(D, std::integral_constant<int, TQ_BF16>{}) : as(D, std::integral_constant<int, TQ_F16>{});
+    };
+    if (dtype == TQ_F32) return from(std::integral_constant<int, TQ_F32>{});
+    return dtype == TQ_BF16 ? from(std::integral_constant<int, TQ_BF16>{}) : from(std::integral_constant<int, TQ_F16>{});
 }

@@ -19,6 +19,9 @@ hipError_t tq_launch_i8_dequantize(const void* codes, const float* scales, uint6
 uint64_t tq_i8_matmul_workspace_bytes_impl(uint64_t m, uint64_t n, uint64_t k);
 hipError_t tq_launch_i8_matmul(const void* a, const float* sa, const void* b, const float* sb, uint64_t m, uint64_t n, uint64_t k,
                                const float* bias, void* out, int dtype, uint64_t ldo, void* workspace, hipStream_t st);
+bool tq_i8_linear_in_one(uint64_t m, uint64_t n, uint64_t k);
+hipError_t tq_launch_i8_linear_few(const void* x, int x_dtype, uint64_t m, uint64_t ldx, const void* w, const float* sw, uint64_t n, uint64_t k,
+                                   const float* bias, void* out, int dtype, uint64_t ldo, hipStream_t st);
 uint64_t tq_orth_workspace_bytes_impl(uint64_t rows, uint64_t cols, int count, int precision);
 hipError_t tq_launch_orth(const void* const* g, int count, int dtype, uint64_t rows, uint64_t cols, float eta, float momentum, int nesterov,
                           float weight_decay, float scale, int steps, const float* coefficients, int precision, float eps,
@@ -154,7 +157,7 @@ int tq_i8_matmul(const void* a_codes_dev, const float* a_scales_dev, const void*
 
 uint64_t tq_i8_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k)
 {
-    if (check_product(m, n, k)) return 0;
+    if (check_product(m, n, k) || tq_i8_linear_in_one(m, n, k)) return 0;
     return padded(tq_i8_code_bytes(m, k)) + padded(4 * m) + tq_i8_matmul_workspace_bytes_impl(m, n, k);
 }
 
@@ -169,6 +172,8 @@ int tq_i8_linear(const void* x_dev, int dtype, uint64_t m, uint64_t ldx, const v
     if (!aligned(bias_dev, 4)) return TQ_EALIGN;
     if ((rc = check_workspace(workspace_dev, workspace_bytes, tq_i8_linear_workspace_bytes(m, n, k)))) return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (tq_i8_linear_in_one(m, n, k))
+        return from_hip(tq_launch_i8_linear_few(x_dev, dtype, m, ldx, w_codes_dev, w_scales_dev, n, k, bias_dev, out_dev, out_dtype, ldo, st));
     char* codes = static_cast<char*>(workspace_dev);
     float* scales = reinterpret_cast<float*>(codes + padded(tq_i8_code_bytes(m, k)));
     if ((rc = from_hip(tq_launch_i8_quantize(x_dev, dtype, m, k, ldx, codes, scales, st)))) return rc;

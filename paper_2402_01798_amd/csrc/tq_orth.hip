@@ -349,7 +349,7 @@ hipError_t launch_begin(const OrthCall& q, const OrthPointers& p, OrthArgs& o, h
 template <int KIND>
 hipError_t launch_orth(const OrthCall& q, hipStream_t st)
 {
-    using Square = std::conditional_t<KIND == kHalf, TileShape<KIND, 256, 256, 2, 2, 64, 5>, TileShape<KIND, 128, 128, 2, 2, 128, 2>>;
+    using Square = std::conditional_t<KIND == kHalf, TileShape<KIND, 256, 256, 2, 4, 128, 2>, TileShape<KIND, 128, 128, 2, 2, 128, 2>>;
     const Layout l = layout(q.rows, q.cols, KIND);
     const bool flip = q.rows > q.cols;
     const uint32_t r = (uint32_t)(flip ? q.cols : q.rows), c = (uint32_t)(flip ? q.rows : q.cols);
