@@ -116,6 +116,8 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
         const uint32_t row = (is_a ? i : i - 4 * S::kBlocksA) * 8 + lane / 8;
         from[i] = min(row, (is_a ? g.m : g.n - col0) - 1) * (uint32_t)stride + ((lane & 7) ^ tile_turn<128>(i * 8 + lane / 8)) * 16;
     }
+    const uint32_t turned = trips ? tx % trips : 0;                // workgroups begin at different places
+    auto group_of = [&](uint32_t t) { return first + (t + turned < trips ? t + turned : t + turned - trips); };
     auto fetch = [&](uint32_t t, uint32_t stage) {
         const int some = __builtin_amdgcn_readfirstlane(t < trips ? -1 : 0);        // of length 0 behind the last
         const auto of_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.b) + col0 * stride, 0, some, 0x20000);
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
 #pragma unroll
         for (int i = 0; i < S::kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(i < 4 * S::kBlocksA ? of_a : of_b, (tile_lds_bytes*)(ring + stage * S::kStage + i * 1024), 16,
-                                                     from[i], (first + t) * 128, 0, 0);
+                                                     from[i], group_of(t) * 128, 0, 0);
     };
 #pragma unroll
     for (uint32_t t = 0; t < STAGES; ++t) fetch(t, t);
@@ -133,38 +135,48 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
             for (uint32_t i = lane; i < g.groups * 8; i += 64)
                 *reinterpret_cast<u32x4*>(kept + row * kept_row(g.groups) + i * 16) = *reinterpret_cast<const u32x4*>(g.a + row * stride + i * 16);
         __syncthreads();
-    } else if constexpr (HOW >= 0) {                               // a wavefront casts a row, 16 requests of a lane on their way together
+    } else if constexpr (HOW >= 0) {                               // rows side by side, each by `team` wavefronts
         using T = typename Element<HOW>::type;
-        constexpr int kAhead = HOW == TQ_F32 ? 8 : 16;
-        const uint32_t octs = g.groups * 16;
-        for (uint32_t row = wave; row < g.m; row += WAVES) {
-            const T* x = static_cast<const T*>(g.x) + row * g.ldx;
+        constexpr int kAhead = HOW == TQ_F32 ? 8 : 16;             // requests of a lane on their way together
+        __shared__ uint32_t part[2][WAVES];
+        const uint32_t octs = g.groups * 16, team = g.m == 1 ? WAVES : g.m == 2 ? WAVES / 2 : g.m <= 4 ? WAVES / 4 : 1, at_once = WAVES / team;
+        const uint32_t me = wave % team * 64 + lane, step = team * 64;
+        for (uint32_t turn = 0; turn * at_once < g.m; ++turn) {
+            const uint32_t row = turn * at_once + wave / team;
+            const bool some = row < g.m;                           // wavefronts without a row meet the others at the barrier
+            const T* x = static_cast<const T*>(g.x) + min(row, g.m - 1) * g.ldx;
             auto load = [&](Eight<HOW>& e, uint32_t oct) {
-                const int64_t n = (int64_t)g.k - (int64_t)oct * 8;
+                const int64_t n = some ? (int64_t)g.k - (int64_t)oct * 8 : 0;
                 if (n >= 8) e.load(x + (uint64_t)oct * 8);
                 else if (n > 0) e.load(x + (uint64_t)oct * 8, (int)n);
                 else e.clear();
             };
             Eight<HOW> w[kAhead];
             uint32_t largest = 0;
-            for (uint32_t o = 0; o < octs; o += kAhead * 64) {
+            for (uint32_t o = 0; o < octs; o += kAhead * step) {
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) load(w[i], o + i * 64 + lane);
+                for (int i = 0; i < kAhead; ++i) load(w[i], o + i * step + me);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) largest = max(largest, w[i].largest());
             }
-            const I8Row s(wave_largest(largest));
-            if (lane == 0) kept_scales[row] = s.scale;
-            for (uint32_t o = 0; o < octs; o += kAhead * 64) {
-                if (octs > kAhead * 64) {                          // a longer row is read again
+            largest = wave_largest(largest);
+            if (lane == 0) part[turn & 1][wave] = largest;
+            __syncthreads();
+            for (uint32_t v = 0; v < team; ++v) largest = max(largest, part[turn & 1][wave / team * team + v]);
+            const I8Row s(largest);
+            if (some && me == 0) kept_scales[row] = s.scale;
+            for (uint32_t o = 0; o < octs; o += kAhead * step) {
+                if (octs > kAhead * step) {                        // a longer row is read again
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) load(w[i], o + i * 64 + lane);
+                    for (int i = 0; i < kAhead; ++i) load(w[i], o + i * step + me);
                 }
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
+                    const uint32_t oct = o + i * step + me;
+                    if (!some || oct >= octs) continue;
                     float v[8];
                     w[i].unpack(v);
-                    if (o + i * 64 + lane < octs) *reinterpret_cast<u32x2*>(kept + row * kept_row(g.groups) + (o + i * 64 + lane) * 8) = s.codes(v);
+                    *reinterpret_cast<u32x2*>(kept + row * kept_row(g.groups) + oct * 8) = s.codes(v);
                 }
             }
         }
@@ -188,7 +200,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
             b[s] = *reinterpret_cast<const tile_i32x4*>(base + S::kBlocksA * 4096 + at);
 #pragma unroll
             for (int f = 0; f < FRAGS; ++f)
-                a[f][s] = *reinterpret_cast<const tile_i32x4*>(HOW == kStream ? base + f * 4096 + at : mine + (first + t) * 128 + s * 32);
+                a[f][s] = *reinterpret_cast<const tile_i32x4*>(HOW == kStream ? base + f * 4096 + at : mine + group_of(t) * 128 + s * 32);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
         fetch(t + STAGES, stage);
@@ -253,7 +265,21 @@ hipError_t launch_few(I8MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
-constexpr uint64_t kKeptBytes = 30 << 10;      // of A in LDS, beside rings of 64 or 128 KiB
+constexpr uint64_t kKeptBytes = 30 << 10;      // of A in LDS, beside rings of 48 or 64 KiB
+
+// Few rows, wavefronts x buffers, us of a linear layer in bf16 (the cast of A with it):
+//   m x n x k            8 x 4    8 x 2    4 x 2    4 x 3    4 x 4
+//   1 x 4096 x 4096        7.7      7.4      7.6      7.7      7.8
+//   1 x 8192 x 8064       15.1     15.4     15.9     15.9     16.0
+//   1 x 8192 x 8192       19.4     16.7     16.3     16.6     16.6     rows a power of two apart wait for each other: fewer of them are
+//   1 x 4096 x 16384      17.9     16.3     16.9     16.9     17.1     asked for at a time
+//   1 x 14336 x 4096               11.9     11.3     11.1     11.5     two workgroups or more on a unit
+//   1 x 14336 x 8192               22.3     23.0     22.7     22.2
+// and of rows that come with B:
+//   24 x 4096 x 4096              10.2     10.2     10.1     10.2
+//   24 x 14336 x 4096             16.8     14.0     15.5     15.9
+//   24 x 8192 x 8192              21.7     17.4     17.8     18.0
+// Requests of 1024 bytes of one row, with a barrier for every 32 rows of that, took as long or longer (8192 x 8192 19.4, 14336 x 4096 14.1).
 
 enum Shape { kFewShape, k256, k192, k256x128, k128x256, k128, k64 };
 
@@ -298,8 +324,8 @@ hipError_t launch_matmul(I8MatmulArgs& g, hipStream_t st)
     switch (shape_of(g.m, g.n, g.groups)) {
         case kFewShape:
             if (g.m * kept_row(g.groups) <= kKeptBytes)
-                return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kKept, 1, 8, 4>(g, st) : launch_few<DTYPE, kKept, 1, 4, 3>(g, st);
-            return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kStream, 1, 8, 2>(g, st) : launch_few<DTYPE, kStream, 1, 4, 2>(g, st);
+                return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kKept, 1, 8, 2>(g, st) : launch_few<DTYPE, kKept, 1, 4, 3>(g, st);
+            return launch_few<DTYPE, kStream, 1, 4, 2>(g, st);
         case k256: return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 4, 128, 2>>(g, st);
         case k192: return launch_tiles<DTYPE, TileShape<kInt8, 192, 192, 2, 6, 128, 3>>(g, st);
         case k256x128: return launch_tiles<DTYPE, TileShape<kInt8, 256, 128, 4, 2, 128, 3>>(g, st);
@@ -368,7 +394,7 @@ hipError_t tq_launch_i8_linear_few(const void* x, int x_dtype, uint64_t m, uint6
     g.groups = (uint32_t)((k + 127) / 128);
     auto as = [&](auto D, auto X) {
         constexpr int T = decltype(D)::value, F = decltype(X)::value;
-        return g.n <= 32 * kComputeUnits ? launch_few<T, F, 1, 8, 4>(g, st) : launch_few<T, F, 1, 4, 3>(g, st);
+        return g.n <= 32 * kComputeUnits ? launch_few<T, F, 1, 8, 2>(g, st) : launch_few<T, F, 1, 4, 3>(g, st);
     };
     auto from = [&](auto D) {
         if (x_dtype == TQ_F32) return as(D, std::integral_constant<int, TQ_F32>{});
