@@ -8,7 +8,7 @@
  * Conventions as in tq.h, but that matrices need only be aligned to an element.  Matrices whose rows follow each other directly, any
  * size; a layer's part of a flat gradient or parameter vector is one.
  *
- *   rows, cols     1 .. 2^31 - 1, rows * cols <= 2^36, the smaller of them at most TQ_ORTH_MAX_SIDE
+ *   rows, cols     1 .. TQ_ORTH_MAX_LENGTH, the smaller of them at most TQ_ORTH_MAX_SIDE
  *   count          1 .. TQ_ORTH_MAX_COUNT matrices of one shape in one call; *_host are host arrays of `count` device pointers.  Results
  *                  are those of `count` calls, bit for bit.
  *   steps          1 .. TQ_ORTH_MAX_STEPS
@@ -37,6 +37,7 @@
 extern "C" {
 #endif
 
+#define TQ_ORTH_MAX_LENGTH (1 << 22)
 #define TQ_ORTH_MAX_SIDE 32768
 #define TQ_ORTH_MAX_COUNT 64
 #define TQ_ORTH_MAX_STEPS 16

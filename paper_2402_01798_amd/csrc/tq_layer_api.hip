@@ -187,8 +187,8 @@ static int check_orth_sizes(uint64_t rows, uint64_t cols, int count, int precisi
     const int rc = check_matrix(rows, cols, cols);
     if (rc) return rc;
     if (count < 1 || (precision != TQ_ORTH_HALF && precision != TQ_ORTH_SPLIT)) return TQ_EINVAL;
-    const uint64_t side = rows < cols ? rows : cols;
-    return count > TQ_ORTH_MAX_COUNT || side > TQ_ORTH_MAX_SIDE || rows * cols > (1ull << 36) ? TQ_EUNSUPPORTED : TQ_OK;
+    const uint64_t side = rows < cols ? rows : cols, length = rows < cols ? cols : rows;
+    return count > TQ_ORTH_MAX_COUNT || side > TQ_ORTH_MAX_SIDE || length > TQ_ORTH_MAX_LENGTH ? TQ_EUNSUPPORTED : TQ_OK;
 }
 
 // Whether the steps keep singular values that begin in [0, 1] where the products' operands hold them: the largest magnitudes of

@@ -199,8 +199,8 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_step_kernel(Step
     char* ws = s.workspace + blockIdx.y * s.stride;
     const uint32_t groups = groups_of(KIND, s.k), row0 = ty * S::BM, col0 = tx * S::BN;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
-    tile_sums<S>(TileOperands{reinterpret_cast<uint8_t*>(ws + s.from_a), reinterpret_cast<uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups},
-                 row0, col0, lds, acc);
+    const TileOperands operands = {reinterpret_cast<uint8_t*>(ws + s.from_a), reinterpret_cast<uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
+    if (!tile_sums<S>(operands, row0, col0, lds, acc)) return;
     const uint64_t to_row = (uint64_t)groups_of(KIND, s.n) * 128, turned_row = (uint64_t)groups_of(KIND, s.m) * 128;
     const bool turn = WHAT == kApply || ty != tx;
     tile_chunks<S>(acc, row0, col0, [&](uint32_t row, uint32_t col, const float (&sums)[8]) {
@@ -245,8 +245,8 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_end_kernel(EndAr
     const uint32_t which = blockIdx.y, groups = groups_of(S::KIND, s.k);
     const char* ws = s.workspace + which * s.stride;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
-    tile_sums<S>(TileOperands{reinterpret_cast<const uint8_t*>(ws + s.from_a), reinterpret_cast<const uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups},
-                 ty * S::BM, tx * S::BN, lds, acc);
+    const TileOperands operands = {reinterpret_cast<const uint8_t*>(ws + s.from_a), reinterpret_cast<const uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
+    if (!tile_sums<S>(operands, ty * S::BM, tx * S::BN, lds, acc)) return;
     tile_chunks<S>(acc, ty * S::BM, tx * S::BN, [&](uint32_t row, uint32_t col, const float (&sums)[8]) {
         if (row >= s.m || col >= s.n) return;
         const int n = (int)min(s.n - col, 8u);
@@ -295,32 +295,85 @@ struct OrthCall {
     char* workspace;
 };
 
+// Tiles of a product: their sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute
+// unit, and what a round of them costs beside that.
+enum Shape { k256, k192, k128, k64, k64InParts };
+struct Pace {
+    Shape shape;
+    uint64_t side;
+    uint32_t ns[3], round;
+};
+constexpr Pace kPaces[2][5] = {
+    {{k256, 256, {1553, 0, 0}, 12000}, {k192, 192, {943, 0, 0}, 9000}, {k128, 128, {580, 925, 0}, 8000}, {k64, 64, {262, 375, 560}, 4000}, {k64InParts, 64, {140, 0, 0}, 5000}},
+    {{k256, 256, {2200, 0, 0}, 12000}, {k192, 192, {1300, 0, 0}, 9000}, {k128, 128, {700, 1200, 0}, 8000}, {k64, 64, {300, 420, 620}, 4000}, {k64InParts, 64, {160, 0, 0}, 5000}}};
+
+uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side, bool below)
+{
+    const uint64_t y = (m + side - 1) / side, x = (n + side - 1) / side;
+    return below ? y * (y + 1) / 2 : x * y;
+}
+
+Shape shape_of(int kind, uint64_t m, uint64_t n, uint64_t k, bool below, uint64_t count)
+{
+    const Pace* best = nullptr;
+    uint64_t least = ~0ull;
+    for (const Pace& p : kPaces[kind == kHalfPair]) {
+        const uint64_t each = (tiles_of(m, n, p.side, below) * count + kComputeUnits - 1) / kComputeUnits, groups = (k + in_group(kind) - 1) / in_group(kind);
+        const uint64_t fit = p.ns[2] ? 3 : p.ns[1] ? 2 : 1, rest = each % fit;
+        const uint64_t t = each / fit * (p.ns[fit - 1] * groups + p.round) + (rest ? p.ns[rest - 1] * groups + p.round : 0);
+        if (t < least) {
+            least = t;
+            best = &p;
+        }
+    }
+    return best->shape;
+}
+
+template <int KIND, typename F>
+hipError_t by_shape(const StepArgs& s, bool below, int count, F f)
+{
+    switch (shape_of(KIND, s.m, s.n, s.k, below, (uint64_t)count)) {
+        case k256: return f(TileShape<KIND, 256, 256, 2, 4, 128, 2>{});
+        case k192: return f(TileShape<KIND, 192, 192, 2, 6, 128, 3>{});
+        case k128: return f(TileShape<KIND, 128, 128, 2, 4, 128, 2>{});
+        case k64: return f(TileShape<KIND, 64, 64, 2, 2, 128, 3>{});
+        case k64InParts: return f(TileShape<KIND, 64, 64, 2, 2, 128, 2, 4>{});
+    }
+    return hipErrorInvalidValue;
+}
+
 template <class S>
 bool set_tiles(StepArgs& s, bool below, int count, dim3& grid)
 {
-    const uint64_t y = ((uint64_t)s.m + S::BM - 1) / S::BM, x = ((uint64_t)s.n + S::BN - 1) / S::BN, tiles = below ? y * (y + 1) / 2 : x * y;
-    s.tiles_x = (uint32_t)x;
-    s.tiles_y = (uint32_t)y;
+    const uint64_t tiles = tiles_of(s.m, s.n, S::BM, below);
+    s.tiles_x = (s.n + S::BN - 1) / S::BN;
+    s.tiles_y = (s.m + S::BM - 1) / S::BM;
     s.tiles = (uint32_t)tiles;
     return tiles <= 0xFFFFFFF0ull && fold_grid((tiles + 7) / 8 * 8, S::kThreads, (unsigned)count, grid);
 }
 
-template <class S, int WHAT>
+template <int KIND, int WHAT>
 hipError_t launch_step(StepArgs s, int count, hipStream_t st)
 {
-    dim3 grid;
-    if (!set_tiles<S>(s, WHAT != kApply, count, grid)) return hipErrorInvalidValue;
-    orth_step_kernel<S, WHAT><<<grid, S::kThreads, S::kBytes, st>>>(s);
-    return hipGetLastError();
+    return by_shape<KIND>(s, WHAT != kApply, count, [&](auto shape) -> hipError_t {
+        using S = decltype(shape);
+        dim3 grid;
+        if (!set_tiles<S>(s, WHAT != kApply, count, grid)) return hipErrorInvalidValue;
+        orth_step_kernel<S, WHAT><<<grid, S::kThreads, S::kBytes, st>>>(s);
+        return hipGetLastError();
+    });
 }
 
-template <class S, int DTYPE, bool UPDATE>
+template <int KIND, int DTYPE, bool UPDATE>
 hipError_t launch_end(EndArgs& a, int count, hipStream_t st)
 {
-    dim3 grid;
-    if (!set_tiles<S>(a.s, false, count, grid)) return hipErrorInvalidValue;
-    orth_end_kernel<S, DTYPE, UPDATE><<<grid, S::kThreads, S::kBytes, st>>>(a);
-    return hipGetLastError();
+    return by_shape<KIND>(a.s, false, count, [&](auto shape) -> hipError_t {
+        using S = decltype(shape);
+        dim3 grid;
+        if (!set_tiles<S>(a.s, false, count, grid)) return hipErrorInvalidValue;
+        orth_end_kernel<S, DTYPE, UPDATE><<<grid, S::kThreads, S::kBytes, st>>>(a);
+        return hipGetLastError();
+    });
 }
 
 template <int KIND>
@@ -349,7 +402,6 @@ hipError_t launch_begin(const OrthCall& q, const OrthPointers& p, OrthArgs& o, h
 template <int KIND>
 hipError_t launch_orth(const OrthCall& q, hipStream_t st)
 {
-    using Square = std::conditional_t<KIND == kHalf, TileShape<KIND, 256, 256, 2, 4, 128, 2>, TileShape<KIND, 128, 128, 2, 2, 128, 2>>;
     const Layout l = layout(q.rows, q.cols, KIND);
     const bool flip = q.rows > q.cols;
     const uint32_t r = (uint32_t)(flip ? q.cols : q.rows), c = (uint32_t)(flip ? q.rows : q.cols);
@@ -387,18 +439,18 @@ hipError_t launch_orth(const OrthCall& q, hipStream_t st)
         s.k = c;
         s.from_a = s.from_b = l.x;
         s.to = s.to_turned = l.a;
-        if ((e = launch_step<Square, kGram>(s, q.count, st)) != hipSuccess) return e;
+        if ((e = launch_step<KIND, kGram>(s, q.count, st)) != hipSuccess) return e;
         s.k = r;
         s.from_a = s.from_b = l.a;
         s.to = s.to_turned = l.b;
-        if ((e = launch_step<Square, kPolynomial>(s, q.count, st)) != hipSuccess) return e;
+        if ((e = launch_step<KIND, kPolynomial>(s, q.count, st)) != hipSuccess) return e;
         if (step + 1 < q.steps) {
             s.n = c;
             s.from_a = l.b;
             s.from_b = xt;
             s.to = l.x;
             s.to_turned = l.xt[~step & 1];
-            e = launch_step<Square, kApply>(s, q.count, st);
+            e = launch_step<KIND, kApply>(s, q.count, st);
             continue;
         }
         EndArgs a = {};
@@ -414,10 +466,10 @@ hipError_t launch_orth(const OrthCall& q, hipStream_t st)
         a.eta = q.eta;
         a.scale = q.scale;
         a.weight_decay = q.weight_decay;
-        if (q.theta) e = launch_end<Square, TQ_F32, true>(a, q.count, st);
-        else if (q.out_dtype == TQ_F32) e = launch_end<Square, TQ_F32, false>(a, q.count, st);
-        else if (q.out_dtype == TQ_BF16) e = launch_end<Square, TQ_BF16, false>(a, q.count, st);
-        else e = launch_end<Square, TQ_F16, false>(a, q.count, st);
+        if (q.theta) e = launch_end<KIND, TQ_F32, true>(a, q.count, st);
+        else if (q.out_dtype == TQ_F32) e = launch_end<KIND, TQ_F32, false>(a, q.count, st);
+        else if (q.out_dtype == TQ_BF16) e = launch_end<KIND, TQ_BF16, false>(a, q.count, st);
+        else e = launch_end<KIND, TQ_F16, false>(a, q.count, st);
     }
     return e;
 }
