@@ -45,7 +45,7 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void i8_tile_kernel(I8Matm
     const uint32_t split = tile / g.tiles, each = (g.groups + g.splits - 1) / g.splits, first = min(split * each, g.groups);
     tile_place(tile - split * g.tiles, g.tiles_y, g.tiles_x, ty, tx);
     typename S::Sums acc[S::kFragsM][S::kFragsN];
-    if (!tile_sums<S>(TileOperands{g.a, g.b, g.m, g.n, g.groups, first, min(each, g.groups - first)}, ty * S::BM, tx * S::BN, lds, acc)) return;
+    tile_sums<S>(TileOperands{g.a, g.b, g.m, g.n, g.groups, first, min(each, g.groups - first)}, ty * S::BM, tx * S::BN, lds, acc);
     tile_chunks<S>(acc, ty * S::BM, tx * S::BN, [&](uint32_t row, uint32_t col, const int (&sums)[8]) {
         if (row >= g.m || col >= g.n) return;
         if (g.splits == 1) return store_scaled<DTYPE>(g, row, col, sums);

@@ -97,13 +97,42 @@ __device__ __forceinline__ void put8(char* row, uint32_t col, const float (&v)[8
     if constexpr (KIND == kHalfPair) *reinterpret_cast<tile_f16x8*>(to + 32) = low;
 }
 
-template <int KIND>
-__device__ __forceinline__ void put1(char* row, uint32_t col, float v)
+// 8 elements of a row in each lane to columns: lanes whose rows are 4 in a row change elements, after which a lane holds 4 rows of the
+// two columns c and c + 4, c = its row % 4.  8 bytes at a time 32 rows of a column are stored by 8 lanes; element by element it took 64.
+__device__ __forceinline__ void turn4(const tile_f16x8& v, uint32_t row, u32x2 (&out)[2])
 {
-    char* to = row + in_row<KIND>(col);
-    const _Float16 high = (_Float16)v;
-    *reinterpret_cast<_Float16*>(to) = high;
-    if constexpr (KIND == kHalfPair) *reinterpret_cast<_Float16*>(to + 32) = (_Float16)low_part(v, high);
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    const uint32_t halves = row & 1 ? 0x03020706u : 0x05040100u;   // of two words: those of this lane's column, the lower row's first
+    u32x4 t;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t other = dpp_move<0xB1>(w[k]);               // of lane ^ 1
+        t[k] = __builtin_amdgcn_perm(other, w[k], halves);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t give = row & 2 ? t[2 * k] : t[2 * k + 1], keep = row & 2 ? t[2 * k + 1] : t[2 * k];
+        const uint32_t got = dpp_move<0x4E>(give);                 // of lane ^ 2
+        out[k] = row & 2 ? u32x2{got, keep} : u32x2{keep, got};
+    }
+}
+
+// The same 8 elements of 64 lanes' rows at their places in the transposed matrix, whose rows are `to_row` bytes, `cols` of them there.
+template <int KIND>
+__device__ __forceinline__ void put_turned(char* to, uint64_t to_row, uint32_t row, uint32_t col, uint32_t cols, const tile_f16x8& high, const tile_f16x8& low)
+{
+    u32x2 h[2], l[2];
+    turn4(high, row, h);
+    if constexpr (KIND == kHalfPair) turn4(low, row, l);
+    if (in_row<KIND>(row & ~3u) >= to_row) return;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t c = col + (row & 3) + 4 * k;
+        if (c >= cols) continue;
+        char* at = to + c * to_row + in_row<KIND>(row & ~3u);
+        *reinterpret_cast<u32x2*>(at) = h[k];
+        if constexpr (KIND == kHalfPair) *reinterpret_cast<u32x2*>(at + 32) = l[k];
+    }
 }
 
 template <int KIND>
@@ -200,7 +229,7 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_step_kernel(Step
     const uint32_t groups = groups_of(KIND, s.k), row0 = ty * S::BM, col0 = tx * S::BN;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
     const TileOperands operands = {reinterpret_cast<uint8_t*>(ws + s.from_a), reinterpret_cast<uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
-    if (!tile_sums<S>(operands, row0, col0, lds, acc)) return;
+    tile_sums<S>(operands, row0, col0, lds, acc);
     const uint64_t to_row = (uint64_t)groups_of(KIND, s.n) * 128, turned_row = (uint64_t)groups_of(KIND, s.m) * 128;
     const bool turn = WHAT == kApply || ty != tx;
     tile_chunks<S>(acc, row0, col0, [&](uint32_t row, uint32_t col, const float (&sums)[8]) {
@@ -215,14 +244,19 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_step_kernel(Step
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = sums[e] * (1.0f / kUnit);
         }
+        tile_f16x8 high, low;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = row < s.m && col + e < s.n ? v[e] : 0.0f;
-        if (there) put8<KIND>(ws + s.to + row * to_row, col, v);
-        if (turn && in_row<KIND>(row) < turned_row) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < s.n) put1<KIND>(ws + s.to_turned + (col + e) * turned_row, row, v[e]);
+        for (int e = 0; e < 8; ++e) {
+            v[e] = row < s.m && col + e < s.n ? v[e] : 0.0f;
+            high[e] = (_Float16)v[e];
+            low[e] = (_Float16)low_part(v[e], high[e]);
         }
+        if (there) {
+            char* to = ws + s.to + row * to_row + in_row<KIND>(col);
+            *reinterpret_cast<tile_f16x8*>(to) = high;
+            if constexpr (KIND == kHalfPair) *reinterpret_cast<tile_f16x8*>(to + 32) = low;
+        }
+        if (turn) put_turned<KIND>(ws + s.to_turned, turned_row, row, col, s.n, high, low);
     });
 }
 
@@ -246,7 +280,7 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_end_kernel(EndAr
     const char* ws = s.workspace + which * s.stride;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
     const TileOperands operands = {reinterpret_cast<const uint8_t*>(ws + s.from_a), reinterpret_cast<const uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
-    if (!tile_sums<S>(operands, ty * S::BM, tx * S::BN, lds, acc)) return;
+    tile_sums<S>(operands, ty * S::BM, tx * S::BN, lds, acc);
     tile_chunks<S>(acc, ty * S::BM, tx * S::BN, [&](uint32_t row, uint32_t col, const float (&sums)[8]) {
         if (row >= s.m || col >= s.n) return;
         const int n = (int)min(s.n - col, 8u);
@@ -262,6 +296,242 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_end_kernel(EndAr
         }
         store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(a.out[which]) + at, n, v);
     });
+}
+
+// Small matrices: a workgroup has X, X^T, A and B of one in its LDS and takes all steps in one launch, where the products of the kernels above
+// would each be a launch of a few us.  Rows are 16 bytes longer than their elements, so that 16 of them lie in different banks; everything is
+// padded to 32 with zeros.
+struct SmallArgs {
+    void* out[TQ_ORTH_MAX_COUNT];
+    const float* theta[TQ_ORTH_MAX_COUNT];
+    float coefficients[TQ_ORTH_MAX_STEPS][3];
+    uint32_t rows, cols;
+    int dtype, out_dtype, steps, nesterov;
+    float momentum, eps, eta, scale, weight_decay;
+};
+
+constexpr uint32_t kSmallWaves = 8, kSmallFrags = 4;              // 32 x 32 outputs that a wavefront may hold
+
+struct SmallPlan {
+    uint32_t r, c, row_x, row_t, xt, a, b, bytes;                  // row_t: of X^T, A and B; bytes: of all four, once for each number of a pair
+};
+__host__ __device__ inline SmallPlan small_plan(uint64_t rows, uint64_t cols)
+{
+    SmallPlan p;
+    p.r = (uint32_t)(((rows < cols ? rows : cols) + 31) / 32 * 32);
+    p.c = (uint32_t)(((rows < cols ? cols : rows) + 31) / 32 * 32);
+    p.row_x = p.c * 2 + 16;
+    p.row_t = p.r * 2 + 16;
+    p.xt = p.r * p.row_x;
+    p.a = p.xt + p.c * p.row_t;
+    p.b = p.a + p.r * p.row_t;
+    p.bytes = p.b + p.r * p.row_t;
+    return p;
+}
+constexpr uint32_t kSmallBytes = (156 << 10);
+
+bool is_small(uint64_t rows, uint64_t cols, int kind)
+{
+    const uint64_t r = rows < cols ? rows : cols, c = rows < cols ? cols : rows;
+    if (r > 128 || c > 4096) return false;
+    const SmallPlan p = small_plan(rows, cols);
+    return p.bytes * (kind == kHalfPair ? 2u : 1u) <= kSmallBytes && p.r / 32 * (p.c / 32) <= kSmallWaves * kSmallFrags;
+}
+
+template <int KIND, bool UPDATE>
+__global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(OrthPointers q, SmallArgs s)
+{
+    using P = TileProduct<KIND>;
+    extern __shared__ char lds[];
+    __shared__ double part[kSmallWaves];
+    constexpr uint32_t kAll = kSmallWaves * 64;
+    const uint32_t which = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t me = lane;
+    if (blockIdx.x) return;
+    const SmallPlan p = small_plan(s.rows, s.cols);
+    const uint32_t size = s.rows * s.cols;
+    const bool flip = s.rows > s.cols;
+    char *x = lds, *xt = lds + p.xt, *a = lds + p.a, *b = lds + p.b;
+    for (uint32_t i = threadIdx.x * 16; i < p.bytes * (KIND == kHalfPair ? 2 : 1); i += kAll * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
+    // 8 elements of U from `at` on, and of the new momentum
+    auto load = [&](uint32_t at, float (&u)[8], float (&v)[8]) {
+        const int n = (int)min(size - at, 8u);
+        if (s.dtype == TQ_F32) load_eight<TQ_F32>(q.g[which], at, n, u);
+        else if (s.dtype == TQ_BF16) load_eight<TQ_BF16>(q.g[which], at, n, u);
+        else load_eight<TQ_F16>(q.g[which], at, n, u);
+        if constexpr (UPDATE) {
+            load8<TQ_F32>(q.v[which] + at, n, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = s.momentum * v[j] + u[j];
+                u[j] = s.nesterov ? u[j] + s.momentum * v[j] : v[j];
+            }
+        }
+        return n;
+    };
+    double sum = 0.0;                                              // of squares, in binary64
+    float u[8], v[8];
+    for (uint32_t at = threadIdx.x * 8; at < size; at += kAll * 8) {
+        const int n = load(at, u, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) sum += (double)u[j] * (double)u[j];
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < kSmallWaves; ++w) sum += part[w];
+    const double factor = (double)kUnit / (sqrt(sum) + (double)s.eps);
+    auto put = [&](char* array, uint32_t stride, uint32_t row, uint32_t col, float v) {
+        char* to = array + row * stride + col * 2;
+        const _Float16 high = (_Float16)v;
+        *reinterpret_cast<_Float16*>(to) = high;
+        if constexpr (KIND == kHalfPair) *reinterpret_cast<_Float16*>(to + p.bytes) = (_Float16)low_part(v, high);
+    };
+    for (uint32_t at = threadIdx.x * 8; at < size; at += kAll * 8) {
+        const int n = load(at, u, v);
+        if constexpr (UPDATE) store8<TQ_F32>(q.v_out[which] + at, n, v);
+        uint32_t row = at / s.cols, col = at % s.cols;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j >= n) break;
+            const float held = (float)((double)u[j] * factor);
+            put(flip ? xt : x, flip ? p.row_t : p.row_x, row, col, held);
+            put(flip ? x : xt, flip ? p.row_x : p.row_t, col, row, held);
+            if (++col == s.cols) {
+                col = 0;
+                ++row;
+            }
+        }
+    }
+    __syncthreads();
+
+    // 32 x 32 outputs of rows of two arrays; a lane's 16 as in tiles.  32 of k at a time, the next 32 on their way.
+    auto product = [&](const char* from_a, const char* from_b, uint32_t stride, uint32_t row_a, uint32_t row_b, uint32_t k) {
+        constexpr int kNumbers = KIND == kHalfPair ? 2 : 1;
+        typename P::Sums acc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+        const char* pa = from_a + (row_a + (me & 31)) * stride + (me >> 5) * 16;
+        const char* pb = from_b + (row_b + (me & 31)) * stride + (me >> 5) * 16;
+        tile_i32x4 va[2][kNumbers], vb[2][kNumbers];
+        auto load = [&](uint32_t i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < kNumbers; ++n) {
+                    va[h][n] = *reinterpret_cast<const tile_i32x4*>(pa + n * p.bytes + i + h * 32);
+                    vb[h][n] = *reinterpret_cast<const tile_i32x4*>(pb + n * p.bytes + i + h * 32);
+                }
+        };
+        load(0);
+        for (uint32_t i = 0; i < k * 2; i += 64) {
+            tile_i32x4 a[2][kNumbers], b[2][kNumbers];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < kNumbers; ++n) {
+                    a[h][n] = va[h][n];
+                    b[h][n] = vb[h][n];
+                }
+            load(i + 64 < k * 2 ? i + 64 : 0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                acc = P::step(b[h][0], a[h][0], acc);
+                if constexpr (KIND == kHalfPair) {
+                    acc = P::step(b[h][0], a[h][1], acc);
+                    acc = P::step(b[h][1], a[h][0], acc);
+                }
+            }
+        }
+        return acc;
+    };
+    auto row_of = [&](uint32_t row0) { return row0 + (me & 31); };
+    auto col_of = [&](uint32_t col0, int e) { return col0 + (e / 4) * 8 + (me >> 5) * 4 + e % 4; };
+    // Into an array, 4 columns at a time.
+    auto place = [&](char* to, uint32_t stride, uint32_t row0, uint32_t col0, const typename P::Sums& v) {
+        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            f16x4 high, low;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                high[i] = (_Float16)v[e + i];
+                low[i] = (_Float16)low_part(v[e + i], high[i]);
+            }
+            char* at = to + row_of(row0) * stride + col_of(col0, e) * 2;
+            *reinterpret_cast<f16x4*>(at) = high;
+            if constexpr (KIND == kHalfPair) *reinterpret_cast<f16x4*>(at + p.bytes) = low;
+        }
+    };
+    const uint32_t down = p.r / 32, across = p.c / 32;
+    for (int step = 0; step < s.steps; ++step) {
+        const float fa = s.coefficients[step][0], fb = s.coefficients[step][1], fc = s.coefficients[step][2];
+        for (uint32_t at = wave; at < down * down; at += kSmallWaves) {
+            const uint32_t row0 = at % down * 32, col0 = at / down * 32;
+            asm volatile("" : "+v"(me));
+            typename P::Sums v = product(x, x, p.row_x, row0, col0, p.c);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] *= 1.0f / kUnit;
+            place(a, p.row_t, row0, col0, v);
+        }
+        __syncthreads();
+        for (uint32_t at = wave; at < down * down; at += kSmallWaves) {
+            const uint32_t row0 = at % down * 32, col0 = at / down * 32;
+            asm volatile("" : "+v"(me));
+            typename P::Sums v = product(a, a, p.row_t, row0, col0, p.r);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const char* from = a + row_of(row0) * p.row_t + col_of(col0, e) * 2;
+                float gram = (float)*reinterpret_cast<const _Float16*>(from);
+                if constexpr (KIND == kHalfPair) gram += (float)*reinterpret_cast<const _Float16*>(from + p.bytes);
+                v[e] = fmaf(fc, v[e] * (1.0f / kUnit), fmaf(fb, gram, row_of(row0) == col_of(col0, e) ? fa * kUnit : 0.0f));
+            }
+            place(b, p.row_t, row0, col0, v);
+        }
+        __syncthreads();
+        asm volatile("" : "+v"(me));                               // places are found where they are used, not kept from step to step
+        typename P::Sums held[kSmallFrags];
+#pragma unroll
+        for (uint32_t f = 0; f < kSmallFrags; ++f) {
+            const uint32_t at = wave + f * kSmallWaves;
+            if (at < down * across) held[f] = product(b, xt, p.row_t, at % down * 32, at / down * 32, p.r);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t f = 0; f < kSmallFrags; ++f) {
+            const uint32_t at = wave + f * kSmallWaves, row0 = at % down * 32, col0 = at / down * 32;
+            if (at >= down * across) continue;
+            asm volatile("" : "+v"(me));
+            if (step + 1 < s.steps) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) held[f][e] *= 1.0f / kUnit;
+                place(x, p.row_x, row0, col0, held[f]);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) put(xt, p.row_t, col_of(col0, e), row_of(row0), held[f][e]);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t i = flip ? col_of(col0, e) : row_of(row0), j = flip ? row_of(row0) : col_of(col0, e);
+                if (i >= s.rows || j >= s.cols) continue;
+                const uint32_t to = i * s.cols + j;
+                float v = held[f][e] * (1.0f / (kUnit * kUnit));
+                if constexpr (UPDATE) {
+                    const float theta = s.theta[which][to];
+                    static_cast<float*>(s.out[which])[to] = theta - s.eta * (s.scale * v + s.weight_decay * theta);
+                } else if (s.out_dtype == TQ_F32) {
+                    static_cast<float*>(s.out[which])[to] = v;
+                } else {
+                    static_cast<uint16_t*>(s.out[which])[to] = s.out_dtype == TQ_BF16 ? Element<TQ_BF16>::store(v) : Element<TQ_F16>::store(v);
+                }
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // A matrix's part of the workspace.
@@ -296,16 +566,28 @@ struct OrthCall {
 };
 
 // Tiles of a product: their sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute
-// unit, and what a round of them costs beside that.
-enum Shape { k256, k192, k128, k64, k64InParts };
+// unit, and what a round of them costs beside that (both transposes are written).  `alone`: five buffers in place of two, one workgroup on a
+// unit.  Kernel times of products, us, * the rule's:
+//                                                        256     192     128   128 alone   64
+//   binary16  4096^3, symmetric                         110    * 92     122     127       160
+//   binary16  4096^3                                  * 131     177     164     180       235
+//   binary16  512 x 512 x 2048, symmetric                46      26      21      18     * 11.5
+//   binary16  512 x 2048 x 512                           23      15      11      11     *  8.5
+//   pairs     2048^3, symmetric                         111      71      55    * 52        55
+//   pairs     2048^3                                    117      78      63    * 62        82
+//   pairs     4 of 1024 x 1024 x 4096, symmetric        213     140     108    * 95       102
+//   pairs     4 of 1024 x 4096 x 1024                 * 104     156     117     137       166
+//   pairs     784 x 1000 x 784                           56      34      23      20     * 11
+// k in two or four parts by more wavefronts of a workgroup took longer than tiles of 64 by one set of them everywhere (784 x 1000: 13).
+enum Shape { k256, k192, k128, k128Alone, k64 };
 struct Pace {
     Shape shape;
     uint64_t side;
     uint32_t ns[3], round;
 };
 constexpr Pace kPaces[2][5] = {
-    {{k256, 256, {1553, 0, 0}, 12000}, {k192, 192, {943, 0, 0}, 9000}, {k128, 128, {580, 925, 0}, 8000}, {k64, 64, {262, 375, 560}, 4000}, {k64InParts, 64, {140, 0, 0}, 5000}},
-    {{k256, 256, {2200, 0, 0}, 12000}, {k192, 192, {1300, 0, 0}, 9000}, {k128, 128, {700, 1200, 0}, 8000}, {k64, 64, {300, 420, 620}, 4000}, {k64InParts, 64, {160, 0, 0}, 5000}}};
+    {{k256, 256, {1553, 0, 0}, 25000}, {k192, 192, {943, 0, 0}, 20000}, {k128, 128, {580, 925, 0}, 12000}, {k128Alone, 128, {540, 0, 0}, 12000}, {k64, 64, {262, 375, 560}, 5000}},
+    {{k256, 256, {1900, 0, 0}, 40000}, {k192, 192, {1100, 0, 0}, 24000}, {k128, 128, {800, 1200, 0}, 15000}, {k128Alone, 128, {730, 0, 0}, 12000}, {k64, 64, {270, 450, 770}, 5000}}};
 
 uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side, bool below)
 {
@@ -336,8 +618,8 @@ hipError_t by_shape(const StepArgs& s, bool below, int count, F f)
         case k256: return f(TileShape<KIND, 256, 256, 2, 4, 128, 2>{});
         case k192: return f(TileShape<KIND, 192, 192, 2, 6, 128, 3>{});
         case k128: return f(TileShape<KIND, 128, 128, 2, 4, 128, 2>{});
+        case k128Alone: return f(TileShape<KIND, 128, 128, 2, 4, 128, 5>{});
         case k64: return f(TileShape<KIND, 64, 64, 2, 2, 128, 3>{});
-        case k64InParts: return f(TileShape<KIND, 64, 64, 2, 2, 128, 2, 4>{});
     }
     return hipErrorInvalidValue;
 }
@@ -399,6 +681,35 @@ hipError_t launch_begin(const OrthCall& q, const OrthPointers& p, OrthArgs& o, h
     return q.dtype == TQ_BF16 ? as(std::integral_constant<int, TQ_BF16>{}) : as(std::integral_constant<int, TQ_F16>{});
 }
 
+constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+
+template <int KIND>
+hipError_t launch_small(const OrthCall& q, const OrthPointers& p, hipStream_t st)
+{
+    SmallArgs s = {};
+    for (int i = 0; i < q.count; ++i) {
+        s.out[i] = q.out[i];
+        s.theta[i] = q.theta ? q.theta[i] : nullptr;
+    }
+    for (int i = 0; i < q.steps; ++i)
+        for (int j = 0; j < 3; ++j) s.coefficients[i][j] = q.coefficients ? q.coefficients[3 * i + j] : kQuintic[j];
+    s.rows = (uint32_t)q.rows;
+    s.cols = (uint32_t)q.cols;
+    s.dtype = q.dtype;
+    s.out_dtype = q.out_dtype;
+    s.steps = q.steps;
+    s.nesterov = q.nesterov;
+    s.momentum = q.momentum;
+    s.eps = q.eps;
+    s.eta = q.eta;
+    s.scale = q.scale;
+    s.weight_decay = q.weight_decay;
+    const uint32_t bytes = small_plan(q.rows, q.cols).bytes * (KIND == kHalfPair ? 2 : 1);
+    if (q.theta) orth_small_kernel<KIND, true><<<dim3(1, q.count), kSmallWaves * 64, bytes, st>>>(p, s);
+    else orth_small_kernel<KIND, false><<<dim3(1, q.count), kSmallWaves * 64, bytes, st>>>(p, s);
+    return hipGetLastError();
+}
+
 template <int KIND>
 hipError_t launch_orth(const OrthCall& q, hipStream_t st)
 {
@@ -411,6 +722,7 @@ hipError_t launch_orth(const OrthCall& q, hipStream_t st)
         p.v[i] = q.v ? q.v[i] : nullptr;
         p.v_out[i] = q.v ? q.v_out[i] : nullptr;
     }
+    if (is_small(q.rows, q.cols, KIND)) return launch_small<KIND>(q, p, st);
     OrthArgs o = {};
     o.workspace = q.workspace;
     o.stride = l.stride;
@@ -429,7 +741,6 @@ hipError_t launch_orth(const OrthCall& q, hipStream_t st)
     s.workspace = q.workspace;
     s.stride = l.stride;
     for (int step = 0; step < q.steps && e == hipSuccess; ++step) {
-        static const float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
         const float* f = q.coefficients ? q.coefficients + 3 * step : kQuintic;
         s.a = f[0];
         s.b = f[1];

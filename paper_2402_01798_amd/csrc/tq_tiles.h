@@ -41,24 +41,23 @@ struct TileProduct<kInt8> {
 };
 
 // BM x BN outputs by WM x WN wavefronts, a slice of ROW bytes of k at a time through a ring of STAGES buffers in LDS: BM rows of A, then BN
-// of B.  PARTS times as many wavefronts take parts of k side by side, each with a ring of its own.
-template <int KIND_, int BM_, int BN_, int WM_, int WN_, int ROW_, int STAGES_, int PARTS_ = 1>
+// of B.
+template <int KIND_, int BM_, int BN_, int WM_, int WN_, int ROW_, int STAGES_>
 struct TileShape {
-    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, ROW = ROW_, STAGES = STAGES_, PARTS = PARTS_;
+    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, ROW = ROW_, STAGES = STAGES_;
     using Product = TileProduct<KIND>;
     using Sums = typename Product::Sums;
-    static constexpr int kWaves = WM * WN, kThreads = kWaves * PARTS * 64;      // wavefronts of a part
+    static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int kFragsM = BM / WM / 32, kFragsN = BN / WN / 32;
-    static constexpr int kStage = (BM + BN) * ROW, kRing = STAGES * kStage, kBytes = PARTS * kRing;
+    static constexpr int kStage = (BM + BN) * ROW, kBytes = STAGES * kStage;
     static constexpr int kPieces = ROW / 16, kRows = 64 / kPieces; // rows that a request of a wavefront covers
     static constexpr int kLoadsA = BM / kRows / kWaves, kLoads = (BM + BN) / kRows / kWaves;   // requests of a wavefront for a buffer
     static constexpr int kOnUnit = (int)kLdsBytes / kBytes;        // workgroups on a compute unit
-    static constexpr int kOnSimd = kOnUnit * kThreads / 256 < 1 ? 1 : kOnUnit * kThreads / 256 > 4 ? 4 : kOnUnit * kThreads / 256;
+    static constexpr int kOnSimd = kOnUnit * kWaves / 4 < 1 ? 1 : kOnUnit * kWaves / 4 > 4 ? 4 : kOnUnit * kWaves / 4;      // wavefronts
     static constexpr bool kPair = KIND == kHalfPair;
     static constexpr int kStep = kPair ? 64 : 32, kSteps = ROW / kStep;        // bytes of a row that are multiplied at a time
     static constexpr int kReads = (kFragsM + kFragsN) * (kPair ? 2 : 1), kProducts = kFragsM * kFragsN * (kPair ? 3 : 1);     // of a step
     static_assert((ROW == 64 || ROW == 128) && kSteps % 2 == 0, "operands are read into two sets of registers in turn");
-    static_assert(PARTS == 1 || (PARTS - 1) * BM * BN * 4 <= kBytes, "the other parts' sums take the rings' place");
     static_assert(BM / kRows % kWaves == 0 && BN / kRows % kWaves == 0 && kRows * kWaves % 16 == 0 && kBytes <= (int)kLdsBytes && STAGES >= 2,
                   "requests in equal numbers");
 };
@@ -111,22 +110,17 @@ __device__ __forceinline__ void repeat(F f)
 // one row's: element e is column (e / 4) * 8 + (lane / 32) * 4 + e % 4 of row lane % 32.
 // A step's operands are read while the step before it is multiplied, one request behind a product; the first ones of the next slice in the
 // second half of a slice's last step, behind the barrier after which every wavefront is done with this slice's buffer.
-// Returns whether this wavefront holds the tile's sums: those of the first part do.
 template <class S>
-__device__ __forceinline__ bool tile_sums(const TileOperands& g, uint32_t row0, uint32_t col0, char* lds,
+__device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, uint32_t col0, char* lds,
                                           typename S::Sums (&acc)[S::kFragsM][S::kFragsN])
 {
 #ifdef __HIP_DEVICE_COMPILE__                                      // the host's pass does not know the type of a buffer
-    const uint32_t lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t part = wave_of_all / S::kWaves, wave = wave_of_all % S::kWaves;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 31, half = lane >> 5, wm = wave / S::WN, wn = wave % S::WN;
     row0 = __builtin_amdgcn_readfirstlane(row0);                   // the same in all lanes, which divisions hide from the compiler
     col0 = __builtin_amdgcn_readfirstlane(col0);
     const uint64_t stride = (uint64_t)g.groups * 128;
-    // this part's slices, and as many trips for all as the longest has
-    const uint32_t slices = g.count * (128 / S::ROW), most = (slices + S::PARTS - 1) / S::PARTS, begin = S::PARTS == 1 ? 0 : min(part * most, slices);
-    const uint32_t trips = S::PARTS == 1 ? slices : min(most, slices - begin);
-    lds += part * S::kRing;
+    const uint32_t trips = g.count * (128 / S::ROW);
     uint32_t from[S::kLoads];
     const uint32_t piece = (lane % S::kPieces) ^ tile_turn<S::ROW>(wave * S::kRows + lane / S::kPieces);       // in each of a wavefront's requests
 #pragma unroll
@@ -142,7 +136,7 @@ __device__ __forceinline__ bool tile_sums(const TileOperands& g, uint32_t row0, 
         const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(i < S::kLoadsA ? g.a + row0 * stride : g.b + col0 * stride), 0,
                                                           __builtin_amdgcn_readfirstlane(t < trips ? -1 : 0), 0x20000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(of, (tile_lds_bytes*)(lds + stage * S::kStage + (i * S::kWaves + wave) * 1024), 16, from[i],
-                                                 g.first * 128 + (begin + t) * S::ROW, 0, 0);
+                                                 g.first * 128 + t * S::ROW, 0, 0);
     };
 #pragma unroll
     for (uint32_t t = 0; t < S::STAGES; ++t) repeat<S::kLoads>([&](auto I) { fetch_one(I, t, t); });
@@ -163,13 +157,12 @@ __device__ __forceinline__ bool tile_sums(const TileOperands& g, uint32_t row0, 
     constexpr int kHalfway = S::kProducts / 2, kLeft = S::kProducts - kHalfway;
     constexpr int kReadsEach = (2 * S::kReads + kLeft - 1) / kLeft, kLoadsEach = (S::kLoads + kLeft - 1) / kLeft;
     uint32_t stage = 0;
-    for (uint32_t t = 0; t < most; ++t) {
-        const bool live = S::PARTS == 1 || t < trips;              // a shorter part's last trip is empty
+    for (uint32_t t = 0; t < trips; ++t) {
         const char* base = lds + stage * S::kStage;
         repeat<S::kSteps - 1>([&](auto I) {
             constexpr int s = decltype(I)::value;
             repeat<S::kProducts>([&](auto P) {
-                if (live) now[s & 1].template product<decltype(P)::value>(acc);
+                now[s & 1].template product<decltype(P)::value>(acc);
                 constexpr int each = (S::kReads + S::kProducts - 1) / S::kProducts;
                 repeat<each>([&](auto R) {
                     constexpr int at = decltype(P)::value * each + decltype(R)::value;
@@ -180,16 +173,14 @@ __device__ __forceinline__ bool tile_sums(const TileOperands& g, uint32_t row0, 
         });
         TileFragments<S>& last = now[(S::kSteps - 1) & 1];
         const uint32_t next = stage + 1 == S::STAGES ? 0 : stage + 1;
-        repeat<kHalfway>([&](auto P) {
-            if (live) last.template product<decltype(P)::value>(acc);
-        });
+        repeat<kHalfway>([&](auto P) { last.template product<decltype(P)::value>(acc); });
         __builtin_amdgcn_sched_barrier(0);
         // the next slice is there, and every wavefront has read this one
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(S::kLoads * (S::STAGES - 2)) : "memory");
         const char* after = lds + next * S::kStage;
         repeat<kLeft>([&](auto Q) {
             constexpr int q = decltype(Q)::value;
-            if (live) last.template product<kHalfway + q>(acc);
+            last.template product<kHalfway + q>(acc);
             repeat<kReadsEach>([&](auto R) {
                 constexpr int at = q * kReadsEach + decltype(R)::value;
                 if constexpr (at < S::kReads) read(now[0], std::integral_constant<int, at>{}, after, 0);
@@ -203,35 +194,7 @@ __device__ __forceinline__ bool tile_sums(const TileOperands& g, uint32_t row0, 
         stage = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // nothing is on its way to LDS any more
-    if constexpr (S::PARTS > 1) {                                  // the parts' sums, joined in their order
-        lds -= part * S::kRing;
-        __syncthreads();
-        auto place = [&](uint32_t p) { return reinterpret_cast<uint32_t*>(lds) + ((p - 1) * S::kWaves + wave) * (S::kFragsM * S::kFragsN * 1024) + lane; };
-#pragma unroll
-        for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::kFragsN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const auto v = acc[i][j][e];
-                    if (part) place(part)[((i * S::kFragsN + j) * 16 + e) * 64] = __builtin_bit_cast(uint32_t, v);
-                }
-        __syncthreads();
-        if (part) return false;
-#pragma unroll
-        for (int p = 1; p < S::PARTS; ++p)
-#pragma unroll
-            for (int i = 0; i < S::kFragsM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::kFragsN; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t w = place(p)[((i * S::kFragsN + j) * 16 + e) * 64];
-                        acc[i][j][e] += __builtin_bit_cast(std::remove_reference_t<decltype(acc[0][0][0] + 0)>, w);
-                    }
-    }
 #endif
-    return true;
 }
 
 // f(row, column of the first, 8 sums side by side) for all of this lane's sums of the tile.
