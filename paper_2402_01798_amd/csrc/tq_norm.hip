@@ -194,7 +194,7 @@ __device__ __forceinline__ float deviation(float x, float quarter_mean, float fo
 }
 
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
-// other; their sums over rows are joined at the end.
+// other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.
 template <int DTYPE, int WTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
 {
@@ -206,48 +206,74 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_backward_ke
     static_assert(WAVES == 1 || kRows == 1, "barriers are for whole workgroups");
     const uint32_t sub = threadIdx.x / kThreads, tid = threadIdx.x % kThreads, block = linear_block();
     if (block >= a.parts) return;
+    constexpr bool kAhead = WAVES < 16;                            // 16 wavefronts of a workgroup have no registers for that
     const float n_inv = 1.0f / (float)a.cols;
-    float dw[V][8] = {}, db[V][8] = {};
-    uint32_t turn = 0;
-    for (uint64_t row = (uint64_t)block * kRows + sub; row < a.rows; row += (uint64_t)a.parts * kRows) {
+    const uint64_t first = (uint64_t)block * kRows + sub, step = (uint64_t)a.parts * kRows;
+    float dw[V][8] = {}, db[V][8] = {}, weights[V][8];
+    Eight<DTYPE> next_x[V], next_dy[V];
+    float next_mean = 0.0f, next_r = 0.0f;
+    auto fetch = [&](uint64_t row) {
+        if (row >= a.rows) return;
         const T* x = static_cast<const T*>(a.x) + row * a.ldx;
         const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-        Eight<DTYPE> wx[V], wdy[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const uint32_t oct = tid + i * kThreads;
             const int n = left_of(a.cols, oct);
             if (n == 8) {
-                wx[i].load(x + (uint64_t)oct * 8);
-                wdy[i].load(dy + (uint64_t)oct * 8);
-            } else if (n) {
-                wx[i].load(x + (uint64_t)oct * 8, n);
-                wdy[i].load(dy + (uint64_t)oct * 8, n);
+                next_x[i].load(x + (uint64_t)oct * 8);
+                next_dy[i].load(dy + (uint64_t)oct * 8);
+            } else if (n) {                                        // behind the end: dy = 0 and weight = 0, which add nothing
+                next_x[i].load(x + (uint64_t)oct * 8, n);
+                next_dy[i].load(dy + (uint64_t)oct * 8, n);
             } else {
-                wx[i].clear();
-                wdy[i].clear();
+                next_x[i].clear();
+                next_dy[i].clear();
             }
         }
-        const float quarter = 0.25f * a.stats_in[2 * row], r = a.stats_in[2 * row + 1], four = 4.0f * r;
+        next_mean = a.stats_in[2 * row];
+        next_r = a.stats_in[2 * row + 1];
+    };
+    auto weights_of = [&](int i, float (&w)[8]) {
+        const uint32_t oct = tid + i * kThreads;
+        const int n = left_of(a.cols, oct);
+        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, w);
+        else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = j < n ? 1.0f : 0.0f;
+        }
+    };
+    if constexpr (kAhead) {
+        fetch(first);
+#pragma unroll
+        for (int i = 0; i < V; ++i) weights_of(i, weights[i]);
+    }
+    uint32_t turn = 0;
+    for (uint64_t row = first; row < a.rows; row += step) {
+        if constexpr (!kAhead) fetch(row);
+        Eight<DTYPE> wx[V], wdy[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            wx[i] = next_x[i];
+            wdy[i] = next_dy[i];
+        }
+        const float quarter = 0.25f * next_mean, r = next_r, four = 4.0f * r;
+        if constexpr (kAhead) fetch(row + step);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const uint32_t oct = tid + i * kThreads;
-            const int n = left_of(a.cols, oct);
-            float v[8], g[8], weight[8];
+            float v[8], g[8];
             wx[i].unpack(v);
             wdy[i].unpack(g);
-            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+            if constexpr (!kAhead) weights_of(i, weights[0]);
+            const float(&weight)[8] = weights[kAhead ? i : 0];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float h = deviation(v[j], quarter, four);
+                const float h = deviation(v[j], quarter, four), gw = g[j] * weight[j];
                 dw[i][j] = fmaf(g[j], h, dw[i][j]);
                 db[i][j] += g[j];
-                if (j < n) {
-                    const float gw = a.weight ? g[j] * weight[j] : g[j];
-                    s1 += gw;
-                    s2 = fmaf(gw, h, s2);
-                }
+                s1 += gw;
+                s2 = fmaf(gw, h, s2);
             }
         }
         if (!a.out) continue;
@@ -261,16 +287,13 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_backward_ke
             const uint32_t oct = tid + i * kThreads;
             const int n = left_of(a.cols, oct);
             if (n == 0) continue;
-            float v[8], g[8], weight[8];
+            float v[8], g[8];
             wx[i].unpack(v);
             wdy[i].unpack(g);
-            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
+            if constexpr (!kAhead) weights_of(i, weights[0]);
+            const float(&weight)[8] = weights[kAhead ? i : 0];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float h = deviation(v[j], quarter, four);
-                const float gw = a.weight ? g[j] * weight[j] : g[j];
-                v[j] = r * ((gw - s1) - h * s2);
-            }
+            for (int j = 0; j < 8; ++j) v[j] = r * ((g[j] * weight[j] - s1) - deviation(v[j], quarter, four) * s2);
             store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
         }
     }
@@ -389,8 +412,10 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
     const uint64_t at = (uint64_t)linear_block() * 32 + lane, all = 2 * (uint64_t)a.cols;
     if ((uint64_t)linear_block() * 32 >= all) return;
     float v = 0.0f;
-    if (at < all)
+    if (at < all) {
+#pragma unroll 8
         for (uint32_t p = strip; p < a.parts; p += 32) v += a.partial[p * all + at];
+    }
     sums[strip][lane] = v;
     __syncthreads();
     if (strip || at >= all) return;
@@ -401,14 +426,18 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
     *to = a.accumulate ? *to + v : v;
 }
 
-// The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.
+// The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.  Between 513 and 1024 columns forward and
+// backward pass take, by one wavefront a row / by four, us: 300 x 1024 bf16 17.4 / 12.7, 1000 x 600 fp32 20.7 / 15.5, 4099 x 1001 fp32
+// 34.8 / 30.2, 4096 x 1024 bf16 24.6 / 25.0, 16384 x 1024 bf16 48.8 / 60: few rows want many wavefronts, many rows no barriers.
+bool wave_a_row(uint64_t rows, uint64_t cols) { return cols <= 512 || (cols <= 1024 && rows >= 8192); }
+
 template <typename F>
-hipError_t by_shape(uint32_t cols, F f)
+hipError_t by_shape(uint32_t rows, uint32_t cols, F f)
 {
     auto as = [&](auto w, auto v) { return f(w, v); };
 #define TQ_NORM_SHAPE(WAVES, V) return as(std::integral_constant<int, WAVES>{}, std::integral_constant<int, V>{})
     if (cols <= 512) TQ_NORM_SHAPE(1, 1);
-    if (cols <= 1024) TQ_NORM_SHAPE(1, 2);
+    if (wave_a_row(rows, cols)) TQ_NORM_SHAPE(1, 2);
     if (cols <= 2048) TQ_NORM_SHAPE(4, 1);
     if (cols <= 4096) TQ_NORM_SHAPE(4, 2);
     if (cols <= 8192) TQ_NORM_SHAPE(8, 2);
@@ -425,13 +454,15 @@ hipError_t by_type(int dtype, F f)
     return dtype == TQ_BF16 ? f(std::integral_constant<int, TQ_BF16>{}) : f(std::integral_constant<int, TQ_F16>{});
 }
 
-uint32_t rows_at_once(uint32_t cols) { return cols <= 1024 ? 4 : 1; }
-
-// Workgroups that share the rows of a backward pass, and with it the partial sums.
+// Workgroups that share the rows of a backward pass, and with it the partial sums: each of them writes sums of its columns, which the last
+// kernel reads, so not more than it takes to keep memory busy.  16384 x 4096 bf16, us of the backward pass: 512 of them 83, 768 86, 1024
+// (without the next row's requests) 138.
 uint32_t parts_of(uint64_t rows, uint64_t cols)
 {
     if (cols > kMostInRegisters) return (uint32_t)(rows < 64 ? rows : 64);
-    const uint64_t most = cols <= 4096 ? 1024 : cols <= 8192 ? 512 : 256, r = rows_at_once((uint32_t)cols), wanted = (rows + r - 1) / r;
+    const bool alone = wave_a_row(rows, cols);                     // four rows in a workgroup then
+    const uint64_t most = alone ? (rows < 8192 ? 256 : 512) : cols <= 2048 ? 768 : cols <= 8192 ? 512 : 256;
+    const uint64_t wanted = alone ? (rows + 3) / 4 : rows;
     return (uint32_t)(wanted < most ? wanted : most);
 }
 
@@ -462,7 +493,7 @@ hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, 
                 norm_forward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
             }
-            return by_shape(a.cols, [&](auto N, auto V) -> hipError_t {
+            return by_shape(a.rows, a.cols, [&](auto N, auto V) -> hipError_t {
                 constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
                 const uint32_t each = kThreads / (kN * 64);
                 if (!fold_grid((rows + each - 1) / each, kThreads, 1, grid)) return hipErrorInvalidValue;
@@ -513,7 +544,7 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
                 norm_backward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
             }
-            return by_shape(a.cols, [&](auto N, auto V) -> hipError_t {
+            return by_shape(a.rows, a.cols, [&](auto N, auto V) -> hipError_t {
                 constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
                 if (!fold_grid(a.parts, kThreads, 1, grid)) return hipErrorInvalidValue;
                 norm_backward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
