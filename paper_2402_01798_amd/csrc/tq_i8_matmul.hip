@@ -281,7 +281,7 @@ constexpr uint64_t kKeptBytes = 30 << 10;      // of A in LDS, beside rings of 4
 //   24 x 8192 x 8192              21.7     17.4     17.8     18.0
 // Requests of 1024 bytes of one row, with a barrier for every 32 rows of that, took as long or longer (8192 x 8192 19.4, 14336 x 4096 14.1).
 
-enum Shape { kFewShape, k256, k192, k256x128, k128x256, k128, k64 };
+enum Shape { kFewShape, k256, k192, k192x256, k256x128, k128x256, k128x320, k128, k64 };
 
 // A tile's sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute unit, and what
 // a round of them costs beside that.
@@ -291,7 +291,8 @@ struct Pace {
     uint32_t ns[3], round;
 };
 constexpr Pace kPaces[] = {{k256, 256, 256, {1553, 0, 0}, 12000},   {k192, 192, 192, {943, 0, 0}, 9000},      {k256x128, 256, 128, {853, 0, 0}, 9000},
-                           {k128x256, 128, 256, {870, 0, 0}, 9000}, {k128, 128, 128, {580, 925, 0}, 8000}, {k64, 64, 64, {262, 375, 560}, 3500}};
+                           {k128x256, 128, 256, {870, 0, 0}, 9000}, {k192x256, 192, 256, {1200, 0, 0}, 10000},
+                           {k128x320, 128, 320, {1030, 0, 0}, 9000}, {k128, 128, 128, {580, 925, 0}, 8000}, {k64, 64, 64, {262, 375, 560}, 3500}};
 
 uint64_t pace(const Pace& p, uint64_t m, uint64_t n, uint64_t groups)
 {
@@ -314,7 +315,7 @@ uint32_t splits_of(uint64_t m, uint64_t n, uint64_t groups)
 {
     if (shape_of(m, n, groups) != k64) return 1;
     const uint64_t tiles = (m + 63) / 64 * ((n + 63) / 64), most = 2 * kComputeUnits / tiles, wanted = groups / 8, s = wanted < most ? wanted : most;
-    return s > 1 && (groups - groups / s) * kPaces[5].ns[0] >= 6000 ? (uint32_t)s : 1;
+    return s > 1 && (groups - groups / s) * kPaces[7].ns[0] >= 6000 ? (uint32_t)s : 1;
 }
 
 template <int DTYPE>
@@ -329,6 +330,8 @@ hipError_t launch_matmul(I8MatmulArgs& g, hipStream_t st)
         case k256: return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 4, 128, 2>>(g, st);
         case k192: return launch_tiles<DTYPE, TileShape<kInt8, 192, 192, 2, 6, 128, 3>>(g, st);
         case k256x128: return launch_tiles<DTYPE, TileShape<kInt8, 256, 128, 4, 2, 128, 3>>(g, st);
+        case k192x256: return launch_tiles<DTYPE, TileShape<kInt8, 192, 256, 2, 4, 128, 2>>(g, st);
+        case k128x320: return launch_tiles<DTYPE, TileShape<kInt8, 128, 320, 4, 2, 128, 2>>(g, st);
         case k128x256: return launch_tiles<DTYPE, TileShape<kInt8, 128, 256, 2, 4, 128, 3>>(g, st);
         case k128: return launch_tiles<DTYPE, TileShape<kInt8, 128, 128, 2, 4, 128, 2>>(g, st);
         case k64: break;
