@@ -137,7 +137,7 @@ def lib():
                   L.tq_i8_linear, L.tq_orthogonalize, L.tq_orthogonalize_multi, L.tq_orthogonal_update,
                   L.tq_orthogonal_update_multi):
             f.restype = i32
-        for name in (*_NATIVE, *_NATIVE_LEARN):
+        for name in (*_NATIVE, *_NATIVE_LEARN, *_NATIVE_LAYER):
             f = getattr(L, name)
             f.address = C.cast(f, C.c_void_p).value
         _lib = L
@@ -154,26 +154,33 @@ _NATIVE = {"tq_stats": "stats", "tq_stats_multi": "stats_multi", "tq_params": "p
            "tq_decompress_aggregate_segments": "aggregate_segments"}
 
 
-# The same for the calls of tq_mx.h, tq_distill.h, tq_norm.h and tq_i8.h.
+# The same for the calls of tq_mx.h and tq_distill.h.
 _NATIVE_LEARN = {"tq_mx_quantize": "mx_quantize", "tq_mx_dequantize": "mx_dequantize", "tq_mx_matmul": "mx_matmul",
                  "tq_mx_linear": "mx_linear", "tq_distill_forward": "distill_forward", "tq_distill_backward": "distill_backward",
-                 "tq_distill": "distill", "tq_layernorm_forward": "layernorm_forward",
-                 "tq_layernorm_backward": "layernorm_backward", "tq_i8_quantize": "i8_quantize",
-                 "tq_i8_dequantize": "i8_dequantize", "tq_i8_matmul": "i8_matmul", "tq_i8_linear": "i8_linear"}
+                 "tq_distill": "distill"}
+# And of tq_norm.h and tq_i8.h.
+_NATIVE_LAYER = {"tq_layernorm_forward": "layernorm_forward", "tq_layernorm_backward": "layernorm_backward",
+                 "tq_i8_quantize": "i8_quantize", "tq_i8_dequantize": "i8_dequantize", "tq_i8_matmul": "i8_matmul",
+                 "tq_i8_linear": "i8_linear"}
 _native_calls = {}
 
 
-def _native_learn(name, *args):
+def _native_learn(name, *args, table=_NATIVE_LEARN):
     """As _native."""
     call = _native_calls.get(name)
     if call is None:
         if _tq_marshal is None:
             return False
-        call = _native_calls[name] = (getattr(_tq_marshal, _NATIVE_LEARN[name]), getattr(lib(), name).address)
+        call = _native_calls[name] = (getattr(_tq_marshal, table[name]), getattr(lib(), name).address)
     rc = call[0](call[1], *args)
     if rc:
         raise TqError(rc, name)
     return rc is not None
+
+
+def _native_layer(name, *args):
+    """As _native."""
+    return _native_learn(name, *args, table=_NATIVE_LAYER)
 
 
 def _native(name, *args):
@@ -792,7 +799,7 @@ def layernorm_workspace_bytes(rows, cols):
 def tq_layernorm_forward(x, weight, bias, y, stats=None, eps=1e-5):
     """y = (x - mean) / sqrt(var + eps) * weight + bias for each row; ``weight`` and ``bias`` may be None.  ``stats`` [rows, 2]: what
     tq_layernorm_backward takes.  ``y`` may be ``x``."""
-    if _native_learn("tq_layernorm_forward", x, weight, bias, y, stats, eps):
+    if _native_layer("tq_layernorm_forward", x, weight, bias, y, stats, eps):
         return y
     px, code, rows, cols, ldx = _matrix_here(x, "x")
     py, _, _, _, ldy = _matrix_here(y, "y")
@@ -809,7 +816,7 @@ def tq_layernorm_forward(x, weight, bias, y, stats=None, eps=1e-5):
 
 def tq_layernorm_backward(x, dy, weight, stats, dx, dweight=None, dbias=None, workspace=None, accumulate=False):
     """``dx`` may be None, ``dy`` or ``x``; ``dweight`` and ``dbias`` float32, added to what they hold if ``accumulate``."""
-    if _native_learn("tq_layernorm_backward", x, dy, weight, stats, dx, dweight, dbias, workspace, accumulate):
+    if _native_layer("tq_layernorm_backward", x, dy, weight, stats, dx, dweight, dbias, workspace, accumulate):
         return dx, dweight, dbias
     px, code, rows, cols, ldx = _matrix_here(x, "x")
     pdy, _, _, _, lddy = _matrix_here(dy, "dy")
@@ -866,7 +873,7 @@ def i8_linear_workspace_bytes(m, n, k):
 
 def tq_i8_quantize(x, form):
     """``form`` takes x [rows, cols], with a scale for each row."""
-    if _native_learn("tq_i8_quantize", x, *form.all()):
+    if _native_layer("tq_i8_quantize", x, *form.all()):
         return form
     px, code, rows, cols, ld = _matrix_here(x, "x")
     if form.rows != rows or form.cols != cols:
@@ -876,7 +883,7 @@ def tq_i8_quantize(x, form):
 
 
 def tq_i8_dequantize(form, out):
-    if _native_learn("tq_i8_dequantize", *form.all(), out):
+    if _native_layer("tq_i8_dequantize", *form.all(), out):
         return out
     po, code, rows, cols, ld = _matrix_here(out, "out")
     if (rows, cols) != (form.rows, form.cols):
@@ -887,7 +894,7 @@ def tq_i8_dequantize(form, out):
 
 def tq_i8_matmul(a, b, out, workspace=None, bias=None):
     """out [m, n] = a [m, k] b [n, k]^T (+ bias [n], float32)."""
-    if _native_learn("tq_i8_matmul", *a.all(), *b.all(), out, workspace, bias):
+    if _native_layer("tq_i8_matmul", *a.all(), *b.all(), out, workspace, bias):
         return out
     po, code, m, n, ld = _matrix_here(out, "out")
     if a.cols != b.cols or a.rows != m or b.rows != n:
@@ -900,7 +907,7 @@ def tq_i8_matmul(a, b, out, workspace=None, bias=None):
 
 def tq_i8_linear(x, w, out, workspace=None, bias=None):
     """out [m, n] = Q(x [m, k]) w [n, k]^T (+ bias [n], float32), Q the rounding of tq_i8_quantize."""
-    if _native_learn("tq_i8_linear", x, *w.all(), out, workspace, bias):
+    if _native_layer("tq_i8_linear", x, *w.all(), out, workspace, bias):
         return out
     px, code, m, k, ldx = _matrix_here(x, "x")
     po, ocode, om, n, ldo = _matrix_here(out, "out")
