@@ -211,9 +211,19 @@ struct StepArgs {
     char* workspace;
     uint64_t stride, from_a, from_b, to, to_turned;    // places in a matrix's part of the workspace
     uint32_t m, n, k;                          // of this product
-    uint32_t tiles_x, tiles_y, tiles;
+    uint32_t tiles_x, tiles_y, tiles, count;   // tiles of each of `count` matrices
     float a, b, c;
 };
+
+// This workgroup's matrix and tile.  A die takes a run of them, of one matrix after the other: spread over the dies each die's cache would hold
+// something of all matrices (four of 1024 x 4096, pairs, X X^T).
+__device__ __forceinline__ bool find_tile(const StepArgs& s, uint32_t& which, uint32_t& tile)
+{
+    if (!tile_number(linear_block(), s.tiles * s.count, tile)) return false;
+    which = __builtin_amdgcn_readfirstlane(tile / s.tiles);
+    tile -= which * s.tiles;
+    return true;
+}
 
 // One of a step's first products, or its last where another step follows.
 template <class S, int WHAT>
@@ -221,11 +231,11 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_step_kernel(Step
 {
     extern __shared__ char lds[];
     constexpr int KIND = S::KIND;
-    uint32_t tile, ty, tx;
-    if (!tile_number(linear_block(), s.tiles, tile)) return;
+    uint32_t which, tile, ty, tx;
+    if (!find_tile(s, which, tile)) return;
     if (WHAT == kApply) tile_place(tile, s.tiles_y, s.tiles_x, ty, tx);
-    else tile_place_below(tile, ty, tx);
-    char* ws = s.workspace + blockIdx.y * s.stride;
+    else tile_place_below(tile, s.tiles_y, ty, tx);
+    char* ws = s.workspace + which * s.stride;
     const uint32_t groups = groups_of(KIND, s.k), row0 = ty * S::BM, col0 = tx * S::BN;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
     const TileOperands operands = {reinterpret_cast<uint8_t*>(ws + s.from_a), reinterpret_cast<uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
@@ -273,10 +283,10 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_end_kernel(EndAr
 {
     extern __shared__ char lds[];
     const StepArgs& s = a.s;
-    uint32_t tile, ty, tx;
-    if (!tile_number(linear_block(), s.tiles, tile)) return;
+    uint32_t which, tile, ty, tx;
+    if (!find_tile(s, which, tile)) return;
     tile_place(tile, s.tiles_y, s.tiles_x, ty, tx);
-    const uint32_t which = blockIdx.y, groups = groups_of(S::KIND, s.k);
+    const uint32_t groups = groups_of(S::KIND, s.k);
     const char* ws = s.workspace + which * s.stride;
     typename S::Sums acc[S::kFragsM][S::kFragsN];
     const TileOperands operands = {reinterpret_cast<const uint8_t*>(ws + s.from_a), reinterpret_cast<const uint8_t*>(ws + s.from_b), s.m, s.n, groups, 0, groups};
@@ -631,7 +641,8 @@ bool set_tiles(StepArgs& s, bool below, int count, dim3& grid)
     s.tiles_x = (s.n + S::BN - 1) / S::BN;
     s.tiles_y = (s.m + S::BM - 1) / S::BM;
     s.tiles = (uint32_t)tiles;
-    return tiles <= 0xFFFFFFF0ull && fold_grid((tiles + 7) / 8 * 8, S::kThreads, (unsigned)count, grid);
+    s.count = (uint32_t)count;
+    return tiles * count <= 0xFFFFFFF0ull && fold_grid((tiles * count + 7) / 8 * 8, S::kThreads, 1, grid);
 }
 
 template <int KIND, int WHAT>

@@ -239,13 +239,27 @@ __device__ __forceinline__ void tile_place(uint32_t tile, uint32_t tiles_y, uint
     ty = band * 4 + in % rows;
     tx = in / rows;
 }
-// Tile `tile` of those on and below the diagonal, row after row.
-__device__ __forceinline__ void tile_place_below(uint32_t tile, uint32_t& ty, uint32_t& tx)
+// Tile `tile` of those on and below the diagonal of `rows` x `rows`, in bands of 4 rows: down a band's rows and on to the next column, at its end
+// what there is of the diagonal's columns.  8 b^2 + 2 b of them come before band b.
+__device__ __forceinline__ void tile_place_below(uint32_t tile, uint32_t rows, uint32_t& ty, uint32_t& tx)
 {
-    ty = (uint32_t)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
-    while ((uint64_t)(ty + 1) * (ty + 2) / 2 <= tile) ++ty;
-    while ((uint64_t)ty * (ty + 1) / 2 > tile) --ty;
-    tx = tile - (uint32_t)((uint64_t)ty * (ty + 1) / 2);
+    uint32_t b = (uint32_t)(sqrtf((float)tile * 0.125f));          // within one of it
+    while (b && 8 * b * b + 2 * b > tile) --b;
+    while (8 * (b + 1) * (b + 1) + 2 * (b + 1) <= tile) ++b;
+    uint32_t in = tile - (8 * b * b + 2 * b);
+    const uint32_t high = min(4u, rows - 4 * b);
+    if (in < 4 * b * high) {
+        tx = in / high;
+        ty = 4 * b + in % high;
+        return;
+    }
+    in -= 4 * b * high;
+    tx = 4 * b;
+    for (uint32_t left = high; in >= left; --left) {
+        in -= left;
+        ++tx;
+    }
+    ty = tx + in;
 }
 
 }  // namespace tq
