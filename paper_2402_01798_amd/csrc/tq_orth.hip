@@ -320,7 +320,8 @@ struct SmallArgs {
     float momentum, eps, eta, scale, weight_decay;
 };
 
-constexpr uint32_t kSmallWaves = 8, kSmallFrags = 4;              // 32 x 32 outputs that a wavefront may hold
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t kSmallWaves = 16, kSmallFrags = 2;              // 32 x 32 outputs that a wavefront may hold
 
 struct SmallPlan {
     uint32_t r, c, row_x, row_t, xt, a, b, bytes;                  // row_t: of X^T, A and B; bytes: of all four, once for each number of a pair
@@ -379,45 +380,52 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(OrthPointe
         }
         return n;
     };
-    double sum = 0.0;                                              // of squares, in binary64
-    float u[8], v[8];
-    for (uint32_t at = threadIdx.x * 8; at < size; at += kAll * 8) {
-        const int n = load(at, u, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) sum += (double)u[j] * (double)u[j];
-    }
-#pragma unroll
-    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    sum = 0.0;
-#pragma unroll
-    for (uint32_t w = 0; w < kSmallWaves; ++w) sum += part[w];
-    const double factor = (double)kUnit / (sqrt(sum) + (double)s.eps);
     auto put = [&](char* array, uint32_t stride, uint32_t row, uint32_t col, float v) {
         char* to = array + row * stride + col * 2;
         const _Float16 high = (_Float16)v;
         *reinterpret_cast<_Float16*>(to) = high;
         if constexpr (KIND == kHalfPair) *reinterpret_cast<_Float16*>(to + p.bytes) = (_Float16)low_part(v, high);
     };
-    for (uint32_t at = threadIdx.x * 8; at < size; at += kAll * 8) {
-        const int n = load(at, u, v);
-        if constexpr (UPDATE) store8<TQ_F32>(q.v_out[which] + at, n, v);
-        uint32_t row = at / s.cols, col = at % s.cols;
+    double sum = 0.0, factor = 0.0;                                // of squares, in binary64
+#pragma nounroll
+    for (int pass = 0; pass < 2; ++pass) {                         // one code for both: what is not in the instruction cache yet is waited for
+#pragma nounroll
+        for (uint32_t at = threadIdx.x * 8; at < size; at += kAll * 8) {
+            float u[8], v[8];
+            const int n = load(at, u, v);
+            if (pass == 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j >= n) break;
-            const float held = (float)((double)u[j] * factor);
-            put(flip ? xt : x, flip ? p.row_t : p.row_x, row, col, held);
-            put(flip ? x : xt, flip ? p.row_x : p.row_t, col, row, held);
-            if (++col == s.cols) {
-                col = 0;
-                ++row;
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) sum += (double)u[j] * (double)u[j];
+                continue;
+            }
+            if constexpr (UPDATE) store8<TQ_F32>(q.v_out[which] + at, n, v);
+            uint32_t row = at / s.cols, col = at % s.cols;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j >= n) break;
+                const float held = (float)((double)u[j] * factor);
+                put(flip ? xt : x, flip ? p.row_t : p.row_x, row, col, held);
+                put(flip ? x : xt, flip ? p.row_x : p.row_t, col, row, held);
+                if (++col == s.cols) {
+                    col = 0;
+                    ++row;
+                }
             }
         }
+        if (pass == 0) {
+#pragma unroll
+            for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+            if (lane == 0) part[wave] = sum;
+        }
+        __syncthreads();
+        if (pass == 0) {
+            sum = 0.0;
+#pragma unroll
+            for (uint32_t w = 0; w < kSmallWaves; ++w) sum += part[w];
+            factor = (double)kUnit / (sqrt(sum) + (double)s.eps);
+        }
     }
-    __syncthreads();
 
     // 32 x 32 outputs of rows of two arrays; a lane's 16 as in tiles.  32 of k at a time, the next 32 on their way.
     auto product = [&](const char* from_a, const char* from_b, uint32_t stride, uint32_t row_a, uint32_t row_b, uint32_t k) {
@@ -463,7 +471,6 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(OrthPointe
     auto col_of = [&](uint32_t col0, int e) { return col0 + (e / 4) * 8 + (me >> 5) * 4 + e % 4; };
     // Into an array, 4 columns at a time.
     auto place = [&](char* to, uint32_t stride, uint32_t row0, uint32_t col0, const typename P::Sums& v) {
-        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             f16x4 high, low;
@@ -494,11 +501,19 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(OrthPointe
             asm volatile("" : "+v"(me));
             typename P::Sums v = product(a, a, p.row_t, row0, col0, p.r);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 16; e += 4) {
                 const char* from = a + row_of(row0) * p.row_t + col_of(col0, e) * 2;
-                float gram = (float)*reinterpret_cast<const _Float16*>(from);
-                if constexpr (KIND == kHalfPair) gram += (float)*reinterpret_cast<const _Float16*>(from + p.bytes);
-                v[e] = fmaf(fc, v[e] * (1.0f / kUnit), fmaf(fb, gram, row_of(row0) == col_of(col0, e) ? fa * kUnit : 0.0f));
+                f16x4 high = *reinterpret_cast<const f16x4*>(from), low = {};
+                if constexpr (KIND == kHalfPair) low = *reinterpret_cast<const f16x4*>(from + p.bytes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float gram = KIND == kHalfPair ? (float)high[i] + (float)low[i] : (float)high[i];
+                    v[e + i] = fmaf(fc, v[e + i] * (1.0f / kUnit), fb * gram);
+                }
+            }
+            if (row0 == col0) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] += row_of(0) == col_of(0, e) ? fa * kUnit : 0.0f;
             }
             place(b, p.row_t, row0, col0, v);
         }
@@ -511,36 +526,37 @@ __global__ __launch_bounds__(kSmallWaves * 64) void orth_small_kernel(OrthPointe
             if (at < down * across) held[f] = product(b, xt, p.row_t, at % down * 32, at / down * 32, p.r);
         }
         __syncthreads();
+        const bool end = step + 1 == s.steps;
 #pragma unroll
         for (uint32_t f = 0; f < kSmallFrags; ++f) {
             const uint32_t at = wave + f * kSmallWaves, row0 = at % down * 32, col0 = at / down * 32;
             if (at >= down * across) continue;
             asm volatile("" : "+v"(me));
-            if (step + 1 < s.steps) {
+            if (end) {                                             // as binary32, in place of everything
+#pragma unroll
+                for (int e = 0; e < 16; ++e) reinterpret_cast<float*>(lds)[row_of(row0) * p.c + col_of(col0, e)] = held[f][e] * (1.0f / (kUnit * kUnit));
+            } else {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) held[f][e] *= 1.0f / kUnit;
                 place(x, p.row_x, row0, col0, held[f]);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) put(xt, p.row_t, col_of(col0, e), row_of(row0), held[f][e]);
-                continue;
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t i = flip ? col_of(col0, e) : row_of(row0), j = flip ? row_of(row0) : col_of(col0, e);
-                if (i >= s.rows || j >= s.cols) continue;
-                const uint32_t to = i * s.cols + j;
-                float v = held[f][e] * (1.0f / (kUnit * kUnit));
-                if constexpr (UPDATE) {
-                    const float theta = s.theta[which][to];
-                    static_cast<float*>(s.out[which])[to] = theta - s.eta * (s.scale * v + s.weight_decay * theta);
-                } else if (s.out_dtype == TQ_F32) {
-                    static_cast<float*>(s.out[which])[to] = v;
-                } else {
-                    static_cast<uint16_t*>(s.out[which])[to] = s.out_dtype == TQ_BF16 ? Element<TQ_BF16>::store(v) : Element<TQ_F16>::store(v);
-                }
             }
         }
         __syncthreads();
+    }
+#pragma nounroll
+    for (uint32_t at = threadIdx.x; at < size; at += kAll) {
+        const uint32_t i = at / s.cols, j = at - i * s.cols;
+        float o = reinterpret_cast<const float*>(lds)[flip ? j * p.c + i : i * p.c + j];
+        if constexpr (UPDATE) {
+            const float theta = s.theta[which][at];
+            static_cast<float*>(s.out[which])[at] = theta - s.eta * (s.scale * o + s.weight_decay * theta);
+        } else if (s.out_dtype == TQ_F32) {
+            static_cast<float*>(s.out[which])[at] = o;
+        } else {
+            static_cast<uint16_t*>(s.out[which])[at] = s.out_dtype == TQ_BF16 ? Element<TQ_BF16>::store(o) : Element<TQ_F16>::store(o);
+        }
     }
 }
 
