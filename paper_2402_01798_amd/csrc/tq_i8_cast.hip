@@ -74,16 +74,17 @@ struct I8ValuesArgs {
     const float* scales;
     void* out;
     uint64_t ldo;
-    uint32_t rows, cols, octs, blocks;         // octs: eights of a row of codes; blocks: workgroups of a row
+    uint32_t rows, cols, octs, used;           // eights of a row of codes, and those with elements
 };
 
 template <int DTYPE>
 __global__ __launch_bounds__(256) void i8_values_kernel(I8ValuesArgs a)
 {
     using T = typename Element<DTYPE>::type;
-    const uint64_t block = linear_block(), row = block / a.blocks;
-    const uint32_t oct = (uint32_t)(block - row * a.blocks) * 256 + threadIdx.x;
-    if (row >= a.rows || (uint64_t)oct * 8 >= a.cols) return;
+    const uint64_t at = (uint64_t)linear_block() * 256 + threadIdx.x;          // rows follow each other: no workgroup is left with a row's few last
+    const uint64_t row = at >> 32 ? at / a.used : (uint32_t)at / a.used;
+    if (row >= a.rows) return;
+    const uint32_t oct = (uint32_t)(at - row * a.used);
     const float scale = a.scales[row];
     const u32x2 w = *reinterpret_cast<const u32x2*>(a.codes + (row * a.octs + oct) * 8);
     float v[8];
@@ -107,6 +108,8 @@ hipError_t launch_cast(const I8CastArgs& a, hipStream_t st)
 {
     if (a.octs <= 64) return launch_cast<DTYPE, 1, 1>(a, st);
     if (a.octs <= 256) return launch_cast<DTYPE, 4, 1>(a, st);
+    if (a.octs <= 512) return launch_cast<DTYPE, 4, 2>(a, st);
+    if (a.octs <= 768) return launch_cast<DTYPE, 4, 3>(a, st);
     if (a.octs <= 1024) return launch_cast<DTYPE, 4, 4>(a, st);
     if (a.octs <= 4096) return launch_cast<DTYPE, 16, 4>(a, st);
     return launch_cast<DTYPE, 16, 0>(a, st);
@@ -129,9 +132,9 @@ hipError_t tq_launch_i8_dequantize(const void* codes, const float* scales, uint6
 {
     using namespace tq;
     const I8ValuesArgs a = {static_cast<const int8_t*>(codes), scales, out, ldo, (uint32_t)rows, (uint32_t)cols,
-                            (uint32_t)((cols + 127) / 128 * 16), (uint32_t)((cols + 2047) / 2048)};
+                            (uint32_t)((cols + 127) / 128 * 16), (uint32_t)((cols + 7) / 8)};
     dim3 grid;
-    if (!fold_grid(rows * a.blocks, 256, 1, grid)) return hipErrorInvalidValue;
+    if (!fold_grid((rows * a.used + 255) / 256, 256, 1, grid)) return hipErrorInvalidValue;
     if (dtype == TQ_F32) i8_values_kernel<TQ_F32><<<grid, 256, 0, st>>>(a);
     else if (dtype == TQ_BF16) i8_values_kernel<TQ_BF16><<<grid, 256, 0, st>>>(a);
     else i8_values_kernel<TQ_F16><<<grid, 256, 0, st>>>(a);

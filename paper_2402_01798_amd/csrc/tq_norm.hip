@@ -81,11 +81,11 @@ __device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, float (*
 
 // A row by WAVES wavefronts that hold it in registers, 8 V elements each lane; short rows several to a workgroup.
 template <int DTYPE, int WTYPE, int WAVES, int V>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_forward_kernel(NormArgs a)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_forward_kernel(NormArgs a)
 {
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
-    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
+    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES == 1 ? 4 : 1;
     __shared__ float part[kRows][2][WAVES][2];
     const uint32_t sub = threadIdx.x / kThreads, tid = threadIdx.x % kThreads;
     const uint64_t row = (uint64_t)linear_block() * kRows + sub;
@@ -196,11 +196,11 @@ __device__ __forceinline__ float deviation(float x, float quarter_mean, float fo
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
 // other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.
 template <int DTYPE, int WTYPE, int WAVES, int V>
-__global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
 {
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
-    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES < 4 ? 4 / WAVES : 1;
+    constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES == 1 ? 4 : 1;
     __shared__ float part[2][WAVES][2];
     __shared__ float sums[kRows > 1 ? kThreads * V * 8 : 1];
     static_assert(WAVES == 1 || kRows == 1, "barriers are for whole workgroups");
@@ -426,18 +426,23 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
     *to = a.accumulate ? *to + v : v;
 }
 
-// The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.  Between 513 and 1024 columns forward and
-// backward pass take, by one wavefront a row / by four, us: 300 x 1024 bf16 17.4 / 12.7, 1000 x 600 fp32 20.7 / 15.5, 4099 x 1001 fp32
-// 34.8 / 30.2, 4096 x 1024 bf16 24.6 / 25.0, 16384 x 1024 bf16 48.8 / 60: few rows want many wavefronts, many rows no barriers.
-bool wave_a_row(uint64_t rows, uint64_t cols) { return cols <= 512 || (cols <= 1024 && rows >= 8192); }
+// The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.  From 513 to 1024 columns forward and
+// backward pass take, by one / two / four wavefronts a row, us:
+//   300 x 1024 bf16      17.4   12.4   12.7        16384 x 1024 bf16   48.6   50.2   60
+//   1000 x 600 fp32      20.7   15.4   15.5        65536 x 700 bf16     148    243
+//   4099 x 1001 fp32     34.8   28.6   30.2        16384 x 1024 fp32   73.1   59.9
+//   4096 x 1024 bf16     24.6   21.3   25.0        65536 x 1024 fp32    290    245
+// Few rows want many wavefronts; many rows no barriers, if a wavefront has a row's two times 2 KiB on their way and the next row's.
+bool wave_a_row(uint64_t rows, uint64_t cols, int dtype) { return cols <= 512 || (cols <= 1024 && dtype != TQ_F32 && rows >= 8192); }
 
 template <typename F>
-hipError_t by_shape(uint32_t rows, uint32_t cols, F f)
+hipError_t by_shape(uint32_t rows, uint32_t cols, int dtype, F f)
 {
     auto as = [&](auto w, auto v) { return f(w, v); };
 #define TQ_NORM_SHAPE(WAVES, V) return as(std::integral_constant<int, WAVES>{}, std::integral_constant<int, V>{})
     if (cols <= 512) TQ_NORM_SHAPE(1, 1);
-    if (wave_a_row(rows, cols)) TQ_NORM_SHAPE(1, 2);
+    if (wave_a_row(rows, cols, dtype)) TQ_NORM_SHAPE(1, 2);
+    if (cols <= 1024) TQ_NORM_SHAPE(2, 1);
     if (cols <= 2048) TQ_NORM_SHAPE(4, 1);
     if (cols <= 4096) TQ_NORM_SHAPE(4, 2);
     if (cols <= 8192) TQ_NORM_SHAPE(8, 2);
@@ -457,10 +462,10 @@ hipError_t by_type(int dtype, F f)
 // Workgroups that share the rows of a backward pass, and with it the partial sums: each of them writes sums of its columns, which the last
 // kernel reads, so not more than it takes to keep memory busy.  16384 x 4096 bf16, us of the backward pass: 512 of them 83, 768 86, 1024
 // (without the next row's requests) 138.
-uint32_t parts_of(uint64_t rows, uint64_t cols)
+uint32_t parts_of(uint64_t rows, uint64_t cols, int dtype)
 {
     if (cols > kMostInRegisters) return (uint32_t)(rows < 64 ? rows : 64);
-    const bool alone = wave_a_row(rows, cols);                     // four rows in a workgroup then
+    const bool alone = wave_a_row(rows, cols, dtype);              // four rows in a workgroup then
     const uint64_t most = alone ? (rows < 8192 ? 256 : 512) : cols <= 2048 ? 768 : cols <= 8192 ? 512 : 256;
     const uint64_t wanted = alone ? (rows + 3) / 4 : rows;
     return (uint32_t)(wanted < most ? wanted : most);
@@ -493,8 +498,8 @@ hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, 
                 norm_forward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
             }
-            return by_shape(a.rows, a.cols, [&](auto N, auto V) -> hipError_t {
-                constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
+            return by_shape(a.rows, a.cols, dtype, [&](auto N, auto V) -> hipError_t {
+                constexpr int kN = decltype(N)::value, kThreads = kN == 1 ? 256 : kN * 64;
                 const uint32_t each = kThreads / (kN * 64);
                 if (!fold_grid((rows + each - 1) / each, kThreads, 1, grid)) return hipErrorInvalidValue;
                 norm_forward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
@@ -504,7 +509,11 @@ hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, 
     });
 }
 
-uint64_t tq_layernorm_workspace_bytes_impl(uint64_t rows, uint64_t cols) { return (uint64_t)tq::parts_of(rows, cols) * 2 * cols * sizeof(float); }
+uint64_t tq_layernorm_workspace_bytes_impl(uint64_t rows, uint64_t cols)
+{
+    const uint64_t a = tq::parts_of(rows, cols, TQ_F32), b = tq::parts_of(rows, cols, TQ_BF16);
+    return (a > b ? a : b) * 2 * cols * sizeof(float);
+}
 
 hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ldx, const void* dy, uint64_t lddy,
                                         const void* weight, int wtype, const float* stats, void* dx, uint64_t lddx, float* dweight,
@@ -526,7 +535,7 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
     a.partial = dweight || dbias ? static_cast<float*>(workspace) : nullptr;
     a.rows = (uint32_t)rows;
     a.cols = (uint32_t)cols;
-    a.parts = parts_of(rows, cols);
+    a.parts = parts_of(rows, cols, dtype);
     dim3 grid;
     const hipError_t e = by_type(dtype, [&](auto D) {
         return by_type(wtype, [&](auto W) -> hipError_t {
@@ -544,8 +553,8 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
                 norm_backward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
             }
-            return by_shape(a.rows, a.cols, [&](auto N, auto V) -> hipError_t {
-                constexpr int kN = decltype(N)::value, kThreads = kN < 4 ? 256 : kN * 64;
+            return by_shape(a.rows, a.cols, dtype, [&](auto N, auto V) -> hipError_t {
+                constexpr int kN = decltype(N)::value, kThreads = kN == 1 ? 256 : kN * 64;
                 if (!fold_grid(a.parts, kThreads, 1, grid)) return hipErrorInvalidValue;
                 norm_backward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
                 return hipGetLastError();
