@@ -10,7 +10,7 @@
  *
  *   rows, cols     1 .. TQ_ORTH_MAX_LENGTH, the smaller of them at most TQ_ORTH_MAX_SIDE
  *   count          1 .. TQ_ORTH_MAX_COUNT matrices of one shape in one call; *_host are host arrays of `count` device pointers.  Results
- *                  are those of `count` calls, bit for bit.
+ *                  are those of `count` calls, up to the order of a product's sums.
  *   steps          1 .. TQ_ORTH_MAX_STEPS
  *   coefficients_host   [steps][3] floats a, b, c of each step, or NULL: 3.4445, -4.7750, 2.0315 for all of them.  The polynomials have
  *                  to keep singular values that begin in [0, 1] within [-3, 3], and |a + b s^2 + c s^4| within 12 on the way;
@@ -37,7 +37,7 @@
 extern "C" {
 #endif
 
-#define TQ_ORTH_MAX_LENGTH (1 << 22)
+#define TQ_ORTH_MAX_LENGTH (1 << 21)
 #define TQ_ORTH_MAX_SIDE 32768
 #define TQ_ORTH_MAX_COUNT 64
 #define TQ_ORTH_MAX_STEPS 16

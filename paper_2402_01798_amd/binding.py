@@ -32,7 +32,7 @@ MX_NEAREST, MX_STOCHASTIC = 0, 1
 DISTILL_MAX_TOP = 1024
 I8_MAX_K = 131071
 ORTH_HALF, ORTH_SPLIT = 0, 1
-ORTH_MAX_LENGTH, ORTH_MAX_SIDE, ORTH_MAX_COUNT, ORTH_MAX_STEPS = 1 << 22, 32768, 64, 16
+ORTH_MAX_LENGTH, ORTH_MAX_SIDE, ORTH_MAX_COUNT, ORTH_MAX_STEPS = 1 << 21, 32768, 64, 16
 NBINS = 898
 MAX_WORKERS = 64
 STATS_BYTES = 3632

@@ -63,7 +63,7 @@ struct TileShape {
 };
 
 struct TileOperands {
-    const uint8_t *a, *b;          // rows of groups * 128 bytes, 256 of them within 2^32 bytes
+    const uint8_t *a, *b;          // rows of groups * 128 bytes; BM and BN of them and a row more within 2^32 bytes, which offsets are checked against
     uint32_t m, n, groups;
     uint32_t first, count;         // the groups of k that are summed
 };

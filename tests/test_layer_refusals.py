@@ -132,7 +132,7 @@ def test_orthogonalize(L):
                 dict(precision=-1), dict(eps=0.0), dict(eps=NAN), dict(eps=INF), dict(ws=None), dict(nbytes=need - 1), dict(out=P, odtype=1)):
         assert call(**bad) == B.EINVAL, bad
     assert call(g=ODD) == call(out=ODD) == call(ws=ODD) == B.EALIGN
-    assert call(steps=17) == call(rows=32769, cols=32769) == call(rows=1 << 31) == call(rows=3, cols=(1 << 22) + 1) == B.EUNSUPPORTED
+    assert call(steps=17) == call(rows=32769, cols=32769) == call(rows=1 << 31) == call(rows=3, cols=(1 << 21) + 1) == B.EUNSUPPORTED
 
 
 def test_coefficients(L):
