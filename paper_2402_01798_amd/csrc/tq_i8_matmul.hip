@@ -36,6 +36,8 @@ __device__ __forceinline__ void store_scaled(const I8MatmulArgs& g, uint32_t row
     store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + row * g.ldo + col, n, v);
 }
 
+// 8192^3 to bf16: 460 to 480 us (2.3 to 2.4 POP/s; a library's product 558).  The matrix units are busy 67 % of the clocks, and the clock is 1.7 GHz then:
+// power bounds it.  Tiles of four wavefronts of 128 x 128 keep the units less busy (506 us).
 template <int DTYPE, class S>
 __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void i8_tile_kernel(I8MatmulArgs g)
 {
@@ -66,6 +68,7 @@ __global__ __launch_bounds__(256) void i8_join_kernel(I8MatmulArgs g)
     const uint32_t col = (uint32_t)(at - row * chunks) * 8;
     const int n = (int)min(g.n - col, 8u);
     int sums[8] = {};
+#pragma unroll 8
     for (uint32_t s = 0; s < g.splits; ++s) {
         float bits[8];
         load8<TQ_F32>(reinterpret_cast<const float*>(g.partial) + (s * (uint64_t)g.m + row) * g.n + col, n, bits);
@@ -284,7 +287,15 @@ constexpr uint64_t kKeptBytes = 30 << 10;      // of A in LDS, beside rings of 4
 enum Shape { kFewShape, k256, k192, k192x256, k256x128, k128x256, k128x320, k128, k64 };
 
 // A tile's sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute unit, and what
-// a round of them costs beside that.
+// a round of them costs beside that.  Us of bf16 products by shape:
+//                         256   192x256  192   256x128  128x256  128x320   128     rule
+//   1037 x 8192 x 4096    54.9   48.1    63.9   62.6     61.1     48.3    58.6     47.5
+//   600 x 14336 x 4096    55.0   49.6    63.4   62.5     60.9     47.2    59.5     47.4
+//   1500 x 4000 x 8192    82.6   72.6    62.3   62.7     63.4     68.0    64.9     62.4
+//   2000 x 6000 x 4096    59.5   83.4    66.7   65.0     66.3     74.9    64.5     59.3
+//   3500 x 2816 x 4096    55.5   52.7    64.2   61.9     62.2     49.9    60.6     50.6
+//   5000 x 5000 x 3000    92.3  104      92.6  103      106       97.4   102       91.7
+//   2056 x 1000 x 1999    28.4   22.4    17.8   17.5     17.4     20.4    12.1     13.2
 struct Pace {
     Shape shape;
     uint64_t bm, bn;
@@ -310,12 +321,21 @@ Shape shape_of(uint64_t m, uint64_t n, uint64_t groups)
     return best->shape;
 }
 
-// Over how many workgroups k is split where few tiles of 64 leave compute units idle.
+// Over how many workgroups k is split where few tiles of 64 leave compute units idle: as many as take least with the second launch and the partial
+// sums' way through memory.  Not split / split, us: 40 x 1000 x 16384 31.3 / 11.5, 128 x 1024 x 16384 31.5 / 12.6, 64 x 64 x 65536 112 / 14.9,
+// 256 x 512 x 8192 17.6 / 11.1, 64 x 4096 x 8192 18.0 / 12.5; 100 x 4096 x 4096 stays whole, 10.7 (in 4 parts 13.4).
 uint32_t splits_of(uint64_t m, uint64_t n, uint64_t groups)
 {
     if (shape_of(m, n, groups) != k64) return 1;
-    const uint64_t tiles = (m + 63) / 64 * ((n + 63) / 64), most = 2 * kComputeUnits / tiles, wanted = groups / 8, s = wanted < most ? wanted : most;
-    return s > 1 && (groups - groups / s) * kPaces[7].ns[0] >= 6000 ? (uint32_t)s : 1;
+    const uint64_t tiles = (m + 63) / 64 * ((n + 63) / 64);
+    uint64_t best = 1, least = 0;
+    for (uint64_t s = 1; s <= 64 && s * 4 <= groups && tiles * s <= 2 * kComputeUnits; ++s) {
+        const uint64_t ns = (groups + s - 1) / s * (tiles * s <= kComputeUnits ? 262 : 375) + (s > 1 ? 5000 + s * m * n * 8 / 5000 : 0);
+        if (s > 1 && ns >= least) continue;
+        least = ns;
+        best = s;
+    }
+    return (uint32_t)best;
 }
 
 template <int DTYPE>

@@ -79,7 +79,8 @@ __device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, float (*
     return s;
 }
 
-// A row by WAVES wavefronts that hold it in registers, 8 V elements each lane; short rows several to a workgroup.
+// A row by WAVES wavefronts that hold it in registers, 8 V elements each lane; short rows several to a workgroup.  Read once, written once:
+// memory bounds it (16384 x 4096 bf16 57 us, 4.7 TB/s; 4096 x 32768 130), a launch where there are few rows (1 x 4096 3.2).
 template <int DTYPE, int WTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_forward_kernel(NormArgs a)
 {
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_forward_ke
 
 constexpr int kLongWaves = 16;
 
-// Rows that do not fit the registers, by a workgroup each, read anew for every pass.
+// Rows that do not fit the registers, by a workgroup each, read anew for every pass, from the caches if they are there: 1000 x 60000 bf16 72 us.
 template <int DTYPE, int WTYPE>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_forward_long_kernel(NormArgs a)
 {
@@ -194,7 +195,8 @@ __device__ __forceinline__ float deviation(float x, float quarter_mean, float fo
 }
 
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
-// other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.
+// other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.  16384 x 4096 bf16 78 us, 5.2 TB/s:
+// memory; without the next row's requests, and with weights read for every row, 127.
 template <int DTYPE, int WTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
 {
@@ -329,12 +331,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
     }
 }
 
-// dx of a row that does not fit the registers.
-template <int DTYPE, int WTYPE>
+// dx of a row whose sums over rows are left to norm_columns_kernel: held in registers (V > 0, 8 V elements a lane) or read twice.  4096 x 32768
+// bf16 207 / 213 us (3.9 TB/s); two workgroups on a unit, whose registers then spill, 266.
+template <int DTYPE, int WTYPE, int V>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(NormArgs a)
 {
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
+    constexpr uint32_t kThreads = kLongWaves * 64;
     __shared__ float part[kLongWaves][2];
     const uint64_t row = linear_block();
     if (row >= a.rows) return;
@@ -343,42 +347,72 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
     T* dx = static_cast<T*>(a.out) + row * a.ldo;
     const float quarter = 0.25f * a.stats_in[2 * row], r = a.stats_in[2 * row + 1], four = 4.0f * r;
     const uint32_t octs = (uint32_t)(((uint64_t)a.cols + 7) / 8);
-    float s1 = 0.0f, s2 = 0.0f;
-    auto each = [&](auto f) {
-        for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
-            const int n = left_of(a.cols, oct);
-            float v[8], g[8], weight[8];
-            load8<DTYPE>(x + (uint64_t)oct * 8, n, v);
-            load8<DTYPE>(dy + (uint64_t)oct * 8, n, g);
-            if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = deviation(v[j], quarter, four);
-                if (a.weight) g[j] *= weight[j];
-            }
-            f(oct, n, v, g);
+    Eight<DTYPE> wx[V ? V : 1], wdy[V ? V : 1];
+    auto fetch = [&](int i, uint32_t oct) {
+        const int n = left_of(a.cols, oct);
+        if (n == 8) {
+            wx[i].load(x + (uint64_t)oct * 8);
+            wdy[i].load(dy + (uint64_t)oct * 8);
+        } else {                                                   // behind the end 0, which adds nothing
+            wx[i].load(x + (uint64_t)oct * 8, n);
+            wdy[i].load(dy + (uint64_t)oct * 8, n);
         }
     };
-    each([&](uint32_t, int n, const float (&h)[8], const float (&g)[8]) {
+    auto values = [&](int i, uint32_t oct, float (&h)[8], float (&g)[8]) {
+        float weight[8];
+        wx[i].unpack(h);
+        wdy[i].unpack(g);
+        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, left_of(a.cols, oct), weight);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) {
-                s1 += g[j];
-                s2 = fmaf(g[j], h[j], s2);
-            }
-    });
+        for (int j = 0; j < 8; ++j) {
+            h[j] = deviation(h[j], quarter, four);
+            if (a.weight) g[j] *= weight[j];
+        }
+    };
+    float s1 = 0.0f, s2 = 0.0f, h[8], g[8];
+    auto add = [&](int i, uint32_t oct) {
+        values(i, oct, h, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s1 += g[j];
+            s2 = fmaf(g[j], h[j], s2);
+        }
+    };
+    auto put = [&](int i, uint32_t oct) {
+        values(i, oct, h, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = r * ((g[j] - s1) - h[j] * s2);
+        store8<DTYPE>(dx + (uint64_t)oct * 8, left_of(a.cols, oct), h);
+    };
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (threadIdx.x + i * kThreads < octs) fetch(i, threadIdx.x + i * kThreads);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (threadIdx.x + i * kThreads < octs) add(i, threadIdx.x + i * kThreads);
+    } else {
+        for (uint32_t oct = threadIdx.x; oct < octs; oct += kThreads) {
+            fetch(0, oct);
+            add(0, oct);
+        }
+    }
     row_total<kLongWaves>(s1, s2, part);
     s1 /= (float)a.cols;
     s2 /= (float)a.cols;
-    each([&](uint32_t oct, int n, const float (&h)[8], const float (&g)[8]) {
-        float v[8];
+    if constexpr (V > 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = r * ((g[j] - s1) - h[j] * s2);
-        store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
-    });
+        for (int i = 0; i < V; ++i)
+            if (threadIdx.x + i * kThreads < octs) put(i, threadIdx.x + i * kThreads);
+    } else {
+        for (uint32_t oct = threadIdx.x; oct < octs; oct += kThreads) {
+            fetch(0, oct);
+            put(0, oct);
+        }
+    }
 }
 
-// Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.
+// Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.  4096 x 32768 bf16 118 us, 4.5 TB/s.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, uint32_t across)
 {
@@ -404,7 +438,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, uint32_t 
     store8<TQ_F32>(to + a.cols, n, db);
 }
 
-// The parts' sums, joined in a fixed order: 32 columns of dweight and dbias by 32 threads each.
+// The parts' sums, joined in a fixed order: 32 columns of dweight and dbias by 32 threads each.  512 parts of 4096 columns 5 us.
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
 {
     __shared__ float sums[32][33];
@@ -446,11 +480,13 @@ hipError_t by_shape(uint32_t rows, uint32_t cols, int dtype, F f)
     if (cols <= 2048) TQ_NORM_SHAPE(4, 1);
     if (cols <= 4096) TQ_NORM_SHAPE(4, 2);
     if (cols <= 8192) TQ_NORM_SHAPE(8, 2);
-    TQ_NORM_SHAPE(16, 2);
+    if (cols <= 16384) TQ_NORM_SHAPE(16, 2);
+    TQ_NORM_SHAPE(16, 4);
 #undef TQ_NORM_SHAPE
 }
 
-constexpr uint32_t kMostInRegisters = 16384;
+// Columns of rows that stay in registers: forward and for dx alone; with sums over rows.
+constexpr uint32_t kMostForward = 32768, kMostInRegisters = 16384;
 
 template <typename F>
 hipError_t by_type(int dtype, F f)
@@ -493,7 +529,7 @@ hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, 
         return by_type(wtype, [&](auto W) -> hipError_t {
             constexpr int kD = decltype(D)::value, kW = decltype(W)::value;
             dim3 grid;
-            if (cols > kMostInRegisters) {
+            if (cols > kMostForward) {
                 if (!fold_grid(rows, kLongWaves * 64, 1, grid)) return hipErrorInvalidValue;
                 norm_forward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
@@ -550,14 +586,19 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
                 }
                 if (!a.out) return hipSuccess;
                 if (!fold_grid(rows, kLongWaves * 64, 1, grid)) return hipErrorInvalidValue;
-                norm_backward_long_kernel<kD, kW><<<grid, kLongWaves * 64, 0, st>>>(a);
+                if (cols <= kMostForward) norm_backward_long_kernel<kD, kW, 4><<<grid, kLongWaves * 64, 0, st>>>(a);
+                else norm_backward_long_kernel<kD, kW, 0><<<grid, kLongWaves * 64, 0, st>>>(a);
                 return hipGetLastError();
             }
             return by_shape(a.rows, a.cols, dtype, [&](auto N, auto V) -> hipError_t {
-                constexpr int kN = decltype(N)::value, kThreads = kN == 1 ? 256 : kN * 64;
-                if (!fold_grid(a.parts, kThreads, 1, grid)) return hipErrorInvalidValue;
-                norm_backward_kernel<kD, kW, kN, decltype(V)::value><<<grid, kThreads, 0, st>>>(a);
-                return hipGetLastError();
+                constexpr int kN = decltype(N)::value, kV = decltype(V)::value, kThreads = kN == 1 ? 256 : kN * 64;
+                if constexpr (kN * kV * 512 > (int)kMostInRegisters) {
+                    return hipErrorInvalidValue;                   // taken above
+                } else {
+                    if (!fold_grid(a.parts, kThreads, 1, grid)) return hipErrorInvalidValue;
+                    norm_backward_kernel<kD, kW, kN, kV><<<grid, kThreads, 0, st>>>(a);
+                    return hipGetLastError();
+                }
             });
         });
     });

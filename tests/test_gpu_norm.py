@@ -48,7 +48,7 @@ def check(x, dy, w, b, dtype, eps=1e-5, extra=0, offset=0):
 
 
 SHAPES = [(1, 1), (3, 1), (2, 2), (5, 7), (1, 8), (9, 9), (64, 64), (33, 511), (7, 512), (6, 513), (10, 1001), (5, 1024), (3, 1025),
-          (2, 2047), (5, 2049), (3, 4096), (4, 4099), (2, 8192), (3, 8200), (2, 16384), (3, 16385), (2, 40001), (2500, 40), (1300, 130)]
+          (2, 2047), (5, 2049), (3, 4096), (4, 4099), (2, 8192), (3, 8200), (2, 16384), (3, 16385), (70, 20003), (2, 32768), (3, 32769), (2, 40001), (2500, 40), (1300, 130)]
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
