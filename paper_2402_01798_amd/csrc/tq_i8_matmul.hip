@@ -36,8 +36,9 @@ __device__ __forceinline__ void store_scaled(const I8MatmulArgs& g, uint32_t row
     store8<DTYPE>(static_cast<typename Element<DTYPE>::type*>(g.out) + row * g.ldo + col, n, v);
 }
 
-// 8192^3 to bf16: 460 to 480 us (2.3 to 2.4 POP/s; a library's product 558).  The matrix units are busy 67 % of the clocks, and the clock is 1.7 GHz then:
-// power bounds it.  Tiles of four wavefronts of 128 x 128 keep the units less busy (506 us).
+// 8192^3 to bf16: 447 to 475 us (2.3 to 2.5 POP/s); a library's product to int32 of the same codes, in turn, 433 to 440.  The matrix units are busy 67 % of
+// the clocks at 1.7 GHz: the low clock points to power.  The first calls after a pause take 580 to 720.  Four wavefronts of 128 x 128 with slices of
+// 64 bytes, not tried apart: 506, units busy 61 %.
 template <int DTYPE, class S>
 __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void i8_tile_kernel(I8MatmulArgs g)
 {

@@ -39,7 +39,7 @@ __device__ __forceinline__ void load_eight(const void* p, uint64_t at, int n, fl
     load8<DTYPE>(static_cast<const typename Element<DTYPE>::type*>(p) + at, n, v);
 }
 
-// Sums of squares in binary64, and the new momentum.  Memory: four of 1024 x 4096 fp32 46 us, 4.4 TB/s.
+// Sums of squares in binary64, and the new momentum.  Memory: four of 1024 x 4096 fp32 48 us, 4.2 TB/s.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void orth_norm_kernel(OrthPointers p, OrthArgs o)
 {
@@ -225,8 +225,8 @@ __device__ __forceinline__ bool find_tile(const StepArgs& s, uint32_t& which, ui
     return true;
 }
 
-// One of a step's first products, or its last where another step follows.  4096 x 4096 in binary16: 80, 83 and 131 us, the matrix units busy 55 to 60 % of
-// the clocks; one round of tiles, whose first requests and stores (67 MB) take 20 to 30 us beside which nothing works.
+// One of a step's first products, or its last where another step follows.  4096 x 4096 in binary16: 80 to 83, 83 to 85 and 138 to 141
+// us, the matrix units busy 51, 49 and 56 % of the clocks.  Each is one round of tiles, so that nothing overlaps its first requests and last stores.
 template <class S, int WHAT>
 __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_step_kernel(StepArgs s)
 {
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(S::kThreads, S::kOnSimd) void orth_end_kernel(EndAr
 // Small matrices: a workgroup has X, X^T, A and B of one in its LDS and takes all steps in one launch, where the products of the kernels above
 // would each be a launch of a few us.  Rows are 16 bytes longer than their elements, so that 16 of them lie in different banks; everything is
 // padded to 32 with zeros.  Us, by the kernels above / this one: 64 x 256 61 / 31, 128 x 128 66 / 34, 128 x 160 67 / 40, 32 x 32 pairs 53 / 15,
-// 64 x 128 pairs 78 / 29, 32 x 900 80 / 51, 16 updates of 64 x 128 120 / 83.  Chains of LDS reads and matrix instructions bound it: its wavefronts
+// 64 x 128 pairs 78 / 29, 32 x 900 80 / 51 (the less of two runs), 16 updates of 64 x 128 120 / 83.  Chains of LDS reads and matrix instructions bound it: its wavefronts
 // wait for half of the time.
 struct SmallArgs {
     void* out[TQ_ORTH_MAX_COUNT];
