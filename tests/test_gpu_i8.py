@@ -101,7 +101,8 @@ def device_form(codes, scales, cols):
 MNK = [(1, 1, 1), (1, 17, 5), (3, 40, 129), (1, 300, 4096), (2, 65, 1000), (7, 100, 128), (16, 96, 513), (17, 33, 700), (31, 1000, 260),
        (32, 64, 4097), (33, 200, 300), (64, 64, 64), (65, 70, 2000), (100, 129, 255), (128, 128, 128), (129, 257, 385), (200, 1000, 1200),
        (300, 500, 64), (520, 260, 1), (1030, 300, 200), (700, 700, 700), (1, 9000, 300), (24, 8200, 130), (40, 8200, 130), (257, 4100, 130),
-       (2100, 2050, 140)]
+       (2100, 2050, 140),
+       (33, 65, 9001), (70, 130, 20011), (129, 257, 40007)]    # k in parts, the last of them shorter
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
