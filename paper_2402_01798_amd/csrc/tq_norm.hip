@@ -194,6 +194,18 @@ __device__ __forceinline__ float deviation(float x, float quarter_mean, float fo
     return fmaf(x, 0.25f, -quarter_mean) * four_rstd;
 }
 
+// Of 8 columns of which a row has n.  Behind its end h is 0: of the 0 that is held there it may be infinite, which no factor of 0 takes back.
+__device__ __forceinline__ void deviations(const float (&x)[8], int n, float quarter_mean, float four_rstd, float (&h)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = deviation(x[j], quarter_mean, four_rstd);
+    if (n < 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= n) h[j] = 0.0f;
+    }
+}
+
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
 // other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.  16384 x 4096 bf16 78 us, 5.2 TB/s:
 // memory; without the next row's requests, with weights read for every row and twice the parts, 127.
@@ -225,7 +237,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
             if (n == 8) {
                 next_x[i].load(x + (uint64_t)oct * 8);
                 next_dy[i].load(dy + (uint64_t)oct * 8);
-            } else if (n) {                                        // behind the end: dy = 0 and weight = 0, which add nothing
+            } else if (n) {                                        // behind the end: dy = 0, weight = 0 and h = 0, which add nothing
                 next_x[i].load(x + (uint64_t)oct * 8, n);
                 next_dy[i].load(dy + (uint64_t)oct * 8, n);
             } else {
@@ -264,18 +276,19 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float v[8], g[8];
+            float v[8], g[8], h[8];
             wx[i].unpack(v);
             wdy[i].unpack(g);
+            deviations(v, left_of(a.cols, tid + i * kThreads), quarter, four, h);
             if constexpr (!kAhead) weights_of(i, weights[0]);
             const float(&weight)[8] = weights[kAhead ? i : 0];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float h = deviation(v[j], quarter, four), gw = g[j] * weight[j];
-                dw[i][j] = fmaf(g[j], h, dw[i][j]);
+                const float gw = g[j] * weight[j];
+                dw[i][j] = fmaf(g[j], h[j], dw[i][j]);
                 db[i][j] += g[j];
                 s1 += gw;
-                s2 = fmaf(gw, h, s2);
+                s2 = fmaf(gw, h[j], s2);
             }
         }
         if (!a.out) continue;
@@ -353,21 +366,21 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
         if (n == 8) {
             wx[i].load(x + (uint64_t)oct * 8);
             wdy[i].load(dy + (uint64_t)oct * 8);
-        } else {                                                   // behind the end 0, which adds nothing
+        } else {                                                   // behind the end dy = 0 and h = 0, which add nothing
             wx[i].load(x + (uint64_t)oct * 8, n);
             wdy[i].load(dy + (uint64_t)oct * 8, n);
         }
     };
     auto values = [&](int i, uint32_t oct, float (&h)[8], float (&g)[8]) {
-        float weight[8];
-        wx[i].unpack(h);
+        const int n = left_of(a.cols, oct);
+        float v[8], weight[8];
+        wx[i].unpack(v);
         wdy[i].unpack(g);
-        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, left_of(a.cols, oct), weight);
+        deviations(v, n, quarter, four, h);
+        if (a.weight) load8<WTYPE>(static_cast<const W*>(a.weight) + (uint64_t)oct * 8, n, weight);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            h[j] = deviation(h[j], quarter, four);
+        for (int j = 0; j < 8; ++j)
             if (a.weight) g[j] *= weight[j];
-        }
     };
     float s1 = 0.0f, s2 = 0.0f, h[8], g[8];
     auto add = [&](int i, uint32_t oct) {
