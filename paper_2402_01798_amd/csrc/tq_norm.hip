@@ -12,6 +12,7 @@ struct NormArgs {
     void* out;                                 // y, or dx; dx may be NULL
     float* stats;
     float* partial;                            // [parts][2][cols]: sums of dy h and of dy
+    float* rest;                               // [rows]: the mean of h from rounded statistics, for rows over 16384 columns
     float *dweight, *dbias;
     uint64_t ldx, lddy, ldo;
     uint32_t rows, cols, parts;
@@ -188,7 +189,11 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_forward_long_kernel(Norm
     }
 }
 
-// h of an element: the difference in quarters, which two numbers of the largest magnitude do not take out of range.
+// The backward pass has the mean as one binary32 number m, up to 2^-24 |m| from the row's: where that is no small part of the deviation, h by it
+// is off in the whole row.  Its own mean d says how far, for that of h is 0: h - d takes m's place, and mean(g (h - d)) = mean(g h) - d mean(g), so
+// that d is one sum more beside the two that dx takes.
+
+// h of an element by m: the difference in quarters, which two numbers of the largest magnitude do not take out of range.
 __device__ __forceinline__ float deviation(float x, float quarter_mean, float four_rstd)
 {
     return fmaf(x, 0.25f, -quarter_mean) * four_rstd;
@@ -198,12 +203,7 @@ __device__ __forceinline__ float deviation(float x, float quarter_mean, float fo
 __device__ __forceinline__ void deviations(const float (&x)[8], int n, float quarter_mean, float four_rstd, float (&h)[8])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = deviation(x[j], quarter_mean, four_rstd);
-    if (n < 8) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j >= n) h[j] = 0.0f;
-    }
+    for (int j = 0; j < 8; ++j) h[j] = j < n ? deviation(x[j], quarter_mean, four_rstd) : 0.0f;
 }
 
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
     constexpr uint32_t kThreads = WAVES * 64, kRows = WAVES == 1 ? 4 : 1;
-    __shared__ float part[2][WAVES][2];
+    __shared__ float part[2][WAVES][3];
     __shared__ float sums[kRows > 1 ? kThreads * V * 8 : 1];
     static_assert(WAVES == 1 || kRows == 1, "barriers are for whole workgroups");
     const uint32_t sub = threadIdx.x / kThreads, tid = threadIdx.x % kThreads, block = linear_block();
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
         }
         const float quarter = 0.25f * next_mean, r = next_r, four = 4.0f * r;
         if constexpr (kAhead) fetch(row + step);
-        float s1 = 0.0f, s2 = 0.0f;
+        float sum[3] = {};                                         // of g, of g h and of h
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float v[8], g[8], h[8];
@@ -285,31 +285,33 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float gw = g[j] * weight[j];
-                dw[i][j] = fmaf(g[j], h[j], dw[i][j]);
-                db[i][j] += g[j];
-                s1 += gw;
-                s2 = fmaf(gw, h[j], s2);
+                sum[0] += gw;
+                sum[1] = fmaf(gw, h[j], sum[1]);
+                sum[2] += h[j];
             }
         }
-        if (!a.out) continue;
-        row_total<WAVES>(s1, s2, part[turn]);
+        row_totals<WAVES>(sum, part[turn]);
         turn ^= 1;
-        s1 *= n_inv;
-        s2 *= n_inv;
+        const float d = sum[2] * n_inv, s1 = sum[0] * n_inv, s2 = sum[1] * n_inv - d * s1;
         T* dx = static_cast<T*>(a.out) + row * a.ldo;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const uint32_t oct = tid + i * kThreads;
             const int n = left_of(a.cols, oct);
-            if (n == 0) continue;
+            if (!kAhead && n == 0) continue;                       // without this 16 wavefronts spill: 2048 x 16384 fp32 110 -> 137 us
             float v[8], g[8];
             wx[i].unpack(v);
             wdy[i].unpack(g);
             if constexpr (!kAhead) weights_of(i, weights[0]);
             const float(&weight)[8] = weights[kAhead ? i : 0];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = r * ((g[j] * weight[j] - s1) - deviation(v[j], quarter, four) * s2);
-            store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
+            for (int j = 0; j < 8; ++j) {
+                const float h = deviation(v[j], quarter, four) - d;
+                dw[i][j] = fmaf(g[j], h, dw[i][j]);
+                db[i][j] += g[j];
+                v[j] = r * ((g[j] * weight[j] - s1) - h * s2);
+            }
+            if (a.out && n) store8<DTYPE>(dx + (uint64_t)oct * 8, n, v);
         }
     }
     if (!a.partial) return;
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
     constexpr uint32_t kThreads = kLongWaves * 64;
-    __shared__ float part[kLongWaves][2];
+    __shared__ float part[kLongWaves][3];
     const uint64_t row = linear_block();
     if (row >= a.rows) return;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
@@ -382,19 +384,20 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
         for (int j = 0; j < 8; ++j)
             if (a.weight) g[j] *= weight[j];
     };
-    float s1 = 0.0f, s2 = 0.0f, h[8], g[8];
+    float sum[3] = {}, s1 = 0.0f, s2 = 0.0f, d = 0.0f, h[8], g[8];     // sums of g, of g h and of h
     auto add = [&](int i, uint32_t oct) {
         values(i, oct, h, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s1 += g[j];
-            s2 = fmaf(g[j], h[j], s2);
+            sum[0] += g[j];
+            sum[1] = fmaf(g[j], h[j], sum[1]);
+            sum[2] += h[j];
         }
     };
     auto put = [&](int i, uint32_t oct) {
         values(i, oct, h, g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[j] = r * ((g[j] - s1) - h[j] * s2);
+        for (int j = 0; j < 8; ++j) h[j] = r * ((g[j] - s1) - (h[j] - d) * s2);
         store8<DTYPE>(dx + (uint64_t)oct * 8, left_of(a.cols, oct), h);
     };
     if constexpr (V > 0) {
@@ -410,9 +413,11 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
             add(0, oct);
         }
     }
-    row_total<kLongWaves>(s1, s2, part);
-    s1 /= (float)a.cols;
-    s2 /= (float)a.cols;
+    row_totals<kLongWaves>(sum, part);
+    d = sum[2] / (float)a.cols;
+    s1 = sum[0] / (float)a.cols;
+    s2 = sum[1] / (float)a.cols - d * s1;
+    if (a.rest && threadIdx.x == 0) a.rest[row] = d;
     if constexpr (V > 0) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -423,6 +428,30 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
             put(0, oct);
         }
     }
+}
+
+// The mean of such a row's h alone, summed as above, bit for bit: where dx is not wanted, or takes the place of what norm_columns_kernel reads.
+template <int DTYPE>
+__global__ __launch_bounds__(kLongWaves * 64) void norm_rest_kernel(NormArgs a)
+{
+    using T = typename Element<DTYPE>::type;
+    __shared__ float part[kLongWaves][1];
+    const uint64_t row = linear_block();
+    if (row >= a.rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    const float quarter = 0.25f * a.stats_in[2 * row], four = 4.0f * a.stats_in[2 * row + 1];
+    const uint32_t octs = (uint32_t)(((uint64_t)a.cols + 7) / 8);
+    float sum[1] = {};
+    for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
+        const int n = left_of(a.cols, oct);
+        float v[8], h[8];
+        load8<DTYPE>(x + (uint64_t)oct * 8, n, v);
+        deviations(v, n, quarter, four, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[0] += h[j];
+    }
+    row_totals<kLongWaves>(sum, part);
+    if (threadIdx.x == 0) a.rest[row] = sum[0] / (float)a.cols;
 }
 
 // Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.  4096 x 32768 bf16 118 us, 4.5 TB/s.
@@ -439,10 +468,10 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, uint32_t 
         float v[8], g[8];
         load8<DTYPE>(static_cast<const T*>(a.x) + row * a.ldx + (uint64_t)oct * 8, n, v);
         load8<DTYPE>(static_cast<const T*>(a.dy) + row * a.lddy + (uint64_t)oct * 8, n, g);
-        const float quarter = 0.25f * a.stats_in[2 * row], four = 4.0f * a.stats_in[2 * row + 1];
+        const float quarter = 0.25f * a.stats_in[2 * row], four = 4.0f * a.stats_in[2 * row + 1], d = a.rest[row];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            dw[j] = fmaf(g[j], deviation(v[j], quarter, four), dw[j]);
+            dw[j] = fmaf(g[j], deviation(v[j], quarter, four) - d, dw[j]);
             db[j] += g[j];
         }
     }
@@ -561,7 +590,7 @@ hipError_t tq_launch_layernorm_forward(const void* x, int dtype, uint64_t rows, 
 uint64_t tq_layernorm_workspace_bytes_impl(uint64_t rows, uint64_t cols)
 {
     const uint64_t a = tq::parts_of(rows, cols, TQ_F32), b = tq::parts_of(rows, cols, TQ_BF16);
-    return (a > b ? a : b) * 2 * cols * sizeof(float);
+    return (a > b ? a : b) * 2 * cols * sizeof(float) + (cols > tq::kMostInRegisters ? rows * sizeof(float) : 0);
 }
 
 hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows, uint64_t cols, uint64_t ldx, const void* dy, uint64_t lddy,
@@ -590,18 +619,29 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
         return by_type(wtype, [&](auto W) -> hipError_t {
             constexpr int kD = decltype(D)::value, kW = decltype(W)::value;
             if (cols > kMostInRegisters) {
-                if (a.partial) {                                   // first: dx may take the place of what it reads
-                    const uint32_t across = (uint32_t)(((cols + 7) / 8 + 255) / 256);
-                    if (!fold_grid((uint64_t)across * a.parts, 256, 1, grid)) return hipErrorInvalidValue;
-                    norm_columns_kernel<kD><<<grid, 256, 0, st>>>(a, across);
-                    const hipError_t e = hipGetLastError();
-                    if (e != hipSuccess) return e;
+                dim3 by_row;
+                if (!fold_grid(rows, kLongWaves * 64, 1, by_row)) return hipErrorInvalidValue;
+                auto put_dx = [&]() -> hipError_t {
+                    if (cols <= kMostForward) norm_backward_long_kernel<kD, kW, 4><<<by_row, kLongWaves * 64, 0, st>>>(a);
+                    else norm_backward_long_kernel<kD, kW, 0><<<by_row, kLongWaves * 64, 0, st>>>(a);
+                    return hipGetLastError();
+                };
+                if (!a.partial) return put_dx();
+                a.rest = a.partial + (uint64_t)a.parts * 2 * cols;
+                const bool apart = a.out && a.out != x && a.out != dy;     // dx leaves what the columns' sums read: it may come first
+                hipError_t e;
+                if (apart) {
+                    e = put_dx();
+                } else {
+                    norm_rest_kernel<kD><<<by_row, kLongWaves * 64, 0, st>>>(a);
+                    e = hipGetLastError();
                 }
-                if (!a.out) return hipSuccess;
-                if (!fold_grid(rows, kLongWaves * 64, 1, grid)) return hipErrorInvalidValue;
-                if (cols <= kMostForward) norm_backward_long_kernel<kD, kW, 4><<<grid, kLongWaves * 64, 0, st>>>(a);
-                else norm_backward_long_kernel<kD, kW, 0><<<grid, kLongWaves * 64, 0, st>>>(a);
-                return hipGetLastError();
+                if (e != hipSuccess) return e;
+                const uint32_t across = (uint32_t)(((cols + 7) / 8 + 255) / 256);
+                if (!fold_grid((uint64_t)across * a.parts, 256, 1, grid)) return hipErrorInvalidValue;
+                norm_columns_kernel<kD><<<grid, 256, 0, st>>>(a, across);
+                e = hipGetLastError();
+                return e != hipSuccess || apart || !a.out ? e : put_dx();
             }
             return by_shape(a.rows, a.cols, dtype, [&](auto N, auto V) -> hipError_t {
                 constexpr int kN = decltype(N)::value, kV = decltype(V)::value, kThreads = kN == 1 ? 256 : kN * 64;

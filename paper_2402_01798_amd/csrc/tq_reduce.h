@@ -23,28 +23,36 @@ __device__ __forceinline__ float wave_total(float v)
 
 __device__ __forceinline__ uint32_t wave_largest(uint32_t v) { return stride16_max(row16_max(v)); }
 
-// Of two values over the WAVES wavefronts of a row, in a fixed order.  `part` [WAVES][2] is this row's and is used once between two
+// Of N values over the WAVES wavefronts of a row, in a fixed order.  `part` [WAVES][N] is this row's and is used once between two
 // barriers: successive calls take turns at two of them.
-template <int WAVES>
-__device__ __forceinline__ void row_total(float& x, float& y, float (*part)[2])
+template <int WAVES, int N>
+__device__ __forceinline__ void row_totals(float (&v)[N], float (*part)[N])
 {
-    x = wave_total(x);
-    y = wave_total(y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_total(v[i]);
     if constexpr (WAVES > 1) {
         const uint32_t wave = (threadIdx.x >> 6) % WAVES;
         if ((threadIdx.x & 63) == 0) {
-            part[wave][0] = x;
-            part[wave][1] = y;
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[wave][i] = v[i];
         }
         __syncthreads();
-        x = part[0][0];
-        y = part[0][1];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) {
-            x += part[w][0];
-            y += part[w][1];
-        }
+        for (int i = 0; i < N; ++i) v[i] = part[0][i];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += part[w][i];
     }
+}
+
+template <int WAVES>
+__device__ __forceinline__ void row_total(float& x, float& y, float (*part)[2])
+{
+    float v[2] = {x, y};
+    row_totals<WAVES>(v, part);
+    x = v[0];
+    y = v[1];
 }
 
 template <int WAVES>

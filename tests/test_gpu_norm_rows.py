@@ -1,10 +1,10 @@
-"""The backward pass of layer norm on rows without deviations: every kernel, columns that fill what a workgroup holds and columns that do
-not.  Against 64 bits, with tolerances counted from the roundings (layer_common)."""
+"""The backward pass of layer norm on rows whose mean is far above their deviations, and on rows without any: every kernel, columns that fill what a
+workgroup holds and columns that do not.  Against 64 bits, with tolerances counted from the roundings (layer_common)."""
 import pytest
 import torch
 
 from paper_2402_01798_amd import binding as B
-from layer_common import HALF_ULP, TYPES, U, norm_forward, norm_sums
+from layer_common import HALF_ULP, TYPES, U, norm_backward, norm_backward_bounds, norm_forward, norm_sums, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,44 @@ def test_equal_elements(rows, cols, dtype, value, eps):
     turns = rows_in_turn(rows, cols)
     sums = dy.double().sum(dim=0)
     assert ((db.double() - sums).abs() <= (turns + 4) * U * dy.double().abs().sum(dim=0) + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("rows, cols", [s for s in SHAPES if s[1] > 1])
+@pytest.mark.parametrize("dtype, mean", [("f32", 2.0 ** 10), ("f32", 1e5), ("f32", -3e5), ("bf16", 100.0), ("f16", 1000.0)])
+def test_a_mean_far_above_the_deviations(rows, cols, dtype, mean):
+    """The statistics hold the mean as one binary32 number, up to 2^-24 |mean| from what it is; dx and dweight are those of the mean itself.
+    With d that difference over the deviation, at most 2^-5 here, h before its own mean is taken out is off by (k / 2 + 6) u (|h| + d), its mean by
+    (k + 2) u (1 + d), for mean |h| <= 1, and the difference by u |h|: together less than the bounds' (k / 2 + 8) u |h| + k u and another 6 u."""
+    g = torch.Generator().manual_seed(cols + 1)
+    x = (torch.randn(rows, cols, generator=g) + mean * (1 + 0.01 * torch.rand(rows, 1, generator=g))).to(TYPES[dtype])
+    dy = (torch.randn(rows, cols, generator=g) * 0.1).to(TYPES[dtype])
+    w = 1 + 0.3 * torch.randn(cols, generator=g)
+    X, DY, W = strided(x, 3, 1), strided(dy, 1, 0), w.cuda()
+    dx, dw, db = backward(X, DY, W, statistics(X, W, 1e-5))
+    x64, dy64, w64 = X.double(), DY.double(), W.double()
+    _, h, m, r = norm_forward(x64, w64, None, 1e-5)
+    assert float((m.abs() * r).max()) * U <= 2.0 ** -5
+    want = norm_backward(dy64, h, w64, r)
+    bounds = norm_backward_bounds(x64, dy64, h, w64, 3 / r, r, dtype, rows_in_turn(rows, cols))       # 2 * mean * r * u: another 6 u
+    for name, got, t, far in zip(("dx", "dweight", "dbias"), (dx, dw, db), want, bounds):
+        worst = ((got.double() - t).abs() / far).max()
+        assert worst <= 1, (name, float(worst))
+
+
+@pytest.mark.parametrize("cols", [40, 900, 5000, 16001, 17003, 32768, 33001])
+def test_some_of_the_gradients_and_in_place(cols):
+    """Whatever is asked for and wherever it goes, the same bits."""
+    g = torch.Generator().manual_seed(cols)
+    x = (torch.randn(300, cols, generator=g) + 5000.0).cuda()
+    dy, w = torch.randn(300, cols, generator=g).cuda(), torch.randn(cols, generator=g).cuda()
+    stats = statistics(x, w, 1e-5)
+    dx, dw, db = backward(x, dy, w, stats)
+    _, dw2, db2 = backward(x, dy, w, stats, None)
+    assert torch.equal(dw2, dw) and torch.equal(db2, db)
+    only = torch.empty_like(x)
+    B.tq_layernorm_backward(x, dy, w, stats, only)
+    assert torch.equal(only, dx)
+    for place in ("x", "dy"):
+        held = {"x": x.clone(), "dy": dy.clone()}
+        got = backward(held["x"], held["dy"], w, stats, held[place])
+        assert all(torch.equal(a, b) for a, b in zip(got, (dx, dw, db)))
