@@ -240,15 +240,11 @@ def _prepare_own(s):
         s["ws"] = workspace(tq.i8_linear_workspace_bytes(m, n, k))
     elif op == "orth":
         s["out"] = torch.empty_like(s["g"])
-        s["ws"] = workspace(tq.orthogonalize_workspace_bytes(case["rows"], case["cols"], 1, _precision(tq, case["dtype"])))
+        s["ws"] = workspace(tq.orthogonalize_workspace_bytes(case["rows"], case["cols"], 1, tq.ORTH_SPLIT))
     else:
         s["new_velocities"] = [torch.empty_like(v) for v in s["velocities"]]
         s["new_thetas"] = [torch.empty_like(t) for t in s["thetas"]]
         s["ws"] = workspace(tq.orthogonalize_workspace_bytes(case["rows"], case["cols"], case["count"], tq.ORTH_SPLIT))
-
-
-def _precision(tq, dtype):
-    return tq.ORTH_SPLIT if dtype == "f32" else tq.ORTH_HALF
 
 
 def _scale(case):
@@ -279,7 +275,7 @@ def _run_own(s):
     if op == "linear":
         return tq.tq_i8_linear(s["x"], s["w"], s["out"], s["ws"], bias=s["bias"])
     if op == "orth":
-        return tq.tq_orthogonalize(s["g"], s["out"], s["ws"], steps=STEPS, precision=_precision(tq, case["dtype"]), eps=EPS)
+        return tq.tq_orthogonalize(s["g"], s["out"], s["ws"], steps=STEPS, precision=tq.ORTH_SPLIT, eps=EPS)
     tq.tq_orthogonal_update_multi(s["gs"], s["velocities"], s["thetas"], s["ws"], eta=ETA, momentum=MOMENTUM, nesterov=True,
                                   weight_decay=DECAY, scale=_scale(case), steps=STEPS, precision=tq.ORTH_SPLIT, eps=EPS,
                                   velocities_out=s["new_velocities"], thetas_out=s["new_thetas"])
