@@ -46,7 +46,7 @@ def build(force: bool = False, extra_flags=(), verbose: bool = False, lib: str =
                      os.path.join(CSRC, "tq_mx_device.h")]
     layer_headers = learn_headers[:1] + learn_headers[2:] + \
         [os.path.join(ROOT, "include", h) for h in ("tq_norm.h", "tq_i8.h", "tq_orth.h")] + \
-        [os.path.join(CSRC, h) for h in ("tq_reduce.h", "tq_i8_device.h", "tq_tiles.h")]
+        [os.path.join(CSRC, h) for h in ("tq_reduce.h", "tq_i8_device.h", "tq_tiles.h", "tq_shapes.h")]
 
     def compile_one(src):
         s = os.path.join(CSRC, src)

@@ -11,6 +11,9 @@
 #include "tq_tiles.h"
 
 namespace tq {
+
+using namespace orth;
+
 namespace {
 
 constexpr float kUnit = 4096.0f;               // what elements in binary16 are held times
@@ -593,52 +596,6 @@ struct OrthCall {
     float eps, eta, momentum, weight_decay, scale;
     char* workspace;
 };
-
-// Tiles of a product: their sides, the time in ns that a group of k took while 1, 2, .. of them, as many as fit, were at work on every compute
-// unit, and what a round of them costs beside that (both transposes are written).  `alone`: five buffers in place of two, one workgroup on a
-// unit.  Kernel times of products, us, * the rule's:
-//                                                        256     192     128   128 alone   64
-//   binary16  4096^3, symmetric                         110    * 92     122     127       160
-//   binary16  4096^3                                  * 131     177     164     180       235
-//   binary16  512 x 512 x 2048, symmetric                46      26      21      18     * 11.5
-//   binary16  512 x 2048 x 512                           23      15      11      11     *  8.5
-//   pairs     2048^3, symmetric                         111      71      55    * 52        55
-//   pairs     2048^3                                    117      78      63    * 62        82
-//   pairs     4 of 1024 x 1024 x 4096, symmetric        213     140     108    * 95       102
-//   pairs     4 of 1024 x 4096 x 1024                 * 104     156     117     137       166
-//   pairs     784 x 1000 x 784                           56      34      23      20     * 11
-// k in two or four parts by more wavefronts of a workgroup took longer than tiles of 64 by one set of them everywhere (784 x 1000: 13).
-enum Shape { k256, k192, k128, k128Alone, k64 };
-struct Pace {
-    Shape shape;
-    uint64_t side;
-    uint32_t ns[3], round;
-};
-constexpr Pace kPaces[2][5] = {
-    {{k256, 256, {1553, 0, 0}, 25000}, {k192, 192, {943, 0, 0}, 20000}, {k128, 128, {580, 925, 0}, 12000}, {k128Alone, 128, {540, 0, 0}, 12000}, {k64, 64, {262, 375, 560}, 5000}},
-    {{k256, 256, {1900, 0, 0}, 40000}, {k192, 192, {1100, 0, 0}, 24000}, {k128, 128, {800, 1200, 0}, 15000}, {k128Alone, 128, {730, 0, 0}, 12000}, {k64, 64, {270, 450, 770}, 5000}}};
-
-uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side, bool below)
-{
-    const uint64_t y = (m + side - 1) / side, x = (n + side - 1) / side;
-    return below ? y * (y + 1) / 2 : x * y;
-}
-
-Shape shape_of(int kind, uint64_t m, uint64_t n, uint64_t k, bool below, uint64_t count)
-{
-    const Pace* best = nullptr;
-    uint64_t least = ~0ull;
-    for (const Pace& p : kPaces[kind == kHalfPair]) {
-        const uint64_t each = (tiles_of(m, n, p.side, below) * count + kComputeUnits - 1) / kComputeUnits, groups = (k + in_group(kind) - 1) / in_group(kind);
-        const uint64_t fit = p.ns[2] ? 3 : p.ns[1] ? 2 : 1, rest = each % fit;
-        const uint64_t t = each / fit * (p.ns[fit - 1] * groups + p.round) + (rest ? p.ns[rest - 1] * groups + p.round : 0);
-        if (t < least) {
-            least = t;
-            best = &p;
-        }
-    }
-    return best->shape;
-}
 
 template <int KIND, typename F>
 hipError_t by_shape(const StepArgs& s, bool below, int count, F f)

@@ -5,16 +5,11 @@
 #include <type_traits>
 
 #include "tq_mx_device.h"
+#include "tq_shapes.h"
 
 namespace tq {
 
-constexpr uint64_t kComputeUnits = 256, kLdsBytes = 160 << 10;
-
-// What a group of 128 bytes holds.  kHalfPair: elements as the sum of two binary16 numbers, 16 larger ones and the 16 smaller ones that go with
-// them, twice.
-enum { kInt8, kHalf, kHalfPair };
-
-constexpr __host__ __device__ uint32_t in_group(int kind) { return kind == kInt8 ? 128u : kind == kHalf ? 64u : 32u; }
+constexpr uint64_t kLdsBytes = 160 << 10;
 
 typedef int tile_i32x4 __attribute__((ext_vector_type(4)));
 typedef int tile_i32x16 __attribute__((ext_vector_type(16)));
