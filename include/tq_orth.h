@@ -18,7 +18,8 @@
  *   precision      TQ_ORTH_SPLIT: operands of the products are held as the sum of two binary16 numbers, 22 bits, with 32-bit sums: the
  *                  accuracy of binary32 arithmetic.  TQ_ORTH_HALF: as one binary16 number, at a third of the multiplications: each
  *                  rounding is 2^-12 of the matrix (in its 2-norm, evenly over all directions), which steps that lift small singular
- *                  values lift with them.  For matrices of random numbers the result is about 1e-3 off, half a step of bf16;
+ *                  values lift with them.  For matrices of random numbers the result is 1.1e-3 to 1.4e-3 of its norm off, less than
+ *                  a bf16 result's own rounding (1.7e-3) but six times an fp16 result's (2e-4), beside which that of TQ_ORTH_SPLIT does not show;
  *                  where directions that are k times below the largest matter, k times as much relative to those.
  *                  Either way an element of X below 2^-26 has fewer bits, and one below 2^-37 none: a matrix with |U|_F below
  *                  about 2^-20 eps loses what eps left of it.

@@ -142,3 +142,14 @@ def test_results_of_16_bits_as_pairs_lose_their_own_rounding_only(rows, cols, dt
     off.add(got - rounded)
     far = norm * 2 * HALF_ULP[dtype] * float(want.norm())
     assert off.square <= far and far < float((rounded - want).norm()) ** 2
+
+
+@pytest.mark.parametrize("rows, cols", [(64, 256), (300, 140), (784, 1000), (1024, 1024)])
+def test_what_binary16_operands_cost(rows, cols):
+    """As tq_orth.h says: more than the rounding of an fp16 result, less than that of a bf16 result."""
+    gs = matrices(rows, cols, 1, rows + 1)
+    want = references(gs, 5, "half")[0][0]
+    off = float((run(gs, "half")[0].double() - want).norm() / want.norm())
+    for dtype in ("bf16", "f16"):
+        rounding = float((want.to(TYPES[dtype]).double() - want).norm() / want.norm())
+        assert (off < rounding) == (dtype == "bf16")
