@@ -82,17 +82,17 @@ __global__ __launch_bounds__(256) void i8_join_kernel(I8MatmulArgs g)
     store_scaled<DTYPE>(g, (uint32_t)row, col, sums);
 }
 
-// Few rows of A, FRAGS x 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds it.
+// Few rows of A, 32 at most, against 32 rows of B, WAVES wavefronts over parts of k: serving, where B is read once and bounds it.
 // B comes through a ring of STAGES buffers for each wavefront, 128 bytes of k at a time.  A, by HOW: in the same ring (kStream); whole into
 // LDS, where it is small (kKept); or cast there by every workgroup, from type HOW (0 ..).
 enum { kStream = -2, kKept = -1 };
 
-template <int HOW, int FRAGS, int WAVES, int STAGES>
+template <int HOW, int WAVES, int STAGES>
 struct Few {
-    static constexpr int kBlocksA = HOW == kStream ? FRAGS : 0;    // blocks of 32 rows in a buffer, A's before B's
+    static constexpr int kBlocksA = HOW == kStream ? 1 : 0;        // blocks of 32 rows in a buffer, A's before B's
     static constexpr int kStage = (kBlocksA + 1) * 4096, kLoads = (kBlocksA + 1) * 4;
-    static constexpr int kRing = WAVES * STAGES * kStage, kSums = WAVES * FRAGS * 32 * 33 * 4;
-    static_assert(kRing <= (int)kLdsBytes && (HOW == kStream || FRAGS == 1), "rows that are kept are few");
+    static constexpr int kRing = WAVES * STAGES * kStage, kSums = WAVES * 32 * 33 * 4;
+    static_assert(kRing <= (int)kLdsBytes, "rings");
 };
 
 __host__ __device__ constexpr uint64_t kept_row(uint64_t groups) { return groups * 128 + 16; }    // 16 more: rows in different banks
@@ -100,11 +100,11 @@ __host__ __device__ constexpr uint64_t kept_row(uint64_t groups) { return groups
 template <class S>
 constexpr uint64_t few_bytes(uint64_t kept) { return S::kRing + kept > (uint64_t)S::kSums ? S::kRing + kept : S::kSums; }
 
-template <int DTYPE, int HOW, int FRAGS, int WAVES, int STAGES>
+template <int DTYPE, int HOW, int WAVES, int STAGES>
 __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
 {
 #ifdef __HIP_DEVICE_COMPILE__                                      // the host's pass does not know the type of a buffer
-    using S = Few<HOW, FRAGS, WAVES, STAGES>;
+    using S = Few<HOW, WAVES, STAGES>;
     using P = TileProduct<kInt8>;
     extern __shared__ char lds[];
     const uint32_t tx = linear_block();
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
     for (int i = 0; i < S::kLoads; ++i) {
         const bool is_a = i < 4 * S::kBlocksA;
         const uint32_t row = (is_a ? i : i - 4 * S::kBlocksA) * 8 + lane / 8;
-        from[i] = min(row, (is_a ? g.m : g.n - col0) - 1) * (uint32_t)stride + ((lane & 7) ^ tile_turn<128>(i * 8 + lane / 8)) * 16;
+        from[i] = min(row, (is_a ? g.m : g.n - col0) - 1) * (uint32_t)stride + ((lane & 7) ^ tile_turn(i * 8 + lane / 8)) * 16;
     }
     const uint32_t turned = trips ? tx % trips : 0;                // workgroups begin at different places
     auto group_of = [&](uint32_t t) { return first + (t + turned < trips ? t + turned : t + turned - trips); };
@@ -191,36 +191,29 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
     }
 
     const char* mine = kept + min(r, g.m - 1) * kept_row(g.groups) + half * 16;
-    P::Sums acc[FRAGS];
+    P::Sums acc;
 #pragma unroll
-    for (int f = 0; f < FRAGS; ++f)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[f][e] = 0;
+    for (int e = 0; e < 16; ++e) acc[e] = 0;
     uint32_t stage = 0;
     for (uint32_t t = 0; t < trips; ++t) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(S::kLoads * (STAGES - 1)) : "memory");
         const char* base = ring + stage * S::kStage;
-        tile_i32x4 a[FRAGS][4], b[4];
+        tile_i32x4 a[4], b[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const uint32_t at = r * 128 + ((2 * s + half) ^ tile_turn<128>(r)) * 16;
+            const uint32_t at = r * 128 + ((2 * s + half) ^ tile_turn(r)) * 16;
             b[s] = *reinterpret_cast<const tile_i32x4*>(base + S::kBlocksA * 4096 + at);
-#pragma unroll
-            for (int f = 0; f < FRAGS; ++f)
-                a[f][s] = *reinterpret_cast<const tile_i32x4*>(HOW == kStream ? base + f * 4096 + at : mine + group_of(t) * 128 + s * 32);
+            a[s] = *reinterpret_cast<const tile_i32x4*>(HOW == kStream ? base + at : mine + group_of(t) * 128 + s * 32);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the buffer is read: it may be filled again
         fetch(t + STAGES, stage);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int f = 0; f < FRAGS; ++f) acc[f] = P::step(a[f][s], b[s], acc[f]);
+        for (int s = 0; s < 4; ++s) acc = P::step(a[s], b[s], acc);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    float scales[4 * FRAGS];                                       // of the rows that this thread joins below
-    constexpr int kEach = FRAGS * 32 * 32 / (WAVES * 64);
-    static_assert(kEach <= 4 * FRAGS, "outputs of a thread");
+    constexpr int kEach = 32 * 32 / (WAVES * 64);                  // outputs of a thread
+    float scales[kEach];                                           // of the rows that it joins below
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
         const uint32_t row = min((threadIdx.x + u * WAVES * 64) / 32, g.m - 1);
@@ -229,9 +222,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
     __syncthreads();                                               // the rings and what is kept behind them are done with
     int* sums = reinterpret_cast<int*>(lds);
 #pragma unroll
-    for (int f = 0; f < FRAGS; ++f)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sums[((wave * FRAGS + f) * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[f][e];
+    for (int e = 0; e < 16; ++e) sums[(wave * 32 + (e / 4) * 8 + half * 4 + e % 4) * 33 + r] = acc[e];
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
@@ -239,7 +230,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8MatmulArgs g)
         if (row >= g.m || col0 + col >= g.n) continue;
         int sum = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += sums[(w * FRAGS * 32 + row) * 33 + col];
+        for (int w = 0; w < WAVES; ++w) sum += sums[(w * 32 + row) * 33 + col];
         float v = (float)sum * scales[u] * g.sb[col0 + col];
         if (g.bias) v += g.bias[col0 + col];
         static_cast<typename Element<DTYPE>::type*>(g.out)[row * g.ldo + col0 + col] = Element<DTYPE>::store(v);
@@ -260,15 +251,15 @@ hipError_t launch_tiles(I8MatmulArgs& g, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DTYPE, int HOW, int FRAGS, int WAVES, int STAGES>
+template <int DTYPE, int HOW, int WAVES, int STAGES>
 hipError_t launch_few(I8MatmulArgs& g, hipStream_t st)
 {
-    using S = Few<HOW, FRAGS, WAVES, STAGES>;
+    using S = Few<HOW, WAVES, STAGES>;
     g.tiles = (g.n + 31) / 32;
     dim3 grid;
     if (!fold_grid(g.tiles, WAVES * 64, 1, grid)) return hipErrorInvalidValue;
     const uint64_t kept = HOW == kStream ? 0 : g.m * kept_row(g.groups) + g.m * 4;
-    i8_few_kernel<DTYPE, HOW, FRAGS, WAVES, STAGES><<<grid, WAVES * 64, few_bytes<S>(kept), st>>>(g);
+    i8_few_kernel<DTYPE, HOW, WAVES, STAGES><<<grid, WAVES * 64, few_bytes<S>(kept), st>>>(g);
     return hipGetLastError();
 }
 
@@ -295,18 +286,18 @@ hipError_t launch_matmul(I8MatmulArgs& g, hipStream_t st)
     switch (shape_of(g.m, g.n, g.groups)) {
         case kFewShape:
             if (g.m * kept_row(g.groups) <= kKeptBytes)
-                return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kKept, 1, 8, 2>(g, st) : launch_few<DTYPE, kKept, 1, 4, 3>(g, st);
-            return launch_few<DTYPE, kStream, 1, 4, 2>(g, st);
-        case k256: return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 4, 128, 2>>(g, st);
-        case k192: return launch_tiles<DTYPE, TileShape<kInt8, 192, 192, 2, 6, 128, 3>>(g, st);
-        case k256x128: return launch_tiles<DTYPE, TileShape<kInt8, 256, 128, 4, 2, 128, 3>>(g, st);
-        case k192x256: return launch_tiles<DTYPE, TileShape<kInt8, 192, 256, 2, 4, 128, 2>>(g, st);
-        case k128x320: return launch_tiles<DTYPE, TileShape<kInt8, 128, 320, 4, 2, 128, 2>>(g, st);
-        case k128x256: return launch_tiles<DTYPE, TileShape<kInt8, 128, 256, 2, 4, 128, 3>>(g, st);
-        case k128: return launch_tiles<DTYPE, TileShape<kInt8, 128, 128, 2, 4, 128, 2>>(g, st);
+                return g.n <= 32 * kComputeUnits ? launch_few<DTYPE, kKept, 8, 2>(g, st) : launch_few<DTYPE, kKept, 4, 3>(g, st);
+            return launch_few<DTYPE, kStream, 4, 2>(g, st);
+        case k256: return launch_tiles<DTYPE, TileShape<kInt8, 256, 256, 2, 4, 2>>(g, st);
+        case k192: return launch_tiles<DTYPE, TileShape<kInt8, 192, 192, 2, 6, 3>>(g, st);
+        case k256x128: return launch_tiles<DTYPE, TileShape<kInt8, 256, 128, 4, 2, 3>>(g, st);
+        case k192x256: return launch_tiles<DTYPE, TileShape<kInt8, 192, 256, 2, 4, 2>>(g, st);
+        case k128x320: return launch_tiles<DTYPE, TileShape<kInt8, 128, 320, 4, 2, 2>>(g, st);
+        case k128x256: return launch_tiles<DTYPE, TileShape<kInt8, 128, 256, 2, 4, 3>>(g, st);
+        case k128: return launch_tiles<DTYPE, TileShape<kInt8, 128, 128, 2, 4, 2>>(g, st);
         case k64: break;
     }
-    const hipError_t e = launch_tiles<DTYPE, TileShape<kInt8, 64, 64, 2, 2, 128, 3>>(g, st);
+    const hipError_t e = launch_tiles<DTYPE, TileShape<kInt8, 64, 64, 2, 2, 3>>(g, st);
     if (e != hipSuccess || g.splits == 1) return e;
     dim3 grid;
     if (!fold_grid(((uint64_t)g.m * ((g.n + 7) / 8) + 255) / 256, 256, 1, grid)) return hipErrorInvalidValue;
@@ -367,7 +358,7 @@ hipError_t tq_launch_i8_linear_few(const void* x, int x_dtype, uint64_t m, uint6
     g.groups = (uint32_t)((k + 127) / 128);
     auto as = [&](auto D, auto X) {
         constexpr int T = decltype(D)::value, F = decltype(X)::value;
-        return g.n <= 32 * kComputeUnits ? launch_few<T, F, 1, 8, 2>(g, st) : launch_few<T, F, 1, 4, 3>(g, st);
+        return g.n <= 32 * kComputeUnits ? launch_few<T, F, 8, 2>(g, st) : launch_few<T, F, 4, 3>(g, st);
     };
     auto from = [&](auto D) {
         if (x_dtype == TQ_F32) return as(D, std::integral_constant<int, TQ_F32>{});

@@ -601,11 +601,11 @@ template <int KIND, typename F>
 hipError_t by_shape(const StepArgs& s, bool below, int count, F f)
 {
     switch (shape_of(KIND, s.m, s.n, s.k, below, (uint64_t)count)) {
-        case k256: return f(TileShape<KIND, 256, 256, 2, 4, 128, 2>{});
-        case k192: return f(TileShape<KIND, 192, 192, 2, 6, 128, 3>{});
-        case k128: return f(TileShape<KIND, 128, 128, 2, 4, 128, 2>{});
-        case k128Alone: return f(TileShape<KIND, 128, 128, 2, 4, 128, 5>{});
-        case k64: return f(TileShape<KIND, 64, 64, 2, 2, 128, 3>{});
+        case k256: return f(TileShape<KIND, 256, 256, 2, 4, 2>{});
+        case k192: return f(TileShape<KIND, 192, 192, 2, 6, 3>{});
+        case k128: return f(TileShape<KIND, 128, 128, 2, 4, 2>{});
+        case k128Alone: return f(TileShape<KIND, 128, 128, 2, 4, 5>{});
+        case k64: return f(TileShape<KIND, 64, 64, 2, 2, 3>{});
     }
     return hipErrorInvalidValue;
 }

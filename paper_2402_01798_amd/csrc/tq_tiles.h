@@ -10,6 +10,7 @@
 namespace tq {
 
 constexpr uint64_t kLdsBytes = 160 << 10;
+constexpr int kGroupBytes = 128;
 
 typedef int tile_i32x4 __attribute__((ext_vector_type(4)));
 typedef int tile_i32x16 __attribute__((ext_vector_type(16)));
@@ -35,24 +36,23 @@ struct TileProduct<kInt8> {
     }
 };
 
-// BM x BN outputs by WM x WN wavefronts, a slice of ROW bytes of k at a time through a ring of STAGES buffers in LDS: BM rows of A, then BN
-// of B.
-template <int KIND_, int BM_, int BN_, int WM_, int WN_, int ROW_, int STAGES_>
+// BM x BN outputs by WM x WN wavefronts, a group of k at a time through a ring of STAGES buffers in LDS: BM rows of A, then BN of B.
+template <int KIND_, int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct TileShape {
-    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, ROW = ROW_, STAGES = STAGES_;
+    static constexpr int KIND = KIND_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     using Product = TileProduct<KIND>;
     using Sums = typename Product::Sums;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int kFragsM = BM / WM / 32, kFragsN = BN / WN / 32;
-    static constexpr int kStage = (BM + BN) * ROW, kBytes = STAGES * kStage;
-    static constexpr int kPieces = ROW / 16, kRows = 64 / kPieces; // rows that a request of a wavefront covers
+    static constexpr int kStage = (BM + BN) * kGroupBytes, kBytes = STAGES * kStage;
+    static constexpr int kPieces = kGroupBytes / 16, kRows = 64 / kPieces;  // rows that a request of a wavefront covers
     static constexpr int kLoadsA = BM / kRows / kWaves, kLoads = (BM + BN) / kRows / kWaves;   // requests of a wavefront for a buffer
     static constexpr int kOnUnit = (int)kLdsBytes / kBytes;        // workgroups on a compute unit
     static constexpr int kOnSimd = kOnUnit * kWaves / 4 < 1 ? 1 : kOnUnit * kWaves / 4 > 4 ? 4 : kOnUnit * kWaves / 4;      // wavefronts
     static constexpr bool kPair = KIND == kHalfPair;
-    static constexpr int kStep = kPair ? 64 : 32, kSteps = ROW / kStep;        // bytes of a row that are multiplied at a time
+    static constexpr int kStep = kPair ? 64 : 32, kSteps = kGroupBytes / kStep; // bytes of a row that are multiplied at a time
     static constexpr int kReads = (kFragsM + kFragsN) * (kPair ? 2 : 1), kProducts = kFragsM * kFragsN * (kPair ? 3 : 1);     // of a step
-    static_assert((ROW == 64 || ROW == 128) && kSteps % 2 == 0, "operands are read into two sets of registers in turn");
+    static_assert(kSteps % 2 == 0, "operands are read into two sets of registers in turn");
     static_assert(BM / kRows % kWaves == 0 && BN / kRows % kWaves == 0 && kRows * kWaves % 16 == 0 && kBytes <= (int)kLdsBytes && STAGES >= 2,
                   "requests in equal numbers");
 };
@@ -65,8 +65,7 @@ struct TileOperands {
 
 // A row's pieces of 16 bytes lie in a buffer in another order from row to row: piece p of row r in place p ^ tile_turn(r), so that
 // 16 rows' pieces of the same k, which are read together, lie in 64 different banks.
-template <int ROW>
-__device__ __forceinline__ uint32_t tile_turn(uint32_t row) { return ROW == 128 ? row >> 1 & 7 : row >> 2 & 3; }
+__device__ __forceinline__ uint32_t tile_turn(uint32_t row) { return row >> 1 & 7; }
 
 // A step's operands in a wavefront's registers; of pairs, their second numbers too.
 template <class S>
@@ -80,8 +79,8 @@ struct TileFragments {
         constexpr int low = R / (S::kFragsM + S::kFragsN), r = R % (S::kFragsM + S::kFragsN);
         if constexpr (low) at ^= 32;
         if constexpr (r == 0) b[low][0] = *reinterpret_cast<const tile_i32x4*>(rows_b + at);
-        else if constexpr (r <= S::kFragsM) a[low][r - 1] = *reinterpret_cast<const tile_i32x4*>(rows_a + (r - 1) * 32 * S::ROW + at);
-        else b[low][r - S::kFragsM] = *reinterpret_cast<const tile_i32x4*>(rows_b + (r - S::kFragsM) * 32 * S::ROW + at);
+        else if constexpr (r <= S::kFragsM) a[low][r - 1] = *reinterpret_cast<const tile_i32x4*>(rows_a + (r - 1) * 32 * kGroupBytes + at);
+        else b[low][r - S::kFragsM] = *reinterpret_cast<const tile_i32x4*>(rows_b + (r - S::kFragsM) * 32 * kGroupBytes + at);
     }
     // The P-th of kProducts.  Of pairs (a + a')(b + b') but for a' b', which is 2^-22 of it.
     template <int P>
@@ -103,8 +102,8 @@ __device__ __forceinline__ void repeat(F f)
 
 // Sums of the tile at (row0, col0).  Rows past the end repeat the last: their sums mean nothing.  A lane holds of 32 x 32 outputs
 // one row's: element e is column (e / 4) * 8 + (lane / 32) * 4 + e % 4 of row lane % 32.
-// A step's operands are read while the step before it is multiplied, one request behind a product; the first ones of the next slice in the
-// second half of a slice's last step, behind the barrier after which every wavefront is done with this slice's buffer.
+// A step's operands are read while the step before it is multiplied, one request behind a product; the first ones of the next group in the
+// second half of a group's last step, behind the barrier after which every wavefront is done with this group's buffer.
 template <class S>
 __device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, uint32_t col0, char* lds,
                                           typename S::Sums (&acc)[S::kFragsM][S::kFragsN])
@@ -114,24 +113,24 @@ __device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, 
     const uint32_t r = lane & 31, half = lane >> 5, wm = wave / S::WN, wn = wave % S::WN;
     row0 = __builtin_amdgcn_readfirstlane(row0);                   // the same in all lanes, which divisions hide from the compiler
     col0 = __builtin_amdgcn_readfirstlane(col0);
-    const uint64_t stride = (uint64_t)g.groups * 128;
-    const uint32_t trips = g.count * (128 / S::ROW);
+    const uint64_t stride = (uint64_t)g.groups * kGroupBytes;
+    const uint32_t trips = g.count;
     uint32_t from[S::kLoads];
-    const uint32_t piece = (lane % S::kPieces) ^ tile_turn<S::ROW>(wave * S::kRows + lane / S::kPieces);       // in each of a wavefront's requests
+    const uint32_t piece = (lane % S::kPieces) ^ tile_turn(wave * S::kRows + lane / S::kPieces);       // in each of a wavefront's requests
 #pragma unroll
     for (int i = 0; i < S::kLoads; ++i) {
         const bool is_a = i < S::kLoadsA;                          // A's rows first
         const uint32_t row = (i * S::kWaves + wave) * S::kRows - (is_a ? 0 : S::BM) + lane / S::kPieces;
         from[i] = min(row, (is_a ? g.m - row0 : g.n - col0) - 1) * (uint32_t)stride + piece * 16;
     }
-    // The slices behind the last are requested with a length of 0 in place of the operands': nothing is read, and every trip is alike.
+    // The groups behind the last are requested with a length of 0 in place of the operands': nothing is read, and every trip is alike.
     auto fetch_one = [&](auto I, uint32_t t, uint32_t stage) {
         constexpr int i = decltype(I)::value;
         // buffer addressing: a lane's place in the tile is a 32-bit number, and what all lanes share a scalar
         const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(i < S::kLoadsA ? g.a + row0 * stride : g.b + col0 * stride), 0,
                                                           __builtin_amdgcn_readfirstlane(t < trips ? -1 : 0), 0x20000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(of, (tile_lds_bytes*)(lds + stage * S::kStage + (i * S::kWaves + wave) * 1024), 16, from[i],
-                                                 g.first * 128 + t * S::ROW, 0, 0);
+                                                 (g.first + t) * kGroupBytes, 0, 0);
     };
 #pragma unroll
     for (uint32_t t = 0; t < S::STAGES; ++t) repeat<S::kLoads>([&](auto I) { fetch_one(I, t, t); });
@@ -141,8 +140,8 @@ __device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, 
         for (int j = 0; j < S::kFragsN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    const uint32_t rows_a = (wm * S::kFragsM * 32 + r) * S::ROW, rows_b = (S::BM + wn * S::kFragsN * 32 + r) * S::ROW;
-    const uint32_t first_piece = (half ^ tile_turn<S::ROW>(lane)) * 16;        // of step 0
+    const uint32_t rows_a = (wm * S::kFragsM * 32 + r) * kGroupBytes, rows_b = (S::BM + wn * S::kFragsN * 32 + r) * kGroupBytes;
+    const uint32_t first_piece = (half ^ tile_turn(lane)) * 16;      // of step 0
     auto read = [&](TileFragments<S>& f, auto R, const char* base, int s) {
         f.template read<decltype(R)::value>(base + rows_a, base + rows_b, first_piece ^ (S::kStep * s));
     };
@@ -170,7 +169,7 @@ __device__ __forceinline__ void tile_sums(const TileOperands& g, uint32_t row0, 
         const uint32_t next = stage + 1 == S::STAGES ? 0 : stage + 1;
         repeat<kHalfway>([&](auto P) { last.template product<decltype(P)::value>(acc); });
         __builtin_amdgcn_sched_barrier(0);
-        // the next slice is there, and every wavefront has read this one
+        // the next group is there, and every wavefront has read this one
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(S::kLoads * (S::STAGES - 2)) : "memory");
         const char* after = lds + next * S::kStage;
         repeat<kLeft>([&](auto Q) {
