@@ -15,8 +15,9 @@
  *   eps         at least 1e-30, finite
  * rows, cols = 1 .. 2^31 - 1, rows * ld* <= 2^40.
  *
- * Sums are binary32, of x around a first estimate of its mean, so that a mean far larger than the deviations costs no bits of
- * those, in either pass: the h that follows in the backward pass from m, which is one binary32 number, has its own mean taken out.
+ * Sums are binary32, along rows of more than 32768 columns binary64, of x around a first estimate of its mean, so that a mean far
+ * larger than the deviations costs no bits of those, in either pass: the h that follows in the backward pass from m, which is one
+ * binary32 number, has its own mean taken out.
  * Rows of any finite values have their result, also where squares would leave the range of binary32.  A row that holds a
  * NaN or an infinity has NaN for r and for all of y, dx, and, through them, dweight; no other row does.  A row of equal elements has h = 0.
  * The same call on the same device gives the same bits every time.

@@ -29,50 +29,53 @@ __device__ __forceinline__ int left_of(uint32_t cols, uint32_t oct)
 
 // A row's mean m, its rest c (m + c is nearer to the mean than m) and 1 / deviation, from passes over its elements:
 // each(f) calls f(value) for all of this thread's.  Where a square or a sum leaves binary32's range, once more in units of 2^80.
+// Sums are of type Sum: binary64 for rows that do not fit the registers, for a thread adds up cols / 1024 elements of those, whose roundings in binary32
+// would be seen (2^26 equal elements of 33000 had h = 1.5).
 struct RowStats {
     float unit;                                // x in units of 1 / unit
     float m, c, r;                             // of x * unit; (x * unit - m - c) * r = h
     float mean, rstd;                          // of x
 };
 
-template <int WAVES, typename Each>
-__device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, float (*part)[WAVES][2], Each each)
+template <int WAVES, typename Sum, typename Each>
+__device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, Sum (*part)[WAVES][2], Each each)
 {
-    const float n = (float)cols;
+    const Sum n = (Sum)cols;
     RowStats s;
     s.unit = 1.0f;
-    float sum = 0.0f, none = 0.0f;
+    Sum sum = 0, none = 0;
     each([&](float x) { sum += x; });
     row_total<WAVES>(sum, none, part[0]);
-    s.m = sum / n;
-    float d1 = 0.0f, d2 = 0.0f;
-    each([&](float x) {
-        const float d = x - s.m;
+    s.m = (float)(sum / n);
+    Sum d1 = 0, d2 = 0;
+    auto deviation = [&](float d) {
         d1 += d;
-        d2 = fmaf(d, d, d2);
-    });
+        if constexpr (std::is_same_v<Sum, float>) d2 = fmaf(d, d, d2);
+        else d2 = fma((double)d, (double)d, d2);
+    };
+    auto variance = [&]() {                    // around m + d1 / n
+        const Sum c = d1 / n;
+        s.c = (float)c;
+        if constexpr (std::is_same_v<Sum, float>) return fmaf(-c, c, d2 / n);
+        else return fma(-c, c, d2 / n);
+    };
+    each([&](float x) { deviation(x - s.m); });
     row_total<WAVES>(d1, d2, part[1]);
-    s.c = d1 / n;
-    const float var = fmaxf(fmaf(-s.c, s.c, d2 / n), 0.0f);
+    const float var = fmaxf((float)variance(), 0.0f);
     s.r = 1.0f / sqrtf(var + eps);
     s.mean = s.m + s.c;
     s.rstd = s.r;
-    if (!(d2 < __builtin_inff())) {            // the whole row's: all its threads take this turn
+    if (!((float)d2 < __builtin_inff())) {     // the whole row's: all its threads take this turn
         s.unit = 0x1p-80f;
-        sum = none = 0.0f;
+        sum = none = 0;
         each([&](float x) { sum += x * s.unit; });
         if constexpr (WAVES > 1) __syncthreads();                  // a wavefront with a row of its own goes on alone
         row_total<WAVES>(sum, none, part[0]);
-        s.m = sum / n;
-        d1 = d2 = 0.0f;
-        each([&](float x) {
-            const float d = x * s.unit - s.m;
-            d1 += d;
-            d2 = fmaf(d, d, d2);
-        });
+        s.m = (float)(sum / n);
+        d1 = d2 = 0;
+        each([&](float x) { deviation(x * s.unit - s.m); });
         row_total<WAVES>(d1, d2, part[1]);
-        s.c = d1 / n;
-        const double v = (double)fmaf(-s.c, s.c, d2 / n), r = 1.0 / sqrt((v > 0.0 || v != v ? v : 0.0) * 0x1p160 + (double)eps);
+        const double v = (double)variance(), r = 1.0 / sqrt((v > 0.0 || v != v ? v : 0.0) * 0x1p160 + (double)eps);
         s.r = (float)(r * 0x1p80);
         s.mean = (s.m + s.c) * 0x1p80f;
         s.rstd = (float)r;
@@ -146,13 +149,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_forward_ke
 
 constexpr int kLongWaves = 16;
 
-// Rows that do not fit the registers, by a workgroup each, read anew for every pass, from the caches if they are there: 1000 x 60000 bf16 72 us.
+// Rows that do not fit the registers, by a workgroup each, read anew for every pass, from the caches if they are there: 1000 x 60000 bf16 73 us.
 template <int DTYPE, int WTYPE>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_forward_long_kernel(NormArgs a)
 {
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
-    __shared__ float part[2][kLongWaves][2];
+    __shared__ double part[2][kLongWaves][2];
     const uint64_t row = linear_block();
     if (row >= a.rows) return;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
@@ -353,8 +356,9 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
 {
     using T = typename Element<DTYPE>::type;
     using W = typename Element<WTYPE>::type;
+    using Sum = std::conditional_t<V != 0, float, double>;         // as in row_stats
     constexpr uint32_t kThreads = kLongWaves * 64;
-    __shared__ float part[kLongWaves][3];
+    __shared__ Sum part[kLongWaves][3];
     const uint64_t row = linear_block();
     if (row >= a.rows) return;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
@@ -384,13 +388,15 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
         for (int j = 0; j < 8; ++j)
             if (a.weight) g[j] *= weight[j];
     };
-    float sum[3] = {}, s1 = 0.0f, s2 = 0.0f, d = 0.0f, h[8], g[8];     // sums of g, of g h and of h
+    Sum sum[3] = {};                                               // of g, of g h and of h
+    float s1 = 0.0f, s2 = 0.0f, d = 0.0f, h[8], g[8];
     auto add = [&](int i, uint32_t oct) {
         values(i, oct, h, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             sum[0] += g[j];
-            sum[1] = fmaf(g[j], h[j], sum[1]);
+            if constexpr (V != 0) sum[1] = fmaf(g[j], h[j], sum[1]);
+            else sum[1] = fma((double)g[j], (double)h[j], sum[1]);
             sum[2] += h[j];
         }
     };
@@ -414,9 +420,9 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
         }
     }
     row_totals<kLongWaves>(sum, part);
-    d = sum[2] / (float)a.cols;
-    s1 = sum[0] / (float)a.cols;
-    s2 = sum[1] / (float)a.cols - d * s1;
+    d = (float)(sum[2] / (Sum)a.cols);
+    s1 = (float)(sum[0] / (Sum)a.cols);
+    s2 = (float)(sum[1] / (Sum)a.cols) - d * s1;
     if (a.rest && threadIdx.x == 0) a.rest[row] = d;
     if constexpr (V > 0) {
 #pragma unroll
@@ -431,17 +437,17 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(Nor
 }
 
 // The mean of such a row's h alone, summed as above, bit for bit: where dx is not wanted, or takes the place of what norm_columns_kernel reads.
-template <int DTYPE>
+template <int DTYPE, typename Sum>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_rest_kernel(NormArgs a)
 {
     using T = typename Element<DTYPE>::type;
-    __shared__ float part[kLongWaves][1];
+    __shared__ Sum part[kLongWaves][1];
     const uint64_t row = linear_block();
     if (row >= a.rows) return;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     const float quarter = 0.25f * a.stats_in[2 * row], four = 4.0f * a.stats_in[2 * row + 1];
     const uint32_t octs = (uint32_t)(((uint64_t)a.cols + 7) / 8);
-    float sum[1] = {};
+    Sum sum[1] = {};
     for (uint32_t oct = threadIdx.x; oct < octs; oct += kLongWaves * 64) {
         const int n = left_of(a.cols, oct);
         float v[8], h[8];
@@ -451,7 +457,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_rest_kernel(NormArgs a)
         for (int j = 0; j < 8; ++j) sum[0] += h[j];
     }
     row_totals<kLongWaves>(sum, part);
-    if (threadIdx.x == 0) a.rest[row] = sum[0] / (float)a.cols;
+    if (threadIdx.x == 0) a.rest[row] = (float)(sum[0] / (Sum)a.cols);
 }
 
 // Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.  4096 x 32768 bf16 118 us, 4.5 TB/s.
@@ -633,7 +639,8 @@ hipError_t tq_launch_layernorm_backward(const void* x, int dtype, uint64_t rows,
                 if (apart) {
                     e = put_dx();
                 } else {
-                    norm_rest_kernel<kD><<<by_row, kLongWaves * 64, 0, st>>>(a);
+                    if (cols <= kMostForward) norm_rest_kernel<kD, float><<<by_row, kLongWaves * 64, 0, st>>>(a);
+                    else norm_rest_kernel<kD, double><<<by_row, kLongWaves * 64, 0, st>>>(a);
                     e = hipGetLastError();
                 }
                 if (e != hipSuccess) return e;

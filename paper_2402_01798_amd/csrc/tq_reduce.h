@@ -21,12 +21,19 @@ __device__ __forceinline__ float wave_total(float v)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+__device__ __forceinline__ double wave_total(double v)
+{
+#pragma unroll
+    for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
 __device__ __forceinline__ uint32_t wave_largest(uint32_t v) { return stride16_max(row16_max(v)); }
 
 // Of N values over the WAVES wavefronts of a row, in a fixed order.  `part` [WAVES][N] is this row's and is used once between two
 // barriers: successive calls take turns at two of them.
-template <int WAVES, int N>
-__device__ __forceinline__ void row_totals(float (&v)[N], float (*part)[N])
+template <int WAVES, int N, typename Sum>
+__device__ __forceinline__ void row_totals(Sum (&v)[N], Sum (*part)[N])
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_total(v[i]);
@@ -46,10 +53,10 @@ __device__ __forceinline__ void row_totals(float (&v)[N], float (*part)[N])
     }
 }
 
-template <int WAVES>
-__device__ __forceinline__ void row_total(float& x, float& y, float (*part)[2])
+template <int WAVES, typename Sum>
+__device__ __forceinline__ void row_total(Sum& x, Sum& y, Sum (*part)[2])
 {
-    float v[2] = {x, y};
+    Sum v[2] = {x, y};
     row_totals<WAVES>(v, part);
     x = v[0];
     y = v[1];
