@@ -15,7 +15,8 @@ struct I8CastArgs {
 };
 
 // A row by WAVES wavefronts; V > 0: it stays in their registers, 8 V elements a lane, else it is read twice.  Short rows four to a workgroup.
-// Memory: 2056 x 4097 fp32 10 us, 4.2 TB/s, rows at odd addresses.
+// Memory: 2056 x 4097 fp32 10 us, 4.2 TB/s; 4104 columns, whose rows begin at multiples of 32 bytes, 0.5 us less, 4096, two eights a lane in place of
+// three, 1.7 less.
 template <int DTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void i8_cast_kernel(I8CastArgs a)
 {
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void i8_cast_kernel(I
     }
 }
 
-// 2056 x 4097 to fp32 12 us, 3.4 TB/s.
+// 2056 x 4097 to fp32 12 us, 3.4 TB/s, and no less to rows at multiples of 32 bytes.
 struct I8ValuesArgs {
     const int8_t* codes;
     const float* scales;

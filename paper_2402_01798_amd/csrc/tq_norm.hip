@@ -84,7 +84,7 @@ __device__ __forceinline__ RowStats row_stats(uint32_t cols, float eps, Sum (*pa
 }
 
 // A row by WAVES wavefronts that hold it in registers, 8 V elements each lane; short rows several to a workgroup.  Read once, written once:
-// memory bounds it (16384 x 4096 bf16 57 us, 4.7 TB/s; 4096 x 32768 130), a launch where there are few rows (1 x 4096 3.2).
+// memory bounds it (16384 x 4096 bf16 57 to 62 us, 4.5 TB/s; 4096 x 32768 122), a launch where there are few rows (1 x 4096 3.2).
 template <int DTYPE, int WTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_forward_kernel(NormArgs a)
 {
@@ -210,7 +210,7 @@ __device__ __forceinline__ void deviations(const float (&x)[8], int n, float qua
 }
 
 // dx of a row and the sums over rows: a workgroup's wavefronts hold WAVES to a row, 8 V columns to a lane, and take rows one after the
-// other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.  16384 x 4096 bf16 78 us, 5.2 TB/s:
+// other, the next row's elements on their way meanwhile; their sums over rows are joined at the end.  16384 x 4096 bf16 77 to 83 us, 5.0 TB/s:
 // memory; without the next row's requests, with weights read for every row and twice the parts, 127.
 template <int DTYPE, int WTYPE, int WAVES, int V>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_kernel(NormArgs a)
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void norm_backward_k
 }
 
 // dx of a row whose sums over rows are left to norm_columns_kernel: held in registers (V > 0, 8 V elements a lane) or read twice.  4096 x 32768
-// bf16 207 / 213 us (3.9 TB/s); two workgroups on a unit, whose registers then spill, 266.
+// bf16 225 us (3.6 TB/s), 213 without the sum of h; two workgroups on a unit, whose registers then spill, 266.
 template <int DTYPE, int WTYPE, int V>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_backward_long_kernel(NormArgs a)
 {
@@ -460,7 +460,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_rest_kernel(NormArgs a)
     if (threadIdx.x == 0) a.rest[row] = (float)(sum[0] / (Sum)a.cols);
 }
 
-// Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.  4096 x 32768 bf16 118 us, 4.5 TB/s.
+// Sums over the rows of such a matrix: a thread takes 8 columns of every parts-th row.  4096 x 32768 bf16 112 us, 4.8 TB/s.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, uint32_t across)
 {
@@ -510,10 +510,10 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
 
 // The wavefronts of a row and the elements of a lane in eighths, for rows of up to 512 WAVES V elements.  From 513 to 1024 columns forward and
 // backward pass take, by one / two / four wavefronts a row, us:
-//   300 x 1024 bf16      17.4   12.4   12.7        16384 x 1024 bf16   48.6   50.2   60
-//   1000 x 600 fp32      20.7   15.4   15.5        65536 x 700 bf16     148    243
-//   4099 x 1001 fp32     34.8   28.6   30.2        16384 x 1024 fp32   73.1   59.9
-//   4096 x 1024 bf16     24.6   21.3   25.0        65536 x 1024 fp32    290    245
+//   300 x 1024 bf16      16.1   10.8   11.0        16384 x 1024 bf16   46.5   51.3   61.0
+//   1000 x 600 fp32      20.3   14.1   14.6        65536 x 700 bf16     167    280    334
+//   4099 x 1001 fp32     37.1   30.7   31.6        16384 x 1024 fp32   84.2   60.2   65.5
+//   4096 x 1024 bf16     24.7   21.7   25.1        65536 x 1024 fp32    293    246    257
 // Few rows want many wavefronts; many rows no barriers, if a wavefront has a row's two times 2 KiB on their way and the next row's.
 bool wave_a_row(uint64_t rows, uint64_t cols, int dtype) { return cols <= 512 || (cols <= 1024 && dtype != TQ_F32 && rows >= 8192); }
 
